@@ -344,6 +344,85 @@ meteora_status meteora_base_gemm(const void* x, const void* W, int T, int d_in, 
                                  meteora_dtype dt, void* out /*[T,d_out]*/, meteora_stream stream);
 
 /*
+ * Rows as 8-bit whole numbers with one scale each: the tokens of an activation, or the output channels of a weight
+ * W[d_out, d_in] (its rows).  With a = max_i |x[t,i]|:
+ *   scale[t] = a / 127,   q[t,i] = 127 * x[t,i] / a  rounded to the nearest whole number, halves to the even one
+ * (the rounding of the exact quotient).  A row of zeros gives zeros and scale 0.  q lies in [-127, 127].
+ * Limits: d % 8 == 0, rows < 2^24.  x in dt; q, scale 16-byte aligned.
+ */
+meteora_status meteora_quantize_rows(const void* x /*[rows,d]*/, int rows, int d, meteora_dtype dt,
+                                     int8_t* q /*[rows,d]*/, float* scale /*[rows]*/, meteora_stream stream);
+
+/*
+ * Product of 8-bit whole numbers with a scale per token and per output channel, over groups of consecutive rows:
+ *   out[t,c] = q_scale[t] * w_scale[e,c] * sum_i q[t,i] * W[e,c,i],   e = the group with offsets[e] <= t < offsets[e+1]
+ * The sum is exact (whole numbers); fp32 scaling, one rounding where dt (the type of out) is METEORA_BF16.
+ *   offsets == NULL: N = 1, all rows are one group: a base projection (the 8-bit counterpart of meteora_base_gemm on rows
+ *                    that are quantised already).
+ *   offsets[N+1] (device): groups as meteora_sort_tokens and meteora_bucket_tokens return them, one matrix per adapter;
+ *                    groups may be empty.  Rows outside every group (t >= offsets[N]) are left as they were in out.
+ *                    Offsets must lie in [0, T] and not fall; whatever they hold, only rows in [0, T) are read and written.
+ * Integer weights are frozen: there is no gradient for W.  The gradient with respect to the rows is a call of this entry point
+ * on the weight transposed and quantised anew.
+ * Limits: d_in % 16 == 0, d_in <= 131056, d_out % 8 == 0, d_out <= 2^20, N <= 64, T < 2^24, T * d_out < 2^33.
+ */
+meteora_status meteora_gemm_i8(const int8_t* q /*[T,d_in]*/, const float* q_scale /*[T]*/, const int8_t* W /*[N,d_out,d_in]*/,
+                               const float* w_scale /*[N,d_out]*/, const int32_t* offsets /*[N+1] or NULL*/, int T, int d_in,
+                               int d_out, int N, meteora_dtype dt, void* out /*[T,d_out]*/, meteora_stream stream);
+
+/*
+ * Base projection with the weight in 8 bits: meteora_quantize_rows of x, then meteora_gemm_i8 with one group.  x and out in dt.
+ * ws: meteora_base_gemm_i8_workspace_bytes(T, d_in) bytes (the quantised rows and their scales), which also holds any smaller T;
+ * 0 for arguments outside the limits of meteora_gemm_i8.
+ */
+size_t meteora_base_gemm_i8_workspace_bytes(int T, int d_in);
+
+meteora_status meteora_base_gemm_i8(const void* x /*[T,d_in]*/, const int8_t* W /*[d_out,d_in]*/, const float* w_scale /*[d_out]*/,
+                                    int T, int d_in, int d_out, meteora_dtype dt, void* out /*[T,d_out]*/, void* ws,
+                                    size_t ws_bytes, meteora_stream stream);
+
+/*
+ * Rows next to each other by adapter (the X_i of Sec. 3.3 as rows that are moved; meteora_bucket_tokens lists them):
+ *   pos[t,j]   the place of pair (t, j) among all pairs whose topk_idx lies in [0, N), by adapter, then token, then slot;
+ *              -1 for other ids (padding tokens, say with -1), which go nowhere
+ *   offsets    the first place of every adapter; offsets[N] = the number of places taken, at most T*k
+ *   xs         row pos[t,j] is x[t].  Rows from offsets[N] on are left as they were.
+ *   xs_scale == NULL: xs[T*k, d] in dt.  Otherwise xs is int8_t[T*k, d], quantised as in meteora_quantize_rows, and xs_scale[T*k]
+ *              holds the rows' scales: the operand of meteora_gemm_i8.
+ * The gradient with respect to x is meteora_unsort_tokens with w = NULL on the gradient of xs (xs in dt; none through the
+ * rounding to 8 bits).
+ * Limits: d % 8 == 0, k <= 8 (k may exceed N, and an id may stand twice in a token's row), N <= 64, T < 2^24.
+ * ws: meteora_sort_workspace_bytes(T, k, N) bytes, which also holds any smaller T; 0 outside the limits.
+ */
+size_t meteora_sort_workspace_bytes(int T, int k, int N);
+
+meteora_status meteora_sort_tokens(const void* x /*[T,d]*/, const int32_t* topk_idx /*[T,k]*/, int T, int k, int N, int d,
+                                   meteora_dtype dt, void* xs /*[T*k,d]*/, float* xs_scale /*[T*k] or NULL*/,
+                                   int32_t* pos /*[T,k]*/, int32_t* offsets /*[N+1]*/, void* ws, size_t ws_bytes,
+                                   meteora_stream stream);
+
+/*
+ * Back to the order of the tokens, with weights:
+ *   out[t] = base[t] + scale * sum_j w[t,j] * ys[pos[t,j]]
+ * over the slots whose place lies in [0, rows), rows being those of ys; the others give nothing, and a token without any is
+ * base[t], or zeros.  fp32 sums in order of the slots, one rounding.  base == NULL: zeros; base may be out itself.  w == NULL: ones.
+ *
+ * meteora_unsort_backward, for dy = dL/d out:
+ *   dys[pos[t,j]] = scale * w[t,j] * dy[t],    dw[t,j] = scale * <dy[t], ys[pos[t,j]]>   (fp32; 0 where the place is none)
+ * Rows of dys that no pos names are left as they were.  dw may be NULL, and then ys too.  The gradient of base is dy.
+ * Every place must be named at most once (as meteora_sort_tokens returns them).
+ * ys, base, out, dy, dys in dt.  Limits: d % 8 == 0, k <= 8, T < 2^24, rows < 2^31.
+ */
+meteora_status meteora_unsort_tokens(const void* ys /*[rows,d]*/, int64_t rows, const int32_t* pos /*[T,k]*/,
+                                     const float* w /*[T,k] or NULL*/, int T, int k, int d, float scale, meteora_dtype dt,
+                                     const void* base /*[T,d] or NULL*/, void* out /*[T,d]*/, meteora_stream stream);
+
+meteora_status meteora_unsort_backward(const void* dy /*[T,d]*/, const void* ys /*[rows,d] or NULL*/, int64_t rows,
+                                       const int32_t* pos /*[T,k]*/, const float* w /*[T,k] or NULL*/, int T, int k, int d,
+                                       float scale, meteora_dtype dt, void* dys /*[rows,d]*/, float* dw /*[T,k] or NULL*/,
+                                       meteora_stream stream);
+
+/*
  * Optional per-stage timing, for benchmarks.  Host only; off by default.
  * While enabled, meteora_lora_forward and meteora_linear_forward record
  * hipEvents on `stream` around each stage (prep, gate_logits, gate_topk,

@@ -84,6 +84,22 @@ def load_library():
     lib.meteora_variant_forward.argtypes = [i, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, f, i, vp, vp, vp, vp, sz, vp]
     lib.meteora_base_gemm.restype = i
     lib.meteora_base_gemm.argtypes = [vp, vp, i, i, i, i, vp, vp]
+    lib.meteora_quantize_rows.restype = i
+    lib.meteora_quantize_rows.argtypes = [vp, i, i, i, vp, vp, vp]
+    lib.meteora_gemm_i8.restype = i
+    lib.meteora_gemm_i8.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, i, vp, vp]
+    lib.meteora_base_gemm_i8_workspace_bytes.restype = sz
+    lib.meteora_base_gemm_i8_workspace_bytes.argtypes = [i, i]
+    lib.meteora_base_gemm_i8.restype = i
+    lib.meteora_base_gemm_i8.argtypes = [vp, vp, vp, i, i, i, i, vp, vp, sz, vp]
+    lib.meteora_sort_workspace_bytes.restype = sz
+    lib.meteora_sort_workspace_bytes.argtypes = [i, i, i]
+    lib.meteora_sort_tokens.restype = i
+    lib.meteora_sort_tokens.argtypes = [vp, vp, i, i, i, i, i, vp, vp, vp, vp, vp, sz, vp]
+    lib.meteora_unsort_tokens.restype = i
+    lib.meteora_unsort_tokens.argtypes = [vp, c.c_int64, vp, vp, i, i, i, f, i, vp, vp, vp]
+    lib.meteora_unsort_backward.restype = i
+    lib.meteora_unsort_backward.argtypes = [vp, vp, c.c_int64, vp, vp, i, i, i, f, i, vp, vp, vp]
     lib.meteora_stage_count.restype = i
     lib.meteora_stage_name.restype = c.c_char_p
     lib.meteora_stage_name.argtypes = [i]
@@ -463,6 +479,141 @@ def base_gemm(x, W, out: Optional[torch.Tensor] = None):
     if st != 0:
         raise MeteoraError(st, "meteora_base_gemm")
     return out
+
+
+def _chk_device(x: torch.Tensor, *others):
+    """x lies on the current device, whose stream the call goes to, and the other tensors beside it."""
+    if x.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors are on {x.device}, which is not the current device")
+    for t in others:
+        if t is not None and t.device != x.device:
+            raise ValueError(f"tensors are on {x.device} and {t.device}")
+
+
+def quantize_rows(x, out=None):
+    """meteora_quantize_rows: (q[rows,d] int8, scale[rows] f32), the rows of x as 8-bit whole numbers with a scale each.
+    `out` = the two result tensors if the caller has them already."""
+    rows, d = x.shape
+    _chk(x, "x")
+    if out is None:
+        out = (torch.empty((rows, d), dtype=torch.int8, device=x.device),
+               torch.empty((rows,), dtype=torch.float32, device=x.device))
+    q, scale = out
+    _chk(q, "q", torch.int8, (rows, d)); _chk(scale, "scale", torch.float32, (rows,))
+    _chk_device(x, q, scale)
+    st = load_library().meteora_quantize_rows(_p(x), rows, d, _dt(x), _p(q), _p(scale), _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_quantize_rows")
+    return q, scale
+
+
+def gemm_i8(q, q_scale, W, w_scale, offsets=None, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16):
+    """meteora_gemm_i8: out[t,c] = q_scale[t] * w_scale[e,c] * sum_i q[t,i] W[e,c,i].  W[d_out,d_in] and w_scale[d_out] without
+    offsets, W[N,d_out,d_in] and w_scale[N,d_out] with offsets[N+1].  `dtype`: of the output, if there is no `out`."""
+    T, d_in = q.shape
+    if (W.dim() == 3) != (offsets is not None):
+        raise ValueError("a W of one matrix per group needs offsets, a single matrix none")
+    d_out = W.shape[-2]
+    N = 1 if offsets is None else W.shape[0]
+    _chk(q, "q", torch.int8); _chk(q_scale, "q_scale", torch.float32, (T,))
+    _chk(W, "W", torch.int8, (d_out, d_in) if offsets is None else (N, d_out, d_in))
+    _chk(w_scale, "w_scale", torch.float32, (d_out,) if offsets is None else (N, d_out))
+    _chk(offsets, "offsets", torch.int32, (N + 1,))
+    if out is None:
+        out = torch.empty((T, d_out), dtype=dtype, device=q.device)
+    _chk(out, "out", None, (T, d_out))
+    _chk_device(q, q_scale, W, w_scale, offsets, out)
+    st = load_library().meteora_gemm_i8(_p(q), _p(q_scale), _p(W), _p(w_scale), _p(offsets), T, d_in, d_out, N, _dt(out),
+                                        _p(out), _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_gemm_i8")
+    return out
+
+
+def base_gemm_i8_workspace_bytes(T, d_in) -> int:
+    return int(load_library().meteora_base_gemm_i8_workspace_bytes(T, d_in))
+
+
+def base_gemm_i8(x, W, w_scale, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """meteora_base_gemm_i8: out = x W^T with W[d_out,d_in] int8 and w_scale[d_out] (quantize_rows of the weight), the rows of
+    x quantised on the way."""
+    T, d_in = x.shape
+    d_out = W.shape[0]
+    _chk(x, "x"); _chk(W, "W", torch.int8, (d_out, d_in)); _chk(w_scale, "w_scale", torch.float32, (d_out,))
+    if out is None:
+        out = torch.empty((T, d_out), dtype=x.dtype, device=x.device)
+    _chk(out, "out", x.dtype, (T, d_out)); _chk(ws, "ws", torch.uint8)
+    ws = _ws(ws, lambda: base_gemm_i8_workspace_bytes(T, d_in), x.device)
+    _chk_device(x, W, w_scale, out, ws)
+    st = load_library().meteora_base_gemm_i8(_p(x), _p(W), _p(w_scale), T, d_in, d_out, _dt(x), _p(out), _p(ws), ws.numel(),
+                                             _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_base_gemm_i8")
+    return out
+
+
+def sort_workspace_bytes(T, k, N) -> int:
+    return int(load_library().meteora_sort_workspace_bytes(T, k, N))
+
+
+def sort_tokens(x, topk_idx, N: int, quantize: bool = False, out: Optional[torch.Tensor] = None,
+                ws: Optional[torch.Tensor] = None):
+    """meteora_sort_tokens: (xs[T*k,d], pos[T,k], offsets[N+1]); with `quantize` (xs int8, xs_scale[T*k], pos, offsets)."""
+    T, d = x.shape
+    k = topk_idx.shape[1]
+    dev = x.device
+    dtype = torch.int8 if quantize else x.dtype
+    _chk(x, "x"); _chk(topk_idx, "topk_idx", torch.int32, (T, k)); _chk(ws, "ws", torch.uint8)
+    if out is None:
+        out = torch.empty((T * k, d), dtype=dtype, device=dev)
+    _chk(out, "out", dtype, (T * k, d))
+    scale = torch.empty((T * k,), dtype=torch.float32, device=dev) if quantize else None
+    pos = torch.empty((T, k), dtype=torch.int32, device=dev)
+    offsets = torch.empty((N + 1,), dtype=torch.int32, device=dev)
+    ws = _ws(ws, lambda: sort_workspace_bytes(T, k, N), dev)
+    _chk_device(x, topk_idx, out, ws)
+    st = load_library().meteora_sort_tokens(_p(x), _p(topk_idx), T, k, N, d, _dt(x), _p(out), _p(scale), _p(pos), _p(offsets),
+                                            _p(ws), ws.numel(), _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_sort_tokens")
+    return (out, scale, pos, offsets) if quantize else (out, pos, offsets)
+
+
+def unsort_tokens(ys, pos, w=None, scale: float = 1.0, base: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None):
+    """meteora_unsort_tokens: out[t] = base[t] + scale * sum_j w[t,j] * ys[pos[t,j]]; `base` may be `out`.  Without weights the
+    gradient of sort_tokens."""
+    rows, d = ys.shape
+    T, k = pos.shape
+    _chk(ys, "ys"); _chk(pos, "pos", torch.int32, (T, k)); _chk(w, "w", torch.float32, (T, k))
+    _chk(base, "base", ys.dtype, (T, d))
+    if out is None:
+        out = torch.empty((T, d), dtype=ys.dtype, device=ys.device)
+    _chk(out, "out", ys.dtype, (T, d))
+    _chk_device(ys, pos, w, base, out)
+    st = load_library().meteora_unsort_tokens(_p(ys), rows, _p(pos), _p(w), T, k, d, float(scale), _dt(ys), _p(base), _p(out),
+                                              _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_unsort_tokens")
+    return out
+
+
+def unsort_backward(dy, ys, pos, w=None, scale: float = 1.0, out: Optional[torch.Tensor] = None, want_dw: bool = True):
+    """meteora_unsort_backward: (dys like ys, dw[T,k] f32 or None) for dy = dL/d(unsort_tokens).  Rows of dys that pos does not
+    name are left as they were in `out` (zeros if there is none)."""
+    rows, d = ys.shape
+    T, k = pos.shape
+    _chk(dy, "dy", ys.dtype, (T, d)); _chk(ys, "ys"); _chk(pos, "pos", torch.int32, (T, k)); _chk(w, "w", torch.float32, (T, k))
+    if out is None:
+        out = torch.zeros((rows, d), dtype=ys.dtype, device=ys.device)
+    _chk(out, "out", ys.dtype, (rows, d))
+    _chk_device(dy, ys, pos, w, out)
+    dw = torch.empty((T, k), dtype=torch.float32, device=dy.device) if want_dw else None
+    st = load_library().meteora_unsort_backward(_p(dy), _p(ys), rows, _p(pos), _p(w), T, k, d, float(scale), _dt(ys), _p(out),
+                                                _p(dw), _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_unsort_backward")
+    return out, dw
 
 
 def stage_timing_enable(on: bool) -> None:

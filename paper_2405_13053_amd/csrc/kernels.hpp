@@ -18,6 +18,7 @@ hipError_t gate_init_kernels();
 hipError_t shrink_init_kernels();
 hipError_t gate_bwd_init_kernels();
 hipError_t bucket_init_scratch();
+hipError_t gemm_i8_init_kernels();
 
 // ---- weight repacking, one launch: W_gate -> split bf16 fragments (bf16 gate), A -> MFMA fragments,
 // stacked B -> its transpose Bt[d_out, N*r rounded up to 64] (zero-padded) for the GEMM's K-extension.
@@ -221,5 +222,23 @@ hipError_t launch_gemm(const void* x, const void* W, int T, int d_in, int d_out,
                        const void* hdense, int ext_stride, const void* Bt, int ext_k,
                        void* out, int accumulate, float* splitk_ws, hipStream_t stream,
                        const int32_t* topk_idx = nullptr, int k = 0, int r = 0);
+
+// ---- 8-bit products: rows as whole numbers with a scale each (d % 8 == 0), and
+// out[t,c] = q_scale[t] * w_scale[e,c] * sum_i q[t,i] * W[e,c,i] for the rows t of group e, [offsets[e], offsets[e+1]) (device;
+// nullptr: N = 1 and all rows).  d_in % 16 == 0, at most 131056; d_out % 8 == 0.  Rows of no group are not written.
+hipError_t launch_quantize_rows(const void* x, int rows, int d, bool bf16, int8_t* q, float* scale, hipStream_t stream);
+hipError_t launch_gemm_i8(const int8_t* q, const float* q_scale, const int8_t* W, const float* w_scale, const int32_t* offsets,
+                          int T, int d_in, int d_out, int N, bool bf16, void* out, hipStream_t stream);
+
+// ---- rows sorted by adapter: pos[T,k], offsets[N+1], xs[pos[t,j]] = x[t] (with xs_scale: as 8-bit whole numbers), and back
+// (rows: those of ys; base, w, dw may be nullptr).  chunk_counts: sort_count_bytes, or sort_count_bytes_reserved for any smaller T too.
+size_t sort_count_bytes(int T, int k, int N);
+size_t sort_count_bytes_reserved(int T, int k, int N);
+hipError_t launch_sort_tokens(const void* x, const int32_t* topk_idx, int T, int k, int N, int d, bool bf16, void* xs,
+                              float* xs_scale, int32_t* pos, int32_t* offsets, int32_t* chunk_counts, hipStream_t stream);
+hipError_t launch_unsort_tokens(const void* ys, int64_t rows, const int32_t* pos, const float* w, int T, int k, int d, bool bf16,
+                                float scale, const void* base, void* out, hipStream_t stream);
+hipError_t launch_unsort_backward(const void* dy, const void* ys, int64_t rows, const int32_t* pos, const float* w, int T, int k,
+                                  int d, bool bf16, float scale, void* dys, float* dw, hipStream_t stream);
 
 }  // namespace meteora

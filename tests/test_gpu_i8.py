@@ -1,0 +1,270 @@
+"""8-bit rows and products against plain fp64 on the CPU or GPU.
+
+Tolerances.  Whole numbers are equal.  out = fl(fl(fl(sum) * q_scale) * w_scale): the sum is exact, so three roundings of 2^-24
+each, and one of eps/2 where the output is bf16; base_gemm_i8's scale a / 127 is rounded once more."""
+import pytest
+import torch
+
+import paper_2405_13053_amd as m
+
+pytestmark = pytest.mark.gpu
+U32 = 2.0 ** -24
+TYPES = [torch.bfloat16, torch.float32]
+
+
+def half_step(dtype):
+    return 0.0 if dtype == torch.float32 else torch.finfo(dtype).eps / 2
+
+
+def close(out, ref, roundings=3):
+    """|out - ref| within `roundings` of fp32 and the output's own, element by element."""
+    tol = (roundings * U32 + half_step(out.dtype)) * 1.001
+    err = (out.double() - ref).abs()
+    bad = err > tol * ref.abs()
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}, worst {float((err / ref.abs().clamp_min(1e-300)).max()):.3e} > {tol:.3e}"
+
+
+def rows_ref(x):
+    """Definition: q = rne(127 x / a) of the exact quotient, in fp64 (exact to 2^-46; see the kernel), scale = a / 127 in fp32."""
+    a = x.abs().amax(1, keepdim=True).double() if x.shape[1] else x.double()
+    q = torch.round(x.double() * 127 / torch.where(a > 0, a, torch.ones_like(a)))
+    return q.to(torch.int8), (a[:, 0].float() / 127)
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def int8(shape, g, lo=-127, hi=128):
+    return torch.randint(lo, hi, shape, generator=g, device="cuda", dtype=torch.int8)
+
+
+def scales(shape, g):
+    return torch.rand(shape, generator=g, device="cuda") * 0.02 + 1e-3
+
+
+# ---- quantize_rows -----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,d", [(1, 8), (3, 24), (5, 136), (64, 2048), (7, 2056), (2, 4104), (33, 5120), (4, 8200), (2, 16384),
+                                    (3, 16392), (2, 40000), (513, 64)])
+def test_quantize_rows(rows, d, dtype):
+    g = gen(rows * 131 + d)
+    x = torch.randn((rows, d), generator=g, device="cuda").to(dtype)
+    x[:, 0] *= 9
+    q, s = m.quantize_rows(x)
+    rq, rs = rows_ref(x.cpu())
+    assert torch.equal(q.cpu(), rq) and torch.equal(s.cpu(), rs)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_quantize_rows_rounds_the_exact_quotient(dtype):
+    """Halves: every odd multiple of a / 254 that the type holds, for maxima of all mantissas; and what lies next to them."""
+    g = gen(5)
+    a = (torch.arange(128, 256, device="cuda").float() * 2.0 ** -7)[:, None]
+    n = torch.arange(-127, 127, device="cuda").float()[None, :] + 0.5
+    x = a * n / 127
+    if dtype == torch.float32:   # any mantissa
+        a = torch.rand((128, 1), generator=g, device="cuda") + 1
+        x = (a.double() * n.double() / 127).float()
+        x = torch.cat([x, torch.nextafter(x, x * 2), torch.nextafter(x, x * 0)], 1)
+    else:
+        x = x.to(dtype).float()
+        x = torch.cat([x, x * (1 + 2.0 ** -7), x * (1 - 2.0 ** -7)], 1)
+    x = torch.cat([a, a / 2, -a / 2, x.clamp(-a, a)], 1)
+    x = torch.nn.functional.pad(x, (0, -x.shape[1] % 8)).to(dtype).contiguous()
+    q, s = m.quantize_rows(x)
+    rq, rs = rows_ref(x.cpu())
+    assert torch.equal(q.cpu(), rq) and torch.equal(s.cpu(), rs)
+    assert (q[:, 1] == 64).all() and (q[:, 2] == -64).all()   # 63.5 goes to the even number
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_quantize_rows_of_zeros_and_of_the_smallest_and_largest(dtype):
+    x = torch.zeros((6, 64), device="cuda", dtype=dtype)
+    x[1, 5] = torch.finfo(dtype).max
+    x[1, 6] = -torch.finfo(dtype).max / 2
+    x[2, 0] = torch.finfo(dtype).tiny
+    x[3, 63] = -1.0
+    x[4, 7], x[4, 8] = 2.0 ** -120, -(2.0 ** -121)
+    x[5, 1] = -0.0
+    q, s = m.quantize_rows(x)
+    rq, rs = rows_ref(x.cpu())
+    assert torch.equal(q.cpu()[[0, 2, 3, 4, 5]], rq[[0, 2, 3, 4, 5]]) and torch.equal(s.cpu()[[0, 1, 3, 5]], rs[[0, 1, 3, 5]])
+    assert q[1, 5] == 127
+
+
+# ---- gemm_i8 -----------------------------------------------------------------------------------------------------------------
+def dense_ref(q, qs, W, ws):
+    return (q.double() @ W.double().t()) * qs.double()[:, None] * ws.double()
+
+
+T_SMALL = [1, 2, 15, 16, 17, 33, 64, 65, 100, 128, 130, 257, 300]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d_in,d_out", [(16, 8), (48, 24), (112, 64), (128, 136), (144, 72), (1024, 520), (1040, 264), (4096, 256),
+                                        (2064, 1032)])
+def test_dense(d_in, d_out, dtype):
+    for T in T_SMALL:
+        g = gen(T * 7919 + d_in + d_out)
+        q, W = int8((T, d_in), g, -128), int8((d_out, d_in), g, -128)
+        qs, ws = scales((T,), g), scales((d_out,), g)
+        out = torch.full((T + 1, d_out), 7.0, device="cuda", dtype=dtype)
+        m.gemm_i8(q, qs, W, ws, out=out[:T])
+        close(out[:T], dense_ref(q, qs, W, ws))
+        assert (out[T] == 7).all(), f"T={T}: written behind the last row"
+
+
+@pytest.mark.parametrize("T,d_in,d_out", [(640, 4096, 4096), (1000, 1040, 2056), (2048, 4096, 1024), (4096, 512, 4096),
+                                          (1531, 4096, 4096), (4097, 272, 4104), (700, 14336, 1024), (3000, 2048, 13824),
+                                          (8192, 64, 1024), (5000, 4096, 64), (16384, 128, 264)])
+def test_dense_large(T, d_in, d_out):
+    g = gen(T + d_in)
+    q, W = int8((T, d_in), g), int8((d_out, d_in), g)
+    qs, ws = scales((T,), g), scales((d_out,), g)
+    ref = dense_ref(q, qs, W, ws)
+    for dtype in TYPES:
+        close(m.gemm_i8(q, qs, W, ws, dtype=dtype), ref)
+
+
+@pytest.mark.parametrize("T", [1, 40, 300, 700])
+def test_the_largest_sums(T):
+    """131056 inputs of -128 on both sides add up to just below 2^31; of -128 and 127 to the other end."""
+    K = 131056
+    q = torch.full((T, K), -128, device="cuda", dtype=torch.int8)
+    W = torch.full((264, K), -128, device="cuda", dtype=torch.int8)
+    W[1::2] = 127
+    one = torch.ones
+    out = m.gemm_i8(q, one(T, device="cuda"), W, one(264, device="cuda"), dtype=torch.float32)
+    sums = torch.tensor([K * 16384.0, -K * 127 * 128.0], device="cuda", dtype=torch.float64).repeat(132).expand(T, 264)
+    close(out, sums, 1)
+
+
+def grouped_case(T, N, d_in, d_out, counts, g):
+    q, W = int8((T, d_in), g), int8((N, d_out, d_in), g)
+    qs, ws = scales((T,), g), scales((N, d_out), g)
+    off = torch.tensor([0] + counts, dtype=torch.int64).cumsum(0).to(torch.int32)
+    return q, qs, W, ws, off
+
+
+GROUPS = [
+    (1, 1, [1]), (1, 4, [0, 0, 1, 0]), (5, 3, [0, 0, 0]), (40, 3, [13, 0, 27]), (64, 4, [16, 16, 16, 16]), (130, 5, [0, 1, 128, 1, 0]),
+    (300, 7, [70, 0, 3, 64, 65, 40, 20]), (300, 2, [299, 0]), (700, 3, [257, 300, 143]), (1000, 64, [15] * 64),
+    (2000, 28, [0] * 27 + [1999]), (1200, 2, [513, 600]), (4096, 8, [512] * 8), (2048, 3, [1100, 20, 900]),
+]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d_in,d_out", [(64, 512), (528, 64), (1024, 8), (16, 1032), (1040, 776)])
+@pytest.mark.parametrize("T,N,counts", GROUPS, ids=lambda v: str(v)[:20])
+def test_groups(T, N, counts, d_in, d_out, dtype):
+    g = gen(T + N + d_in)
+    q, qs, W, ws, off = grouped_case(T, N, d_in, d_out, counts, g)
+    out = torch.full((T, d_out), 7.0, device="cuda", dtype=dtype)
+    m.gemm_i8(q, qs, W, ws, offsets=off.cuda(), out=out)
+    for e in range(N):
+        a, b = int(off[e]), int(off[e + 1])
+        close(out[a:b], dense_ref(q[a:b], qs[a:b], W[e], ws[e]))
+    assert (out[int(off[-1]):] == 7).all()   # rows of no group
+
+
+def test_offsets_outside_the_rows_write_nothing_outside():
+    g = gen(3)
+    q, qs, W, ws, _ = grouped_case(100, 4, 64, 64, [25] * 4, g)
+    for bad in ([0, 50, 40, 200, 1 << 30], [-5, -1, 20, 100, 100], [2 ** 31 - 1] * 5, [-2 ** 31, 2 ** 31 - 1, 0, 3, 9]):
+        buf = torch.full((300, 64), 7.0, device="cuda", dtype=torch.float32)
+        m.gemm_i8(q, qs, W, ws, offsets=torch.tensor(bad, dtype=torch.int32, device="cuda"), out=buf[100:200])
+        assert (buf[:100] == 7).all() and (buf[200:] == 7).all()
+
+
+def test_operands_and_outputs_beyond_32_bit_offsets():
+    g = gen(9)
+    T, K, n = 270000, 16384, 64   # q: 4.4 GB
+    q, W, qs, ws = int8((T, K), g), int8((n, K), g), scales((T,), g), scales((n,), g)
+    out = m.gemm_i8(q, qs, W, ws, dtype=torch.float32)
+    rows = torch.cat([torch.arange(0, T, 1777), torch.arange(T - 70, T)]).cuda()
+    close(out[rows], dense_ref(q[rows], qs[rows], W, ws))
+    N, n, K = 64, 8192, 8208      # W: 4.3 GB
+    q, W, qs, ws = int8((200, K), g), int8((N, n, K), g), scales((200,), g), scales((N, n), g)
+    off = torch.tensor([0] * 62 + [3, 90, 200], dtype=torch.int32)
+    out = m.gemm_i8(q, qs, W, ws, offsets=off.cuda(), dtype=torch.float32)
+    for e in (61, 62, 63):
+        a, b = int(off[e]), int(off[e + 1])
+        close(out[a:b], dense_ref(q[a:b], qs[a:b], W[e], ws[e]))
+    T, K, n = 150000, 16, 16384   # out: 9.8 GB in fp32
+    q, W, qs, ws = int8((T, K), g), int8((n, K), g), scales((T,), g), scales((n,), g)
+    out = m.gemm_i8(q, qs, W, ws, dtype=torch.float32)
+    rows = torch.cat([torch.arange(0, T, 3001), torch.arange(T - 70, T)]).cuda()
+    close(out[rows], dense_ref(q[rows], qs[rows], W, ws))
+
+
+# ---- base_gemm_i8 --------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,d_in,d_out", [(1, 4096, 4096), (1, 16, 8), (2, 5120, 520), (4, 4096, 1024), (7, 1040, 264), (16, 512, 512),
+                                          (64, 4096, 4096), (65, 528, 1032), (300, 4096, 1024), (1000, 1024, 4096), (2, 16400, 64)])
+def test_base_gemm_i8(T, d_in, d_out, dtype):
+    g = gen(T + d_out)
+    x = torch.randn((T, d_in), generator=g, device="cuda").to(dtype)
+    W, ws = m.quantize_rows(torch.randn((d_out, d_in), generator=g, device="cuda"))
+    ws_buf = torch.empty(m.base_gemm_i8_workspace_bytes(T + 3, d_in), dtype=torch.uint8, device="cuda")
+    out = m.base_gemm_i8(x, W, ws, ws=ws_buf)
+    q, _ = rows_ref(x)
+    s = x.abs().amax(1).double() / 127
+    close(out, dense_ref(q, s, W, ws), 4)
+    again = m.base_gemm_i8(x, W, ws)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("T", [1, 4, 64, 500])
+def test_base_gemm_i8_rows_of_zeros(T):
+    x = torch.zeros((T, 256), device="cuda", dtype=torch.bfloat16)
+    x[::2] = 1.0
+    W, ws = m.quantize_rows(torch.randn((64, 256), device="cuda"))
+    out = m.base_gemm_i8(x, W, ws)
+    assert (out[1::2] == 0).all() and torch.isfinite(out).all()
+
+
+def test_another_stream_and_a_graph_replayed_between_eager_calls():
+    g = gen(11)
+    for T, d_in, d_out in ((1, 4096, 1024), (64, 1024, 1024), (300, 1024, 512), (2048, 512, 2048)):
+        x = torch.randn((T, d_in), generator=g, device="cuda").bfloat16()
+        W, ws = m.quantize_rows(torch.randn((d_out, d_in), generator=g, device="cuda"))
+        wsb = torch.empty(m.base_gemm_i8_workspace_bytes(T, d_in), dtype=torch.uint8, device="cuda")
+        m.init()
+        want = m.base_gemm_i8(x, W, ws)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            got = m.base_gemm_i8(x, W, ws, ws=wsb)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got, want)
+        xin, out = x.clone(), torch.empty_like(want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            m.base_gemm_i8(xin, W, ws, out=out, ws=wsb)
+        for i in range(3):
+            xin.copy_(torch.randn((T, d_in), generator=g, device="cuda"))
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, m.base_gemm_i8(xin, W, ws)), f"replay {i}"
+
+
+def test_binding_checks():
+    q, s = torch.zeros((4, 64), dtype=torch.int8, device="cuda"), torch.zeros(4, device="cuda")
+    with pytest.raises(ValueError):
+        m.gemm_i8(q, s, q[:, ::2], s)                      # not contiguous
+    with pytest.raises(ValueError):
+        m.gemm_i8(q, s[:3], q, s)
+    with pytest.raises(TypeError):
+        m.gemm_i8(q.float(), s, q, s)
+    with pytest.raises(TypeError):
+        m.gemm_i8(q, s, q, s, dtype=torch.float16)
+    with pytest.raises(m.MeteoraError) as e:
+        m.quantize_rows(torch.zeros((4, 12), device="cuda"))
+    assert e.value.status == 2
+    with pytest.raises(TypeError):
+        m.quantize_rows(torch.zeros((4, 16), device="cuda", dtype=torch.float16))
+    with pytest.raises(m.MeteoraError) as e:
+        m.base_gemm_i8(torch.zeros((4, 64), device="cuda"), torch.zeros((8, 64), dtype=torch.int8, device="cuda"),
+                       torch.zeros(8, device="cuda"), ws=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == 3
