@@ -93,7 +93,7 @@ meteora_status meteora_sort_tokens(const void* x, const int32_t* topk_idx, int T
                                    meteora_stream stream) {
     if (!x || !topk_idx || !xs || !pos || !offsets || !sort_shape_ok(T, k, N) || d < 1) return METEORA_ERR_INVALID_ARG;
     if (!known(dt) || !sort_shape_supported(T, k, N) || d % 8 != 0) return METEORA_ERR_UNSUPPORTED;
-    if (!aligned(x, 16) || !aligned(topk_idx, 4) || !aligned(xs, 16) || !aligned(pos, 4) || !aligned(offsets, 4) ||
+    if (!aligned(x, 16) || !aligned(topk_idx, 16) || !aligned(xs, 16) || !aligned(pos, 4) || !aligned(offsets, 4) ||
         (xs_scale && !aligned(xs_scale, 4)))
         return METEORA_ERR_UNSUPPORTED;
     if (!ws || !aligned(ws, 256) || ws_bytes < sort_count_bytes(T, k, N)) return METEORA_ERR_WORKSPACE;

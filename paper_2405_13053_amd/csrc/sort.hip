@@ -7,6 +7,8 @@
 //
 // All of them move bytes and nothing else, so every one goes by tokens: a token's row is read once and written k times, or k
 // rows are read and one written, at places that pos names; nothing is added to memory, and results do not depend on an order.
+#include <type_traits>
+
 #include "common.hpp"
 #include "kernels.hpp"
 #include "quant.hpp"
@@ -16,62 +18,112 @@ namespace meteora {
 constexpr int kSortThreads = 256;
 
 // ---- positions ------------------------------------------------------------------------------------------------------------
-// chunk_counts[c][j] = pairs of chunk c (chunk_tokens tokens) with id j
+// How often each adapter stands in a list of ids, counted by a workgroup in LDS.  8 copies of every counter, a lane's own by its low
+// bits, so that a skewed load does not make 64 lanes wait for one word.  Counts: the order does not show.
+constexpr int kCopies = 8, kCopyStride = kCopies + 1;   // copies of one counter lie in different banks
+struct Counters { int n[kMaxAdapters * kCopyStride]; };
+__device__ __forceinline__ void clear(Counters& c) {
+    for (int i = threadIdx.x; i < kMaxAdapters * kCopyStride; i += kSortThreads) c.n[i] = 0;
+}
+__device__ __forceinline__ void count(Counters& c, int key, int by) {
+    atomicAdd(&c.n[key * kCopyStride + (threadIdx.x & (kCopies - 1))], by);
+}
+__device__ __forceinline__ int total(const Counters& c, int key) {
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) sum += c.n[key * kCopyStride + i];
+    return sum;
+}
+
+// chunk_counts[c][j] = pairs of chunk c with id j
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t* __restrict__ topk_idx, int64_t pairs,
                                                                   int chunk_pairs, int N, int32_t* __restrict__ chunk_counts) {
-    __shared__ int hist[kMaxAdapters];
-    if (threadIdx.x < kMaxAdapters) hist[threadIdx.x] = 0;
+    __shared__ Counters c;
+    clear(c);
     __syncthreads();
     const int64_t base = (int64_t)blockIdx.x * chunk_pairs;
     for (int i = threadIdx.x; i < chunk_pairs && base + i < pairs; i += kSortThreads) {
         const int key = topk_idx[base + i];
-        if (key >= 0 && key < N) atomicAdd(&hist[key], 1);   // counts: the order does not show
+        if (key >= 0 && key < N) count(c, key, 1);
     }
     __syncthreads();
-    if (threadIdx.x < N) chunk_counts[(size_t)blockIdx.x * N + threadIdx.x] = hist[threadIdx.x];
+    if (threadIdx.x < N) chunk_counts[(size_t)blockIdx.x * N + threadIdx.x] = total(c, threadIdx.x);
 }
 
 struct SortArgs {
     const int32_t* topk_idx;
     int64_t pairs;                 // T * k
     int T, k, N, d, chunk_tokens, nchunks;
-    const int32_t* chunk_counts;
+    const int32_t* chunk_counts;   // of sort_count_kernel, or nullptr: every workgroup counts all ids
     int32_t* pos;                  // [T,k]
     int32_t* offsets;              // [N+1]
     float* xs_scale;               // [T*k]
 };
 
-// A workgroup's chunk of tokens: the first place of every adapter's pairs of this chunk, then the chunk's pairs in order.
-__device__ __forceinline__ void sort_positions(const SortArgs& a, int* places /*LDS, chunk pairs*/) {
-    __shared__ int tot[4][kMaxAdapters], bef[4][kMaxAdapters], running[kMaxAdapters], wave_hist[4][kMaxAdapters];
+constexpr int kSortChunkPairs = 2048;   // at most, in LDS
+
+struct SortShared {
+    Counters before, rest;
+    int running[kMaxAdapters], wave_hist[4][kMaxAdapters], places[kSortChunkPairs];
+};
+
+// The places of this workgroup's chunk of pairs, to LDS and to pos.
+__device__ __forceinline__ void sort_positions(const SortArgs& a, SortShared& sh) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x;
-    int t = 0, b = 0;
-    if (lane < a.N)
-        for (int cc = wave; cc < a.nchunks; cc += 4) {
-            const int v = a.chunk_counts[(size_t)cc * a.N + lane];
-            t += v;
-            if (cc < c) b += v;
+    const int chunk_pairs = a.chunk_tokens * a.k;
+    const int64_t base = (int64_t)c * chunk_pairs;
+    clear(sh.before);
+    clear(sh.rest);
+    __syncthreads();
+    if (a.chunk_counts == nullptr) {
+        // 16 ids a thread at a time, all requested before the first is counted: the loop waits for loads, not for arithmetic
+        const int pairs = (int)a.pairs, first = (int)base;
+        for (int i0 = threadIdx.x * 4; i0 < pairs; i0 += kSortThreads * 16) {
+            int4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * kSortThreads * 4;
+                v[u] = make_int4(-1, -1, -1, -1);
+                if (i + 4 <= pairs) v[u] = *reinterpret_cast<const int4*>(a.topk_idx + i);
+                else if (i < pairs) v[u] = make_int4(a.topk_idx[i], i + 1 < pairs ? a.topk_idx[i + 1] : -1, i + 2 < pairs ? a.topk_idx[i + 2] : -1, -1);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * kSortThreads * 4;
+                const int key[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (key[e] >= 0 && key[e] < a.N) count(i + e < first ? sh.before : sh.rest, key[e], 1);
+            }
         }
-    tot[wave][lane] = t;
-    bef[wave][lane] = b;
+    } else {
+        const int entries = a.nchunks * a.N, first = c * a.N;
+        for (int i0 = threadIdx.x; i0 < entries; i0 += kSortThreads * 8) {
+            int n[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) n[u] = i0 + u * kSortThreads < entries ? a.chunk_counts[i0 + u * kSortThreads] : 0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = i0 + u * kSortThreads;
+                if (n[u] != 0) count(i < first ? sh.before : sh.rest, i % a.N, n[u]);
+            }
+        }
+    }
     __syncthreads();
     if (wave == 0) {
-        const int v = tot[0][lane] + tot[1][lane] + tot[2][lane] + tot[3][lane];
+        const int b = total(sh.before, lane), v = b + total(sh.rest, lane);   // adapters from N on: zeros
         int incl = v;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
             const int n = __shfl_up(incl, off);
             if (lane >= off) incl += n;
         }
-        running[lane] = incl - v + bef[0][lane] + bef[1][lane] + bef[2][lane] + bef[3][lane];
+        sh.running[lane] = incl - v + b;
         if (c == 0) {
             if (lane < a.N) a.offsets[lane] = incl - v;
             if (lane == a.N - 1) a.offsets[a.N] = incl;
         }
     }
-    __syncthreads();
-    const int chunk_pairs = a.chunk_tokens * a.k;
-    const int64_t base = (int64_t)c * chunk_pairs;
     for (int i0 = 0; i0 < chunk_pairs; i0 += kSortThreads) {
         const int i = i0 + threadIdx.x;
         const bool in = i < chunk_pairs && base + i < a.pairs;
@@ -84,66 +136,98 @@ __device__ __forceinline__ void sort_positions(const SortArgs& a, int* places /*
             peers &= ((key >> bit) & 1) ? m : ~m;
         }
         const int rank = __popcll(peers & (lane == 0 ? 0ull : ~0ull >> (64 - lane)));
-        wave_hist[wave][lane] = 0;
+        sh.wave_hist[wave][lane] = 0;
         __syncthreads();
-        if (valid && rank == 0) wave_hist[wave][key] = __popcll(peers);
+        if (valid && rank == 0) sh.wave_hist[wave][key] = __popcll(peers);
         __syncthreads();
         int p = -1;
         if (valid) {
-            p = running[key] + rank;
-            for (int w = 0; w < wave; ++w) p += wave_hist[w][key];
+            p = sh.running[key] + rank;
+            for (int w = 0; w < wave; ++w) p += sh.wave_hist[w][key];
         }
         if (in) {
-            places[i] = p;
+            sh.places[i] = p;
             a.pos[base + i] = p;
         }
         __syncthreads();
-        if (threadIdx.x < kMaxAdapters)
-            running[threadIdx.x] += wave_hist[0][threadIdx.x] + wave_hist[1][threadIdx.x] + wave_hist[2][threadIdx.x] +
-                                    wave_hist[3][threadIdx.x];
-        __syncthreads();
+        if (i0 + kSortThreads < chunk_pairs && threadIdx.x < kMaxAdapters)
+            sh.running[threadIdx.x] += sh.wave_hist[0][threadIdx.x] + sh.wave_hist[1][threadIdx.x] +
+                                       sh.wave_hist[2][threadIdx.x] + sh.wave_hist[3][threadIdx.x];
+    }
+    __syncthreads();
+}
+
+// Rows as they are, 16 bytes a piece; 2^lanes_log2 threads to a row.  The first pieces are on their way while the places are found.
+constexpr int kSortHeld = 8;
+__global__ __launch_bounds__(kSortThreads) void sort_rows_kernel(const SortArgs a, const u32x4* __restrict__ x, int row16,
+                                                                 int lanes_log2, u32x4* __restrict__ xs) {
+    __shared__ SortShared sh;
+    const int t0 = blockIdx.x * a.chunk_tokens, tokens = min(a.chunk_tokens, a.T - t0);
+    const int lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1);
+    struct Cursor { int t, c; };
+    Cursor get{(int)threadIdx.x >> lanes_log2, lane}, put = get;
+    if (lane >= row16) get.t = put.t = tokens;
+    auto next = [&](Cursor& p) {
+        p.c += lanes;
+        if (p.c >= row16) {
+            p.c = lane;
+            p.t += kSortThreads >> lanes_log2;
+        }
+    };
+    u32x4 held[kSortHeld];
+    auto load = [&] {
+#pragma unroll
+        for (int u = 0; u < kSortHeld; ++u) {
+            if (get.t < tokens) held[u] = x[(size_t)(t0 + get.t) * row16 + get.c];
+            next(get);
+        }
+    };
+    load();
+    sort_positions(a, sh);
+    while (put.t < tokens) {
+#pragma unroll
+        for (int u = 0; u < kSortHeld; ++u) {
+            if (put.t < tokens)
+                for (int j = 0; j < a.k; ++j) {
+                    const int p = sh.places[put.t * a.k + j];
+                    if (p >= 0) xs[(size_t)p * row16 + put.c] = held[u];
+                }
+            next(put);
+        }
+        load();
     }
 }
 
-constexpr int kSortChunkPairs = 2048;   // at most, in LDS
-
-// rows as they are, 16 bytes a piece
-__global__ __launch_bounds__(kSortThreads) void sort_rows_kernel(const SortArgs a, const u32x4* __restrict__ x, int row16,
-                                                                 u32x4* __restrict__ xs) {
-    __shared__ int places[kSortChunkPairs];
-    sort_positions(a, places);
-    const int t0 = blockIdx.x * a.chunk_tokens, tokens = min(a.chunk_tokens, a.T - t0);
-    for (int t = 0; t < tokens; ++t)
-        for (int i = threadIdx.x; i < row16; i += kSortThreads) {
-            const u32x4 v = x[(size_t)(t0 + t) * row16 + i];
-            for (int j = 0; j < a.k; ++j) {
-                const int p = places[t * a.k + j];
-                if (p >= 0) xs[(size_t)p * row16 + i] = v;
-            }
-        }
-}
-
-// rows as 8-bit whole numbers
-template <typename TX, int HELD>
+// Rows as 8-bit whole numbers
+template <typename TX, int G, int HELD>
 __global__ __launch_bounds__(kSortThreads) void sort_quantize_kernel(const SortArgs a, const TX* __restrict__ x,
                                                                      int8_t* __restrict__ xs) {
     static_assert(kSortThreads == kQuantThreads, "a workgroup quantises a row");
-    __shared__ int places[kSortChunkPairs];
+    __shared__ SortShared sh;
     __shared__ float red[2][4];
-    sort_positions(a, places);
-    const int t0 = blockIdx.x * a.chunk_tokens, tokens = min(a.chunk_tokens, a.T - t0);
-    for (int t = 0; t < tokens; ++t) {
-        const int* place = places + t * a.k;
-        const float top = quantize_row<TX, HELD>(x + (size_t)(t0 + t) * a.d, a.d / 8, red[t & 1], [&](int i, uint2 v) {
+    const int t0 = blockIdx.x * a.chunk_tokens, tokens = min(a.chunk_tokens, a.T - t0), pieces = a.d / 8;
+    const TX* rows = x + (size_t)t0 * a.d;
+    constexpr int GROUPS = kSortThreads / G;
+    QuantRow<TX, G, HELD> r;
+    int t = threadIdx.x / G;
+    if (t < tokens) r.load(rows + (size_t)t * a.d, pieces);
+    sort_positions(a, sh);
+    for (int n = 0; t < tokens; t += GROUPS, ++n) {   // G = 256: the same for all threads
+        const TX* src = rows + (size_t)t * a.d;
+        const int* place = sh.places + t * a.k;
+        const float top = r.top(src, pieces, red[n & 1]);
+        r.store(src, pieces, top, [&](int i, uint2 v) {
             for (int j = 0; j < a.k; ++j)
                 if (place[j] >= 0) reinterpret_cast<uint2*>(xs + (size_t)place[j] * a.d)[i] = v;
         });
-        if ((int)threadIdx.x < a.k && place[threadIdx.x] >= 0) a.xs_scale[place[threadIdx.x]] = top / 127.f;
+        const int lane = threadIdx.x & (G - 1);
+        if (lane < a.k && place[lane] >= 0) a.xs_scale[place[lane]] = top / 127.f;
+        if (t + GROUPS < tokens) r.load(src + (size_t)GROUPS * a.d, pieces);
     }
 }
 
-// Tokens per workgroup: the histograms of all chunks are read by every workgroup.
-constexpr int kSortChunks = 512;
+// Tokens per workgroup: with few pairs every workgroup counts all of them; beyond, it adds up the histograms of all chunks.
+constexpr int kSortChunks = 512, kSortDirectPairs = 16384;
 static int sort_chunk_tokens(int T, int k) {
     int c = 1;
     while (c < kSortChunkPairs / k / 2 && ceil_div(T, c) > kSortChunks) c *= 2;
@@ -155,18 +239,18 @@ size_t sort_count_bytes_reserved(int T, int k, int N) {   // of any batch of up 
     return own > few ? own : few;
 }
 
+static int lanes_log2_for(int row16) {
+    int l = 0;
+    while (l < 8 && (1 << l) < row16) ++l;
+    return l;
+}
+
 template <typename TX>
 static hipError_t launch_sort_quantize(const SortArgs& a, const TX* x, int8_t* xs, hipStream_t stream) {
-    const int per_thread = ceil_div(a.d / 8, kQuantThreads);
-    auto go = [&](auto kern) {
-        kern<<<a.nchunks, kSortThreads, 0, stream>>>(a, x, xs);
+    return quant_row_shape(a.d, [&](auto g, auto held) {
+        sort_quantize_kernel<TX, decltype(g)::value, decltype(held)::value><<<a.nchunks, kSortThreads, 0, stream>>>(a, x, xs);
         return hipGetLastError();
-    };
-    if (per_thread <= 1) return go(&sort_quantize_kernel<TX, 1>);
-    if (per_thread <= 2) return go(&sort_quantize_kernel<TX, 2>);
-    if (per_thread <= 4) return go(&sort_quantize_kernel<TX, 4>);
-    if (per_thread <= kQuantHeld) return go(&sort_quantize_kernel<TX, kQuantHeld>);
-    return go(&sort_quantize_kernel<TX, 0>);
+    });
 }
 
 hipError_t launch_sort_tokens(const void* x, const int32_t* topk_idx, int T, int k, int N, int d, bool bf16, void* xs,
@@ -174,14 +258,18 @@ hipError_t launch_sort_tokens(const void* x, const int32_t* topk_idx, int T, int
     SortArgs a{};
     a.topk_idx = topk_idx; a.pairs = (int64_t)T * k; a.T = T; a.k = k; a.N = N; a.d = d;
     a.chunk_tokens = sort_chunk_tokens(T, k); a.nchunks = ceil_div(T, a.chunk_tokens);
-    a.chunk_counts = chunk_counts; a.pos = pos; a.offsets = offsets; a.xs_scale = xs_scale;
-    sort_count_kernel<<<a.nchunks, kSortThreads, 0, stream>>>(topk_idx, a.pairs, a.chunk_tokens * k, N, chunk_counts);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    a.pos = pos; a.offsets = offsets; a.xs_scale = xs_scale;
+    if (a.pairs > kSortDirectPairs) {
+        a.chunk_counts = chunk_counts;
+        sort_count_kernel<<<a.nchunks, kSortThreads, 0, stream>>>(topk_idx, a.pairs, a.chunk_tokens * k, N, chunk_counts);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     if (xs_scale != nullptr)
         return bf16 ? launch_sort_quantize(a, (const bf16_t*)x, (int8_t*)xs, stream)
                     : launch_sort_quantize(a, (const float*)x, (int8_t*)xs, stream);
-    sort_rows_kernel<<<a.nchunks, kSortThreads, 0, stream>>>(a, (const u32x4*)x, d / (bf16 ? 8 : 4), (u32x4*)xs);
+    const int row16 = d / (bf16 ? 8 : 4);
+    sort_rows_kernel<<<a.nchunks, kSortThreads, 0, stream>>>(a, (const u32x4*)x, row16, lanes_log2_for(row16), (u32x4*)xs);
     return hipGetLastError();
 }
 
@@ -248,12 +336,6 @@ __global__ __launch_bounds__(256) void unsort_kernel(const UnsortArgs a, const u
         }
         out[(size_t)t * a.row16 + i] = Piece16<TX>::put(f);
     }
-}
-
-static int lanes_log2_for(int row16) {
-    int l = 0;
-    while (l < 8 && (1 << l) < row16) ++l;
-    return l;
 }
 
 hipError_t launch_unsort_tokens(const void* ys, int64_t rows, const int32_t* pos, const float* w, int T, int k, int d, bool bf16,
