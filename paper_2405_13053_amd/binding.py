@@ -483,10 +483,11 @@ def base_gemm(x, W, out: Optional[torch.Tensor] = None):
 
 def _chk_device(x: torch.Tensor, *others):
     """x lies on the current device, whose stream the call goes to, and the other tensors beside it."""
-    if x.device.index != torch._C._cuda_getDevice():
+    dev = x.get_device()
+    if dev != torch._C._cuda_getDevice():
         raise ValueError(f"tensors are on {x.device}, which is not the current device")
     for t in others:
-        if t is not None and t.device != x.device:
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors are on {x.device} and {t.device}")
 
 
@@ -539,11 +540,18 @@ def base_gemm_i8(x, W, w_scale, out: Optional[torch.Tensor] = None, ws: Optional
     x quantised on the way."""
     T, d_in = x.shape
     d_out = W.shape[0]
-    _chk(x, "x"); _chk(W, "W", torch.int8, (d_out, d_in)); _chk(w_scale, "w_scale", torch.float32, (d_out,))
+    dev, dtype = x.device, x.dtype
     if out is None:
-        out = torch.empty((T, d_out), dtype=x.dtype, device=x.device)
-    _chk(out, "out", x.dtype, (T, d_out)); _chk(ws, "ws", torch.uint8)
-    ws = _ws(ws, lambda: base_gemm_i8_workspace_bytes(T, d_in), x.device)
+        _chk(x, "x")
+        out = torch.empty((T, d_out), dtype=dtype, device=dev)
+    # written out, as in linear_forward
+    if not (W.dtype == torch.int8 and w_scale.dtype == torch.float32 and out.dtype == dtype and W.shape == (d_out, d_in) and
+            w_scale.shape == (d_out,) and out.shape == (T, d_out) and x.is_cuda and x.is_contiguous() and W.is_contiguous() and
+            w_scale.is_contiguous() and out.is_contiguous()):
+        _chk(x, "x"); _chk(W, "W", torch.int8, (d_out, d_in)); _chk(w_scale, "w_scale", torch.float32, (d_out,))
+        _chk(out, "out", dtype, (T, d_out))
+    _chk(ws, "ws", torch.uint8)
+    ws = _ws(ws, lambda: base_gemm_i8_workspace_bytes(T, d_in), dev)
     _chk_device(x, W, w_scale, out, ws)
     st = load_library().meteora_base_gemm_i8(_p(x), _p(W), _p(w_scale), T, d_in, d_out, _dt(x), _p(out), _p(ws), ws.numel(),
                                              _stream())

@@ -76,6 +76,8 @@ meteora_status meteora_base_gemm_i8(const void* x, const int8_t* W, const float*
     if (!ws || !aligned(ws, 256) || ws_bytes < base_gemm_i8_bytes(T, d_in)) return METEORA_ERR_WORKSPACE;
     if (T == 0) return METEORA_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (base_gemm_i8_in_one(T, d_in))
+        return status(launch_base_gemm_i8_in_one(x, W, w_scale, T, d_in, d_out, dt == METEORA_BF16, out, st));
     int8_t* q = static_cast<int8_t*>(ws);
     float* scale = reinterpret_cast<float*>(q + align_up((size_t)T * d_in, 256));
     const hipError_t e = launch_quantize_rows(x, T, d_in, dt == METEORA_BF16, q, scale, st);

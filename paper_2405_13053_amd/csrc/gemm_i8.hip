@@ -9,11 +9,13 @@
 // gemm_i8_ring_kernel   many rows: output tiles of 64 x 64 to 256 x 256, operands through rings of LDS slots
 // gemm_i8_wave_kernel   few rows: a workgroup's wavefronts split K between them, each with a ring of its own, and add their tiles in LDS
 // gemm_i8_one_kernel    up to 128 inputs: the output is what there is to move
+// gemm_i8_row_kernel    up to 4 tokens of meteora_base_gemm_i8: their quantisation too
 #include <math.h>
 
 #include "common.hpp"
 #include "gemm_mfma.hpp"
 #include "kernels.hpp"
+#include "quant.hpp"
 
 namespace meteora {
 
@@ -110,10 +112,67 @@ __device__ __forceinline__ void i8_load_lds(const I8Operand& o, unsigned char* d
     __builtin_amdgcn_raw_ptr_buffer_load_lds(o.rsrc, (__attribute__((address_space(3))) void*)dst, 16, voff, soff, 0, POLICY);
 }
 
+// One operand of the wavefront rings: an instruction moves 8 rows x 128 bytes; 16-byte chunk c of row r lies at position swz(r, c).
+// Rows past the last load zeros, as do a last K tile's columns past d_in.  Requests may go on past the last K tile, from behind the
+// matrix's end, so that their number is always the same.
+template <int B>
+struct WaveOperand {
+    I8Operand mat;
+    uint32_t even, odd, even_last, odd_last, ld8;   // offsets of the chunk in rows j * 8 + (lane / 8), j even and odd
+    uint32_t v_even, v_odd, kbase;
+    int last;                                       // the K tile that is partly there
+    __device__ __forceinline__ WaveOperand(const int8_t* base, int rows, uint32_t ld, int lane) : mat(i8_operand(base, rows, ld)) {
+        const int rsub = lane >> 3, p = lane & 7;
+        const uint32_t c_even = (uint32_t)swz(rsub, p) * 16, c_odd = (uint32_t)swz(rsub + 8, p) * 16, left = ld % 128;
+        even = (uint32_t)rsub * ld + c_even;
+        odd = (uint32_t)rsub * ld + c_odd;
+        even_last = c_even < left ? even : kOutside;
+        odd_last = c_odd < left ? odd : kOutside;
+        ld8 = ld * 8;
+        last = left != 0 ? (int)(ld / 128) : -1;
+    }
+    __device__ __forceinline__ void at_tile(int kt, int nk) {
+        v_even = kt == last ? even_last : even;
+        v_odd = kt == last ? odd_last : odd;
+        kbase = kt < nk ? (uint32_t)kt * 128 : kOutside;
+    }
+    template <int POLICY>
+    __device__ __forceinline__ void request(unsigned char* slot, int j) const {   // rows j * 8 to j * 8 + 7 of the K tile
+        i8_load_lds<POLICY>(mat, slot + j * 1024, j & 1 ? v_odd : v_even, (int)(kbase + (uint32_t)j * ld8));
+    }
+};
+
 template <int TB, int RB, int WV, int D>
 constexpr int wave_i8_lds() {
     constexpr int ring = WV * D * (TB + RB) * 2048, sums = WV * TB * RB * 1024;
     return ring > sums ? ring : sums;
+}
+
+// The wavefronts' tiles are added in LDS ([wave][block][lane]) and leave as scaled rows.  W is the first operand, so a lane holds 4
+// consecutive columns of row l15 of a block; qs, ws: the scales of the blocks wave, wave + WV, ...
+template <typename TO, int TB, int RB, int WV, int OUT>
+__device__ __forceinline__ void wave_i8_sums(const GemmI8Args& a, const i32x4 (&acc)[TB][RB], unsigned char* smem, const float (&qs)[OUT],
+                                             const f32x4 (&ws)[OUT], int row0, int rows, int n0, int cols, int wave, int lane) {
+    const int l15 = lane & 15, kq = lane >> 4;
+    i32x4* part = reinterpret_cast<i32x4*>(smem);
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int r = 0; r < RB; ++r) part[(wave * TB * RB + t * RB + r) * 64 + lane] = acc[t][r];
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < OUT; ++u) {
+        const int b = wave + u * WV;
+        const int row = b / RB * 16 + l15, col = b % RB * 16 + kq * 4;   // d_out % 8 == 0: 4 columns are all in or all out
+        if (b >= TB * RB || row >= rows || col >= cols) continue;
+        i32x4 sum = part[b * 64 + lane];
+#pragma unroll
+        for (int v = 1; v < WV; ++v) sum += part[(v * TB * RB + b) * 64 + lane];
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (float)sum[i] * qs[u] * ws[u][i];
+        store4((TO*)a.out + (size_t)(row0 + row) * a.d_out + n0 + col, v);
+    }
 }
 
 // Few rows: TB x 16 rows of q, RB x 16 rows of W, WV wavefronts, each with every WV-th K tile of 128 inputs and a ring of its own of
@@ -135,8 +194,6 @@ __global__ __launch_bounds__(WV * 64) void gemm_i8_wave_kernel(const GemmI8Args 
     const int rows = rt.rows, e = rt.e, row0 = rt.row0;
     const int n0 = tile_n * a.tile_cols, cols = min(a.tile_cols, a.d_out - n0);
     const uint32_t ld = (uint32_t)a.d_in;
-    const I8Operand xr = i8_operand(a.q + (size_t)row0 * ld, rows, ld);
-    const I8Operand wr = i8_operand(a.W + ((size_t)e * a.d_out + n0) * ld, cols, ld);
     unsigned char* const ring = smem + wave * D * (TB + RB) * 2048;
 
     // scales of the blocks that this wavefront writes in the end: on their way before anything else
@@ -150,28 +207,16 @@ __global__ __launch_bounds__(WV * 64) void gemm_i8_wave_kernel(const GemmI8Args 
         ws[u] = *reinterpret_cast<const f32x4*>(a.w_scale + (size_t)e * a.d_out + n0 + min(b % RB * 16 + kq * 4, cols - 4));
     }
 
-    // An instruction moves 8 rows x 128 bytes; 16-byte chunk c of row r lies at position swz(r, c).  Rows past the tile's last load
-    // zeros, as do a last K tile's columns past d_in.  Requests go on past the last tile, from behind the matrices' end, so that their
-    // number is always the same.
-    const int rsub = lane >> 3, p = lane & 7;
+    WaveOperand<TB> x(a.q + (size_t)row0 * ld, rows, ld, lane);
+    WaveOperand<RB> w(a.W + ((size_t)e * a.d_out + n0) * ld, cols, ld, lane);
     const int nk = ceil_div(a.d_in, 128), n = wave < nk ? (nk - 1 - wave) / WV + 1 : 0;
-    const int last = a.d_in % 128 != 0 ? nk - 1 : -1;   // the K tile that is partly there
-    const uint32_t c_even = (uint32_t)swz(rsub, p) * 16, c_odd = (uint32_t)swz(rsub + 8, p) * 16;   // chunk of rows j * 8 + rsub
-    const uint32_t even = (uint32_t)rsub * ld + c_even, odd = (uint32_t)rsub * ld + c_odd;
-    const uint32_t left = ld % 128;
-    const uint32_t even_last = c_even < left ? even : kOutside, odd_last = c_odd < left ? odd : kOutside;
-    uint32_t v_even, v_odd, kbase;
     auto at_tile = [&](int kt) {
-        v_even = kt == last ? even_last : even;
-        v_odd = kt == last ? odd_last : odd;
-        kbase = kt < nk ? (uint32_t)kt * 128 : kOutside;
+        x.at_tile(kt, nk);
+        w.at_tile(kt, nk);
     };
-    const uint32_t ld8 = ld * 8;
-    // load i of that K tile: W's first
-    auto request = [&](unsigned char* slot, int i) {
-        const int j = i < NW ? i : i - NW;
-        if (i < NW) i8_load_lds<kReadOnceI8>(wr, slot + i * 1024, j & 1 ? v_odd : v_even, (int)(kbase + (uint32_t)j * ld8));
-        else i8_load_lds<0>(xr, slot + i * 1024, j & 1 ? v_odd : v_even, (int)(kbase + (uint32_t)j * ld8));
+    auto request = [&](unsigned char* slot, int i) {   // load i of that K tile: W's first
+        if (i < NW) w.template request<kReadOnceI8>(slot, i);
+        else x.template request<0>(slot + NW * 1024, i - NW);
     };
 #pragma unroll
     for (int d = 0; d < D; ++d) {
@@ -230,26 +275,99 @@ __global__ __launch_bounds__(WV * 64) void gemm_i8_wave_kernel(const GemmI8Args 
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land in what follows
     __syncthreads();
 
-    // W is the first operand: a lane holds 4 consecutive columns of row l15 of a block.  [wave][block][lane] in LDS.
-    i32x4* part = reinterpret_cast<i32x4*>(smem);
+    wave_i8_sums<TO, TB, RB, WV>(a, acc, smem, qs, ws, row0, rows, n0, cols, wave, lane);
+}
+
+// ------------------------------------------------------------------------------------------
+// A few tokens and their quantisation in one launch (meteora_base_gemm_i8): every workgroup quantises all of x itself, into LDS, while
+// the first tiles of W are on their way.  That reads x once per workgroup from L2, which up to 32 KB of it (bf16) costs less than the launch.
+// W goes through the wavefronts' rings as above; a lane without a row of its own multiplies another's, and its result is not kept.
+// ------------------------------------------------------------------------------------------
+constexpr int kRowThreads = 256, kRowMaxTokens = 4, kRowMaxBytes = 16384;   // T * d_in, x in 8 bits
+constexpr int row_i8_stride(int d_in) { return (d_in + 127) / 128 * 128 + 16; }   // rows start 4 banks apart
+template <int RB, int D>
+constexpr int row_i8_ring_bytes() { return 4 * D * RB * 2048; }   // and the sums in its place
+template <int RB, int D>
+constexpr int row_i8_lds_most() { return row_i8_ring_bytes<RB, D>() + kRowMaxBytes + kRowMaxTokens * (127 + 16); }
+
+template <typename TX, int RB, int D, int G, int HELD>
+__global__ __launch_bounds__(kRowThreads) void gemm_i8_row_kernel(const GemmI8Args a, const TX* __restrict__ x) {
+    constexpr int WV = 4, NL = 2 * RB;
+    static_assert(kRowThreads == kQuantThreads && D >= 2 && (D - 1) * NL < 64, "a workgroup quantises a row; vmcnt");
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    __shared__ float red[4], row_scale[kRowMaxTokens];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l15 = lane & 15, kq = lane >> 4;
+    const int n0 = xcd_order(blockIdx.x, a.tiles_n) * a.tile_cols, cols = min(a.tile_cols, a.d_out - n0);
+    const uint32_t ld = (uint32_t)a.d_in;
+    unsigned char* const ring = smem + wave * D * RB * 2048;
+    unsigned char* const xq = smem + row_i8_ring_bytes<RB, D>();
+    const int stride = row_i8_stride(a.d_in);
+
+    WaveOperand<RB> w(a.W + (size_t)n0 * ld, cols, ld, lane);
+    const int nk = ceil_div(a.d_in, 128), n = wave < nk ? (nk - 1 - wave) / WV + 1 : 0;
 #pragma unroll
-    for (int t = 0; t < TB; ++t)
+    for (int d = 0; d < D; ++d) {
+        w.at_tile(wave + d * WV, nk);
 #pragma unroll
-        for (int r = 0; r < RB; ++r) part[(wave * TB * RB + t * RB + r) * 64 + lane] = acc[t][r];
-    __syncthreads();
+        for (int i = 0; i < NL; ++i) w.template request<kReadOnceI8>(ring + d * RB * 2048, i);
+    }
+    {
+        // one row by the workgroup, several by a wavefront each
+        QuantRow<TX, G, HELD> r;
+        const int pieces = a.d_in / 8;
+        for (int t = tid / G; t < a.T; t += kRowThreads / G) {
+            const TX* src = x + (size_t)t * a.d_in;
+            r.load(src, pieces);
+            const float top = r.top(src, pieces, red);
+            r.store(src, pieces, top, [&](int i, uint2 v) { *reinterpret_cast<uint2*>(xq + t * stride + i * 8) = v; });
+            if ((tid & (G - 1)) == 0) row_scale[t] = top / 127.f;
+        }
+    }
+    float qs[(RB + WV - 1) / WV];
+    f32x4 ws[(RB + WV - 1) / WV];
+    constexpr int OUT = (RB + WV - 1) / WV;
 #pragma unroll
     for (int u = 0; u < OUT; ++u) {
-        const int b = wave + u * WV;
-        const int row = b / RB * 16 + l15, col = b % RB * 16 + kq * 4;   // d_out % 8 == 0: 4 columns are all in or all out
-        if (b >= TB * RB || row >= rows || col >= cols) continue;
-        i32x4 sum = part[b * 64 + lane];
-#pragma unroll
-        for (int v = 1; v < WV; ++v) sum += part[(v * TB * RB + b) * 64 + lane];
-        float v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (float)sum[i] * qs[u] * ws[u][i];
-        store4((TO*)a.out + (size_t)(row0 + row) * a.d_out + n0 + col, v);
+        const int b = min(wave + u * WV, RB - 1);
+        ws[u] = *reinterpret_cast<const f32x4*>(a.w_scale + n0 + min(b * 16 + kq * 4, cols - 4));
     }
+    __syncthreads();   // x is there (and so are W's first tiles: the compiler has waited for the loads of x, which are younger)
+#pragma unroll
+    for (int u = 0; u < OUT; ++u) qs[u] = row_scale[min(l15, a.T - 1)];
+    const unsigned char* const mine = xq + (l15 % a.T) * stride;
+
+    i32x4 acc[1][RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) acc[0][r] = i32x4{0, 0, 0, 0};
+    int slot = 0;
+    for (int i = 0; i < n; ++i) {
+        // of the loads only those of the D - 1 tiles behind this one may be in flight
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * NL) : "memory");
+        u32x4 wf[2][RB], xf[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+                wf[ks][r] = *reinterpret_cast<const u32x4*>(ring + (slot * RB + r) * 2048 + l15 * 128 + swz(l15, ks * 4 + kq) * 16);
+            xf[ks] = *reinterpret_cast<const u32x4*>(mine + (wave + i * WV) * 128 + (ks * 4 + kq) * 16);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot is read
+        w.at_tile(wave + (i + D) * WV, nk);
+#pragma unroll
+        for (int j = 0; j < NL; ++j) w.template request<kReadOnceI8>(ring + slot * RB * 2048, j);
+        slot = slot + 1 == D ? 0 : slot + 1;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+                acc[0][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, wf[ks][r]),
+                                                                  __builtin_bit_cast(i32x4, xf[ks]), acc[0][r], 0, 0, 0);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land in what follows
+    __syncthreads();
+    wave_i8_sums<TX, 1, RB, WV>(a, acc, smem, qs, ws, 0, a.T, n0, cols, wave, lane);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -670,6 +788,36 @@ static hipError_t launch_i8(const GemmI8Args& a, hipStream_t stream) {
     }
 }
 
+template <typename TX, int RB, int D>
+static hipError_t launch_row(GemmI8Args a, const TX* x, hipStream_t stream) {
+    a.tile_cols = wave_tile_cols(1, a.d_out, RB * 16);
+    a.tiles_n = ceil_div(a.d_out, a.tile_cols);
+    const int lds = row_i8_ring_bytes<RB, D>() + a.T * row_i8_stride(a.d_in);
+    auto go = [&](auto kern) {
+        const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(kern), row_i8_lds_most<RB, D>());
+        if (e != hipSuccess) return e;
+        kern<<<a.tiles_n, kRowThreads, lds, stream>>>(a, x);
+        return hipGetLastError();
+    };
+    if (a.T == 1) return a.d_in <= 4096 ? go(&gemm_i8_row_kernel<TX, RB, D, 256, 2>) : go(&gemm_i8_row_kernel<TX, RB, D, 256, 8>);
+    return a.d_in <= 4096 ? go(&gemm_i8_row_kernel<TX, RB, D, 64, 8>) : go(&gemm_i8_row_kernel<TX, RB, D, 64, 16>);
+}
+
+// Against two launches, W not in the caches, GPU alone (an eager call saves 3 us of the host as well): 1, 2 and 4 x 4096 -> 4096 6.9, 7.9,
+// 8.1 and 8.5, 8.9, 8.9 us, -> 14336 12.4, 13.7, 13.9 and 15.5, 15.5, 15.6; 1 and 3 x 5120 -> 13824 14.8, 17.3 and 17.2, 17.4; 1 x 14336 ->
+// 4096 14.1 and 15.5; 8 x 4096 -> 4096 10.2 and 9.1.  32 columns a tile and 16: 1 x 4096 -> 4096 7.3 and 6.9, -> 14336 12.4 and 14.4.
+bool base_gemm_i8_in_one(int T, int d_in) { return T <= kRowMaxTokens && T * d_in <= kRowMaxBytes; }
+
+template <typename TX>
+static hipError_t launch_base(const GemmI8Args& a, const TX* x, hipStream_t stream) {
+    return a.d_out <= 4096 ? launch_row<TX, 1, 5>(a, x, stream) : launch_row<TX, 2, 3>(a, x, stream);
+}
+hipError_t launch_base_gemm_i8_in_one(const void* x, const int8_t* W, const float* w_scale, int T, int d_in, int d_out, bool bf16,
+                                      void* out, hipStream_t stream) {
+    const GemmI8Args a{nullptr, nullptr, W, w_scale, nullptr, out, T, d_in, d_out, 1, 1, 0, 0};
+    return bf16 ? launch_base(a, (const bf16_t*)x, stream) : launch_base(a, (const float*)x, stream);
+}
+
 hipError_t launch_gemm_i8(const int8_t* q, const float* q_scale, const int8_t* W, const float* w_scale, const int32_t* offsets,
                           int T, int d_in, int d_out, int N, bool bf16, void* out, hipStream_t stream) {
     const GemmI8Args a{q, q_scale, W, w_scale, offsets, out, T, d_in, d_out, N, 0, 0, 0};
@@ -685,13 +833,23 @@ static hipError_t init_ring() {
     const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_ring_kernel<TO, MB, NB, D, true>), ring_i8_lds<MB, NB, D>());
     return e != hipSuccess ? e : ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_ring_kernel<TO, MB, NB, D, false>), ring_i8_lds<MB, NB, D>());
 }
+template <typename TX, int RB, int D>
+static hipError_t init_row() {
+    hipError_t e = hipSuccess;
+    for (const void* k : {reinterpret_cast<const void*>(&gemm_i8_row_kernel<TX, RB, D, 256, 2>),
+                          reinterpret_cast<const void*>(&gemm_i8_row_kernel<TX, RB, D, 256, 8>),
+                          reinterpret_cast<const void*>(&gemm_i8_row_kernel<TX, RB, D, 64, 8>),
+                          reinterpret_cast<const void*>(&gemm_i8_row_kernel<TX, RB, D, 64, 16>)})
+        if (e == hipSuccess) e = ensure_lds_limit(k, row_i8_lds_most<RB, D>());
+    return e;
+}
 template <typename TO>
-static hipError_t init_i8() {   // every kernel that launch_i8 may start
+static hipError_t init_i8() {   // every kernel that launch_i8 and launch_base may start
     hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_one_kernel<TO, 2, 4>), one_i8_lds<TO, 2, 4>());
     for (hipError_t f : {init_wave<TO, 1, 1, 4, 5>(), init_wave<TO, 1, 2, 4, 5>(), init_wave<TO, 1, 4, 4, 3>(), init_wave<TO, 2, 2, 4, 4>(),
                          init_ring<TO, 2, 2, 5>(), init_ring<TO, 3, 2, 5>(), init_ring<TO, 4, 2, 4>(), init_ring<TO, 4, 4, 3>(),
                          init_ring<TO, 4, 4, 2>(), init_ring<TO, 6, 4, 3>(), init_ring<TO, 7, 4, 3>(), init_ring<TO, 8, 4, 3>(),
-                         init_ring<TO, 8, 8, 2>()})
+                         init_ring<TO, 8, 8, 2>(), init_row<TO, 1, 5>(), init_row<TO, 2, 3>()})
         if (e == hipSuccess) e = f;
     return e;
 }

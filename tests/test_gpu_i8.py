@@ -215,6 +215,22 @@ def test_base_gemm_i8(T, d_in, d_out, dtype):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,d_in,d_out", [(1, 16384, 24), (1, 4112, 5000), (1, 144, 4104), (2, 8192, 264), (2, 8176, 4120), (3, 5456, 40),
+                                          (3, 48, 8200), (4, 4096, 8200), (4, 4080, 16), (4, 4112, 64), (5, 3264, 64), (1, 16400, 64)])
+def test_base_gemm_i8_of_a_few_tokens(T, d_in, d_out, dtype):
+    """Either side of what quantises inside the product, against the two calls, which it equals."""
+    g = gen(T * 3 + d_in)
+    x = torch.randn((T, d_in), generator=g, device="cuda").to(dtype)
+    x[0, d_in - 1] = 7.0   # the largest in the last place
+    W, ws = m.quantize_rows(torch.randn((d_out, d_in), generator=g, device="cuda"))
+    out = torch.full((T + 1, d_out), 7.0, device="cuda", dtype=dtype)
+    m.base_gemm_i8(x, W, ws, out=out[:T])
+    q, s = m.quantize_rows(x)
+    assert torch.equal(out[:T], m.gemm_i8(q, s, W, ws, dtype=dtype)) and (out[T] == 7).all()
+    close(out[:T], dense_ref(q, x.abs().amax(1).double() / 127, W, ws), 4)
+
+
 @pytest.mark.parametrize("T", [1, 4, 64, 500])
 def test_base_gemm_i8_rows_of_zeros(T):
     x = torch.zeros((T, 256), device="cuda", dtype=torch.bfloat16)
