@@ -512,17 +512,21 @@ def gemm_i8(q, q_scale, W, w_scale, offsets=None, out: Optional[torch.Tensor] = 
     """meteora_gemm_i8: out[t,c] = q_scale[t] * w_scale[e,c] * sum_i q[t,i] W[e,c,i].  W[d_out,d_in] and w_scale[d_out] without
     offsets, W[N,d_out,d_in] and w_scale[N,d_out] with offsets[N+1].  `dtype`: of the output, if there is no `out`."""
     T, d_in = q.shape
-    if (W.dim() == 3) != (offsets is not None):
+    if W.dim() != (2 if offsets is None else 3):
         raise ValueError("a W of one matrix per group needs offsets, a single matrix none")
     d_out = W.shape[-2]
     N = 1 if offsets is None else W.shape[0]
-    _chk(q, "q", torch.int8); _chk(q_scale, "q_scale", torch.float32, (T,))
-    _chk(W, "W", torch.int8, (d_out, d_in) if offsets is None else (N, d_out, d_in))
-    _chk(w_scale, "w_scale", torch.float32, (d_out,) if offsets is None else (N, d_out))
-    _chk(offsets, "offsets", torch.int32, (N + 1,))
     if out is None:
         out = torch.empty((T, d_out), dtype=dtype, device=q.device)
-    _chk(out, "out", None, (T, d_out))
+    # written out, as in linear_forward
+    if not (q.dtype == torch.int8 and W.dtype == torch.int8 and q_scale.dtype == torch.float32 and w_scale.dtype == torch.float32 and
+            q_scale.shape == (T,) and W.shape[-1] == d_in and w_scale.shape == W.shape[:-1] and out.shape == (T, d_out) and
+            q.is_cuda and q.is_contiguous() and q_scale.is_contiguous() and W.is_contiguous() and w_scale.is_contiguous() and
+            out.is_contiguous()):
+        _chk(q, "q", torch.int8); _chk(q_scale, "q_scale", torch.float32, (T,))
+        _chk(W, "W", torch.int8, (d_out, d_in) if offsets is None else (N, d_out, d_in))
+        _chk(w_scale, "w_scale", torch.float32, (d_out,) if offsets is None else (N, d_out)); _chk(out, "out", None, (T, d_out))
+    _chk(offsets, "offsets", torch.int32, (N + 1,))
     _chk_device(q, q_scale, W, w_scale, offsets, out)
     st = load_library().meteora_gemm_i8(_p(q), _p(q_scale), _p(W), _p(w_scale), _p(offsets), T, d_in, d_out, N, _dt(out),
                                         _p(out), _stream())
@@ -571,13 +575,15 @@ def sort_tokens(x, topk_idx, N: int, quantize: bool = False, out: Optional[torch
     k = topk_idx.shape[1]
     dev = x.device
     dtype = torch.int8 if quantize else x.dtype
-    _chk(x, "x"); _chk(topk_idx, "topk_idx", torch.int32, (T, k)); _chk(ws, "ws", torch.uint8)
     if out is None:
         out = torch.empty((T * k, d), dtype=dtype, device=dev)
-    _chk(out, "out", dtype, (T * k, d))
+    # written out, as in linear_forward
+    if not (x.is_cuda and x.is_contiguous() and topk_idx.dtype == torch.int32 and topk_idx.shape == (T, k) and
+            topk_idx.is_contiguous() and out.dtype == dtype and out.shape == (T * k, d) and out.is_contiguous()):
+        _chk(x, "x"); _chk(topk_idx, "topk_idx", torch.int32, (T, k)); _chk(out, "out", dtype, (T * k, d))
+    _chk(ws, "ws", torch.uint8)
     scale = torch.empty((T * k,), dtype=torch.float32, device=dev) if quantize else None
-    pos = torch.empty((T, k), dtype=torch.int32, device=dev)
-    offsets = torch.empty((N + 1,), dtype=torch.int32, device=dev)
+    pos, offsets = topk_idx.new_empty((T, k)), topk_idx.new_empty((N + 1,))
     ws = _ws(ws, lambda: sort_workspace_bytes(T, k, N), dev)
     _chk_device(x, topk_idx, out, ws)
     st = load_library().meteora_sort_tokens(_p(x), _p(topk_idx), T, k, N, d, _dt(x), _p(out), _p(scale), _p(pos), _p(offsets),
@@ -593,11 +599,15 @@ def unsort_tokens(ys, pos, w=None, scale: float = 1.0, base: Optional[torch.Tens
     gradient of sort_tokens."""
     rows, d = ys.shape
     T, k = pos.shape
-    _chk(ys, "ys"); _chk(pos, "pos", torch.int32, (T, k)); _chk(w, "w", torch.float32, (T, k))
-    _chk(base, "base", ys.dtype, (T, d))
     if out is None:
-        out = torch.empty((T, d), dtype=ys.dtype, device=ys.device)
-    _chk(out, "out", ys.dtype, (T, d))
+        out = ys.new_empty((T, d))
+    # written out, as in linear_forward
+    if not (ys.is_cuda and ys.is_contiguous() and pos.is_contiguous() and pos.dtype == torch.int32 and out.is_contiguous() and
+            out.dtype == ys.dtype and out.shape == (T, d) and
+            (w is None or (w.dtype == torch.float32 and w.shape == (T, k) and w.is_contiguous())) and
+            (base is None or (base.dtype == ys.dtype and base.shape == (T, d) and base.is_contiguous()))):
+        _chk(ys, "ys"); _chk(pos, "pos", torch.int32, (T, k)); _chk(w, "w", torch.float32, (T, k))
+        _chk(base, "base", ys.dtype, (T, d)); _chk(out, "out", ys.dtype, (T, d))
     _chk_device(ys, pos, w, base, out)
     st = load_library().meteora_unsort_tokens(_p(ys), rows, _p(pos), _p(w), T, k, d, float(scale), _dt(ys), _p(base), _p(out),
                                               _stream())

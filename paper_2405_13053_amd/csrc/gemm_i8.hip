@@ -714,33 +714,39 @@ static hipError_t launch_one_i8(GemmI8Args a, hipStream_t stream) {
 }
 
 // ---- which kernel and tile: the one that takes the least by
-//     us^3 = (launch + rounds * (round + nk * step) + tiles / 256 * nk * share)^3 + (bytes / 6e6)^3
-// nk K tiles, rounds of one (or per_cu) tiles per CU, bytes read and written once.  The four times of a tile shape are fitted to 350
-// dense sizes (1 to 8192 rows, 256 to 14336 inputs and outputs, W not in the caches), within 3 to 11% of them; on these sizes the choice is
-// 1.1% slower on average than the best shape of each.  Groups: how their rows are dealt is on the device, so the sum of two deals
-// decides, even, and 7/8 of the rows to an eighth of the groups: 2.2% slower than the best on 216 even deals, 4.7% on as many that fall
-// off as 1 / j^2 (2.1 and 11.9% by the even deal alone).
+//     us^3 = (launch + rounds * (round + nk * step) + tiles / 256 * nk * share)^3 + (bytes / rate)^3
+// nk K tiles, rounds of one (or per_cu) tiles per CU, bytes read and written once, 6 TB/s by the wavefront rings and 5.5 by the others.
+// The four times of a tile shape are fitted to 350 dense sizes (1 to 8192 rows, 256 to 14336 inputs and outputs, W not in the caches),
+// within 3 to 11% of them; on these sizes the choice is 1.1% slower on average than the best shape of each.  Groups: how their rows are
+// dealt is known on the device only, so two deals are weighed 7 to 3, an even one and 7/8 of the rows to an eighth of the groups: 1.7%
+// slower than the best on 216 even deals, 6.7% on as many that fall off as 1 / j^2 (2.1 and 11.9% by the even deal alone).
 struct I8Shape {
     int rows, cols, per_cu;
     bool wave;              // gemm_i8_wave_kernel
     float launch, round, step, share;
 };
 constexpr I8Shape kI8Shapes[] = {
-    {16, 16, 1, true, 3.12f, 0.85f, 0.054f, 0.f},     {16, 32, 1, true, 2.08f, 1.87f, 0.099f, 0.f},
-    {16, 64, 1, true, 1.65f, 2.19f, 0.126f, 0.031f},  {32, 32, 1, true, 2.44f, 1.78f, 0.116f, 0.019f},
-    {64, 64, 1, false, 2.22f, 1.82f, 0.152f, 0.079f}, {96, 64, 1, false, 2.06f, 2.09f, 0.180f, 0.097f},
-    {128, 64, 1, false, 2.02f, 2.20f, 0.210f, 0.126f}, {128, 128, 1, false, 1.98f, 2.67f, 0.337f, 0.173f},
-    {128, 128, 2, false, 1.68f, 2.59f, 0.357f, 0.295f}, {192, 128, 1, false, 2.01f, 3.57f, 0.438f, 0.198f},
-    {224, 128, 1, false, 2.06f, 3.95f, 0.487f, 0.208f}, {256, 128, 1, false, 1.94f, 4.46f, 0.548f, 0.235f},
-    {256, 256, 1, false, 1.53f, 7.18f, 0.932f, 0.349f},
+    {16, 16, 1, true, 3.12f, 0.85f, 0.054f, 0.000f},
+    {16, 32, 1, true, 2.08f, 1.87f, 0.099f, 0.000f},
+    {16, 64, 1, true, 1.65f, 2.19f, 0.126f, 0.031f},
+    {32, 32, 1, true, 2.44f, 1.78f, 0.116f, 0.019f},
+    {64, 64, 1, false, 2.17f, 1.86f, 0.153f, 0.075f},
+    {96, 64, 1, false, 2.00f, 2.14f, 0.181f, 0.092f},
+    {128, 64, 1, false, 1.98f, 2.24f, 0.211f, 0.122f},
+    {128, 128, 1, false, 1.98f, 2.67f, 0.337f, 0.171f},
+    {128, 128, 2, false, 1.74f, 2.53f, 0.357f, 0.294f},
+    {192, 128, 1, false, 2.02f, 3.56f, 0.438f, 0.197f},
+    {224, 128, 1, false, 2.08f, 3.92f, 0.487f, 0.207f},
+    {256, 128, 1, false, 1.98f, 4.42f, 0.548f, 0.234f},
+    {256, 256, 1, false, 1.66f, 7.04f, 0.932f, 0.347f},
 };
 constexpr int kI8ShapeCount = sizeof(kI8Shapes) / sizeof(kI8Shapes[0]);
 
-static float shape_us(const GemmI8Args& a, const I8Shape& s, float row_tiles, int cols, float groups) {
+static float shape_us(const GemmI8Args& a, const I8Shape& s, float row_tiles, int cols, float groups) {   // groups: with rows
     const float nk = (float)ceil_div(a.d_in, kI8Tile), tiles = row_tiles * (float)ceil_div(a.d_out, cols);
     const float rounds = ceilf(tiles / (float)(256 * s.per_cu));
     const float own = s.launch + rounds * (s.round + nk * s.step) + tiles / 256.f * nk * s.share;
-    const float mem = (groups * (float)a.d_out * (float)a.d_in + (float)a.T * ((float)a.d_in + 2.f * (float)a.d_out)) / 6e6f;
+    const float mem = (groups * (float)a.d_out * (float)a.d_in + (float)a.T * ((float)a.d_in + 2.f * (float)a.d_out)) / (s.wave ? 6e6f : 5.5e6f);
     return cbrtf(own * own * own + mem * mem * mem);
 }
 
@@ -759,7 +765,7 @@ static int choose_shape(const GemmI8Args& a) {
             const float even = (float)N * (float)ceil_div(ceil_div(a.T, N), s.rows);
             const float skewed = (float)many * (float)ceil_div(ceil_div(in_many, many), s.rows) +
                                  (few > 0 ? (float)few * (float)ceil_div(ceil_div(in_few, few), s.rows) : 0.f);
-            us = shape_us(a, s, even, cols, (float)N) + shape_us(a, s, skewed, cols, (float)(many + few));
+            us = 0.7f * shape_us(a, s, even, cols, (float)N) + 0.3f * shape_us(a, s, skewed, cols, (float)(many + few));
         }
         if (i == 0 || us < least) { least = us; best = i; }
     }
