@@ -87,7 +87,7 @@ meteora_status meteora_base_gemm_i8(const void* x, const int8_t* W, const float*
 
 size_t meteora_sort_workspace_bytes(int T, int k, int N) {
     if (!sort_shape_ok(T, k, N) || !sort_shape_supported(T, k, N)) return 0;
-    return align_up(sort_count_bytes_reserved(T, k, N), 256) + 256;
+    return align_up(sort_count_bytes(N), 256) + 256;
 }
 
 meteora_status meteora_sort_tokens(const void* x, const int32_t* topk_idx, int T, int k, int N, int d, meteora_dtype dt, void* xs,
@@ -98,7 +98,7 @@ meteora_status meteora_sort_tokens(const void* x, const int32_t* topk_idx, int T
     if (!aligned(x, 16) || !aligned(topk_idx, 16) || !aligned(xs, 16) || !aligned(pos, 4) || !aligned(offsets, 4) ||
         (xs_scale && !aligned(xs_scale, 4)))
         return METEORA_ERR_UNSUPPORTED;
-    if (!ws || !aligned(ws, 256) || ws_bytes < sort_count_bytes(T, k, N)) return METEORA_ERR_WORKSPACE;
+    if (!ws || !aligned(ws, 256) || (T > 0 && ws_bytes < sort_count_bytes(N))) return METEORA_ERR_WORKSPACE;
     if (T == 0) return METEORA_OK;
     return status(launch_sort_tokens(x, topk_idx, T, k, N, d, dt == METEORA_BF16, xs, xs_scale, pos, offsets,
                                      static_cast<int32_t*>(ws), static_cast<hipStream_t>(stream)));

@@ -235,9 +235,8 @@ hipError_t launch_base_gemm_i8_in_one(const void* x, const int8_t* W, const floa
                                       void* out, hipStream_t stream);
 
 // ---- rows sorted by adapter: pos[T,k], offsets[N+1], xs[pos[t,j]] = x[t] (with xs_scale: as 8-bit whole numbers), and back
-// (rows: those of ys; base, w, dw may be nullptr).  chunk_counts: sort_count_bytes, or sort_count_bytes_reserved for any smaller T too.
-size_t sort_count_bytes(int T, int k, int N);
-size_t sort_count_bytes_reserved(int T, int k, int N);
+// (rows: those of ys; base, w, dw may be nullptr).  chunk_counts: sort_count_bytes, whatever T.
+size_t sort_count_bytes(int N);
 hipError_t launch_sort_tokens(const void* x, const int32_t* topk_idx, int T, int k, int N, int d, bool bf16, void* xs,
                               float* xs_scale, int32_t* pos, int32_t* offsets, int32_t* chunk_counts, hipStream_t stream);
 hipError_t launch_unsort_tokens(const void* ys, int64_t rows, const int32_t* pos, const float* w, int T, int k, int d, bool bf16,

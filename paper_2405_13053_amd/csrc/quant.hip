@@ -24,7 +24,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_rows_kernel(const TX* 
 
 template <typename TX>
 static hipError_t launch_quantize(const TX* x, int rows, int d, int8_t* q, float* scale, hipStream_t stream) {
-    return quant_row_shape(d, [&](auto g, auto held) {
+    return quant_row_shape(d, rows >= 2048, [&](auto g, auto held) {
         constexpr int G = decltype(g)::value, HELD = decltype(held)::value;
         quantize_rows_kernel<TX, G, HELD><<<ceil_div(rows, kQuantThreads / G), kQuantThreads, 0, stream>>>(x, rows, d, q, scale);
         return hipGetLastError();
