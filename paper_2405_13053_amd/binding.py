@@ -621,10 +621,15 @@ def unsort_backward(dy, ys, pos, w=None, scale: float = 1.0, out: Optional[torch
     name are left as they were in `out` (zeros if there is none)."""
     rows, d = ys.shape
     T, k = pos.shape
-    _chk(dy, "dy", ys.dtype, (T, d)); _chk(ys, "ys"); _chk(pos, "pos", torch.int32, (T, k)); _chk(w, "w", torch.float32, (T, k))
+    dtype = ys.dtype
     if out is None:
-        out = torch.zeros((rows, d), dtype=ys.dtype, device=ys.device)
-    _chk(out, "out", ys.dtype, (rows, d))
+        out = torch.zeros((rows, d), dtype=dtype, device=ys.device)
+    # written out, as in linear_forward
+    if not (dy.dtype == dtype and dy.shape == (T, d) and out.dtype == dtype and out.shape == (rows, d) and pos.dtype == torch.int32 and
+            ys.is_cuda and ys.is_contiguous() and dy.is_contiguous() and out.is_contiguous() and pos.is_contiguous() and
+            (w is None or (w.dtype == torch.float32 and w.shape == (T, k) and w.is_contiguous()))):
+        _chk(dy, "dy", dtype, (T, d)); _chk(ys, "ys"); _chk(pos, "pos", torch.int32, (T, k)); _chk(w, "w", torch.float32, (T, k))
+        _chk(out, "out", dtype, (rows, d))
     _chk_device(dy, ys, pos, w, out)
     dw = torch.empty((T, k), dtype=torch.float32, device=dy.device) if want_dw else None
     st = load_library().meteora_unsort_backward(_p(dy), _p(ys), rows, _p(pos), _p(w), T, k, d, float(scale), _dt(ys), _p(out),

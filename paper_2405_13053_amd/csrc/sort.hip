@@ -467,13 +467,14 @@ hipError_t launch_unsort_tokens(const void* ys, int64_t rows, const int32_t* pos
     return hipGetLastError();
 }
 
-// One workgroup, or 2^lanes_log2 of its threads, per token.
-template <typename TX>
-__global__ __launch_bounds__(256) void unsort_backward_kernel(const UnsortArgs a, const u32x4* __restrict__ dy,
-                                                              const u32x4* __restrict__ ys, u32x4* __restrict__ dys,
-                                                              float* __restrict__ dw) {
-    __shared__ float part[4][kMaxTopK];
-    const int t = (int)((blockIdx.x * 256ll + threadIdx.x) >> a.lanes_log2);
+// One workgroup, or 2^lanes_log2 of its threads, per token.  THREADS: 256, and for few tokens with long rows 1024, so that the loop over a
+// row waits for memory fewer times.
+template <typename TX, int THREADS>
+__global__ __launch_bounds__(THREADS) void unsort_backward_kernel(const UnsortArgs a, const u32x4* __restrict__ dy,
+                                                                  const u32x4* __restrict__ ys, u32x4* __restrict__ dys,
+                                                                  float* __restrict__ dw) {
+    __shared__ float part[THREADS / 64][kMaxTopK];
+    const int t = (int)((blockIdx.x * (int64_t)THREADS + threadIdx.x) >> a.lanes_log2);
     const int lanes = 1 << a.lanes_log2;
     float dot[kMaxTopK] = {};
     if (t < a.T)
@@ -508,7 +509,7 @@ __global__ __launch_bounds__(256) void unsort_backward_kernel(const UnsortArgs a
                 if (j < a.k) dw[(size_t)t * a.k + j] = a.scale * dot[j];
         return;
     }
-    const int wave = threadIdx.x >> 6, per = lanes / 64;   // 2 or 4 wavefronts share a token
+    const int wave = threadIdx.x >> 6, per = lanes / 64;   // wavefronts that share a token
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
         for (int j = 0; j < kMaxTopK; ++j) part[wave][j] = dot[j];
@@ -525,10 +526,18 @@ hipError_t launch_unsort_backward(const void* dy, const void* ys, int64_t rows, 
                                   int d, bool bf16, float scale, void* dys, float* dw, hipStream_t stream) {
     UnsortArgs a{pos, w, T, k, d / (bf16 ? 8 : 4), rows, 0, 0, scale};
     a.lanes_log2 = lanes_log2_for(a.row16);
-    const unsigned grid = (unsigned)ceil_div64((int64_t)T << a.lanes_log2, 256);
-    if (bf16) unsort_backward_kernel<bf16_t><<<grid, 256, 0, stream>>>(a, (const u32x4*)dy, (const u32x4*)ys, (u32x4*)dys, dw);
-    else unsort_backward_kernel<float><<<grid, 256, 0, stream>>>(a, (const u32x4*)dy, (const u32x4*)ys, (u32x4*)dys, dw);
-    return hipGetLastError();
+    auto go = [&](auto kern, int threads) {
+        kern<<<(unsigned)ceil_div64((int64_t)T << a.lanes_log2, threads), threads, 0, stream>>>(a, (const u32x4*)dy, (const u32x4*)ys,
+                                                                                               (u32x4*)dys, dw);
+        return hipGetLastError();
+    };
+    // 256 threads to a row and 1024, top-2: 64 x 4096 7.5 and 6.8 us, 64 x 14336 14.4 and 9.3, 512 x 4096 10.0 and 10.1, 512 x 14336 25.8
+    // and 18.2, 1024 x 4096 12.3 and 16.9; top-8 300 x 5120 24.6 and 15.9
+    if (a.row16 >= 512 && T <= 512) {
+        a.lanes_log2 = 10;
+        return bf16 ? go(&unsort_backward_kernel<bf16_t, 1024>, 1024) : go(&unsort_backward_kernel<float, 1024>, 1024);
+    }
+    return bf16 ? go(&unsort_backward_kernel<bf16_t, 256>, 256) : go(&unsort_backward_kernel<float, 256>, 256);
 }
 
 }  // namespace meteora
