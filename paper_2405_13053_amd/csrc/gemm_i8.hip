@@ -33,6 +33,7 @@ struct GemmI8Args {
     int T, d_in, d_out, N;
     int tiles_m, tiles_n;   // row tiles of the grid (at least as many as there are), column tiles
     int tile_cols;          // columns of a tile (wave kernel)
+    int tail;               // 1: the tiles of a last, half-empty round are left to gemm_i8_ring_kernel's TAIL form
 };
 
 // The row tiles of all groups, each cut into tiles of BM rows, one group behind the other.  Whatever the offsets hold, the rows lie in
@@ -441,8 +442,16 @@ __device__ __forceinline__ void ring_i8_epilogue(const GemmI8Args& a, i32x4 (&ac
     }
 }
 
-// PART: d_in may end in a partial K tile
-template <typename TO, int MB, int NB, int D, bool PART>
+// 256 x 256 tiles, one to a CU, beyond whole rounds of 256 of them: up to 128 are done in smaller tiles, one or two to a CU, by a second
+// launch instead of as a round of their own.  The first of them:
+constexpr int kTailTiles = 128;
+__host__ __device__ constexpr int tail_start(int tiles) {
+    return tiles > 256 && tiles % 256 <= kTailTiles ? tiles - tiles % 256 : tiles;
+}
+
+// PART: d_in may end in a partial K tile.  TAIL: this workgroup's tile is a part of one of 256 x 256 behind tail_start (the number of
+// tiles of groups is known here only).
+template <typename TO, int MB, int NB, int D, bool PART, bool TAIL = false>
 __global__ __launch_bounds__(256) void gemm_i8_ring_kernel(const GemmI8Args a) {
     constexpr int BM = MB * 32, BN = NB * 32, PX = MB, PW = NB;   // 2 x 2 wavefronts; load instructions per wavefront and tile
     static_assert((NB % 2 == 0 || MB % 2 == 0) && D >= 2 && D <= 5 && (D - 1) * (PX + PW) < 64, "2 x 2 micro-blocks; vmcnt");
@@ -457,13 +466,23 @@ __global__ __launch_bounds__(256) void gemm_i8_ring_kernel(const GemmI8Args a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
     const int l15 = lane & 15, kq = lane >> 4;
-    const RowTiles<BM> row_tiles(a, lane);
-    if ((int)blockIdx.x >= row_tiles.count * a.tiles_n) return;
+    constexpr int PM = TAIL ? 256 / BM : 1, PN = TAIL ? 256 / BN : 1;   // tiles are dealt as PM x PN of them
+    const RowTiles<BM * PM> row_tiles(a, lane);
+    const int tiles = row_tiles.count * a.tiles_n;
+    const int id = TAIL ? tail_start(tiles) + (int)blockIdx.x / (PM * PN) : (int)blockIdx.x;
+    if (id >= (!TAIL && a.tail ? tail_start(tiles) : tiles)) return;
     int tile_m, tile_n;
-    tile_of_workgroup(blockIdx.x, row_tiles.count, a.tiles_n, tile_m, tile_n);
-    const RowTile rt = row_tiles.at(a, tile_m);
-    const int rows = rt.rows, e = rt.e, row0 = rt.row0;
-    const int n0 = tile_n * BN, cols = min(BN, a.d_out - n0);
+    tile_of_workgroup(id, row_tiles.count, a.tiles_n, tile_m, tile_n);
+    RowTile rt = row_tiles.at(a, tile_m);
+    int n0 = tile_n * BN * PN;
+    if constexpr (TAIL) {
+        const int m0 = (int)blockIdx.x % PM * BM;
+        rt.row0 += m0;
+        rt.rows = min(BM, rt.rows - m0);
+        n0 += (int)blockIdx.x / PM % PN * BN;
+        if (rt.rows <= 0 || n0 >= a.d_out) return;
+    }
+    const int rows = rt.rows, e = rt.e, row0 = rt.row0, cols = min(BN, a.d_out - n0);
 
     const int nk_main = a.d_in / kI8Tile, nk = nk_main + (PART && a.d_in % kI8Tile != 0 ? 1 : 0);
     const int8_t* xb = a.q + (size_t)row0 * a.d_in;
@@ -699,6 +718,40 @@ static hipError_t launch_ring_i8(GemmI8Args a, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// The tail of `rest` tiles of 256 x 256 at most
+template <typename TO, int MB, int NB, int D>
+static hipError_t launch_tail_i8(GemmI8Args a, int rest, hipStream_t stream) {
+    a.tiles_m = most_row_tiles(a, 256);
+    a.tiles_n = ceil_div(a.d_out, 256);
+    constexpr int lds = ring_i8_lds<MB, NB, D>();
+    const auto kern = a.d_in % kI8Tile != 0 ? &gemm_i8_ring_kernel<TO, MB, NB, D, true, true> : &gemm_i8_ring_kernel<TO, MB, NB, D, false, true>;
+    const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(kern), lds);
+    if (e != hipSuccess) return e;
+    kern<<<rest * (64 / (MB * NB)), 256, lds, stream>>>(a);
+    return hipGetLastError();
+}
+
+// Index in kI8Shapes of the tail's tiles: as small as one to a CU allows, two of the largest
+static int tail_shape(int rest) { return rest <= 16 ? 4 : rest <= 32 ? 6 : 8; }
+
+// 256 x 256 tiles, and the tail where there is, or (groups) may be, one.  As the best of the shapes with a round of their own for the rest,
+// and so, us: 4300, 5000, 6000 and 9000 x 4096 -> 4096 69.4, 77.7, 89.0, 141 and 69.2, 74.4, 83.8, 122; 5000 x 4096 -> 14336 247 and 235; 8
+// groups of 4096 -> 4096, 4002 and 8192 rows that fall off as 1 / j^2 92.5, 141 and 80.7, 123, dealt evenly (whole rounds: the second launch
+// finds nothing) 53.4, 102 and 55.1, 105.
+template <typename TO>
+static hipError_t launch_largest_i8(GemmI8Args a, hipStream_t stream) {
+    const int64_t tiles = (int64_t)most_row_tiles(a, 256) * ceil_div(a.d_out, 256);
+    a.tail = tiles > 256 && (a.offsets != nullptr || tail_start((int)tiles) != tiles) ? 1 : 0;
+    const hipError_t e = launch_ring_i8<TO, 8, 8, 2>(a, stream);
+    if (e != hipSuccess || a.tail == 0) return e;
+    const int rest = a.offsets != nullptr ? kTailTiles : (int)tiles - tail_start((int)tiles);
+    switch (tail_shape(rest)) {
+        case 4: return launch_tail_i8<TO, 2, 2, 5>(a, rest, stream);
+        case 6: return launch_tail_i8<TO, 4, 2, 4>(a, rest, stream);
+        default: return launch_tail_i8<TO, 4, 4, 2>(a, rest, stream);
+    }
+}
+
 template <typename TO, int MB, int NB>
 static hipError_t launch_one_i8(GemmI8Args a, hipStream_t stream) {
     static_assert(MB >= 2, "order of the fragments");
@@ -740,12 +793,20 @@ constexpr I8Shape kI8Shapes[] = {
     {256, 128, 1, false, 1.98f, 4.42f, 0.548f, 0.234f},
     {256, 256, 1, false, 1.66f, 7.04f, 0.932f, 0.347f},
 };
+static_assert(kI8Shapes[4].rows * kI8Shapes[4].cols == 64 * 64 && kI8Shapes[6].rows * kI8Shapes[6].cols == 128 * 64 &&
+              kI8Shapes[8].per_cu == 2, "tail_shape");
 constexpr int kI8ShapeCount = sizeof(kI8Shapes) / sizeof(kI8Shapes[0]);
 
 static float shape_us(const GemmI8Args& a, const I8Shape& s, float row_tiles, int cols, float groups) {   // groups: with rows
     const float nk = (float)ceil_div(a.d_in, kI8Tile), tiles = row_tiles * (float)ceil_div(a.d_out, cols);
-    const float rounds = ceilf(tiles / (float)(256 * s.per_cu));
-    const float own = s.launch + rounds * (s.round + nk * s.step) + tiles / 256.f * nk * s.share;
+    float rounds = ceilf(tiles / (float)(256 * s.per_cu)), tail = 0.f;
+    const float rest = tiles - 256.f * (rounds - 1.f);
+    if (s.rows * s.cols == 256 * 256 && rounds > 1.f && rest <= (float)kTailTiles) {
+        const I8Shape& q = kI8Shapes[tail_shape(a.offsets != nullptr ? kTailTiles : (int)rest)];
+        rounds -= 1.f;
+        tail = q.launch + q.round + nk * q.step + rest * (float)(256 * 256 / (q.rows * q.cols)) / 256.f * nk * q.share;
+    }
+    const float own = s.launch + rounds * (s.round + nk * s.step) + (tail > 0.f ? rounds : tiles / 256.f) * nk * s.share + tail;
     const float mem = (groups * (float)a.d_out * (float)a.d_in + (float)a.T * ((float)a.d_in + 2.f * (float)a.d_out)) / (s.wave ? 6e6f : 5.5e6f);
     return cbrtf(own * own * own + mem * mem * mem);
 }
@@ -790,7 +851,7 @@ static hipError_t launch_i8(const GemmI8Args& a, hipStream_t stream) {
         case 9: return launch_ring_i8<TO, 6, 4, 3>(a, stream);
         case 10: return launch_ring_i8<TO, 7, 4, 3>(a, stream);
         case 11: return launch_ring_i8<TO, 8, 4, 3>(a, stream);
-        default: return launch_ring_i8<TO, 8, 8, 2>(a, stream);
+        default: return launch_largest_i8<TO>(a, stream);
     }
 }
 
@@ -820,13 +881,13 @@ static hipError_t launch_base(const GemmI8Args& a, const TX* x, hipStream_t stre
 }
 hipError_t launch_base_gemm_i8_in_one(const void* x, const int8_t* W, const float* w_scale, int T, int d_in, int d_out, bool bf16,
                                       void* out, hipStream_t stream) {
-    const GemmI8Args a{nullptr, nullptr, W, w_scale, nullptr, out, T, d_in, d_out, 1, 1, 0, 0};
+    const GemmI8Args a{nullptr, nullptr, W, w_scale, nullptr, out, T, d_in, d_out, 1, 1, 0, 0, 0};
     return bf16 ? launch_base(a, (const bf16_t*)x, stream) : launch_base(a, (const float*)x, stream);
 }
 
 hipError_t launch_gemm_i8(const int8_t* q, const float* q_scale, const int8_t* W, const float* w_scale, const int32_t* offsets,
                           int T, int d_in, int d_out, int N, bool bf16, void* out, hipStream_t stream) {
-    const GemmI8Args a{q, q_scale, W, w_scale, offsets, out, T, d_in, d_out, N, 0, 0, 0};
+    const GemmI8Args a{q, q_scale, W, w_scale, offsets, out, T, d_in, d_out, N, 0, 0, 0, 0};
     return bf16 ? launch_i8<bf16_t>(a, stream) : launch_i8<float>(a, stream);
 }
 
@@ -838,6 +899,12 @@ template <typename TO, int MB, int NB, int D>
 static hipError_t init_ring() {
     const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_ring_kernel<TO, MB, NB, D, true>), ring_i8_lds<MB, NB, D>());
     return e != hipSuccess ? e : ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_ring_kernel<TO, MB, NB, D, false>), ring_i8_lds<MB, NB, D>());
+}
+template <typename TO, int MB, int NB, int D>
+static hipError_t init_tail() {
+    constexpr int lds = ring_i8_lds<MB, NB, D>();
+    const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_ring_kernel<TO, MB, NB, D, true, true>), lds);
+    return e != hipSuccess ? e : ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_ring_kernel<TO, MB, NB, D, false, true>), lds);
 }
 template <typename TX, int RB, int D>
 static hipError_t init_row() {
@@ -855,7 +922,7 @@ static hipError_t init_i8() {   // every kernel that launch_i8 and launch_base m
     for (hipError_t f : {init_wave<TO, 1, 1, 4, 5>(), init_wave<TO, 1, 2, 4, 5>(), init_wave<TO, 1, 4, 4, 3>(), init_wave<TO, 2, 2, 4, 4>(),
                          init_ring<TO, 2, 2, 5>(), init_ring<TO, 3, 2, 5>(), init_ring<TO, 4, 2, 4>(), init_ring<TO, 4, 4, 3>(),
                          init_ring<TO, 4, 4, 2>(), init_ring<TO, 6, 4, 3>(), init_ring<TO, 7, 4, 3>(), init_ring<TO, 8, 4, 3>(),
-                         init_ring<TO, 8, 8, 2>(), init_row<TO, 1, 5>(), init_row<TO, 2, 3>()})
+                         init_ring<TO, 8, 8, 2>(), init_tail<TO, 2, 2, 5>(), init_tail<TO, 4, 2, 4>(), init_tail<TO, 4, 4, 2>(), init_row<TO, 1, 5>(), init_row<TO, 2, 3>()})
         if (e == hipSuccess) e = f;
     return e;
 }

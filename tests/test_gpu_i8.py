@@ -127,6 +127,35 @@ def test_dense_large(T, d_in, d_out):
         close(m.gemm_i8(q, qs, W, ws, dtype=dtype), ref)
 
 
+@pytest.mark.parametrize("T,d_in,d_out", [(4300, 4096, 4096), (4600, 4112, 4096), (5000, 4096, 4104), (6001, 4096, 4096), (9000, 2064, 4096),
+                                          (1025, 4096, 16640), (20000, 512, 2040)])
+def test_dense_with_a_last_round_of_few_tiles(T, d_in, d_out):
+    """272, 288, 340, 384, 576, 325 and 632 tiles of 256 x 256: what lies behind whole rounds of 256 is done in smaller ones."""
+    g = gen(T + d_in)
+    q, W = int8((T, d_in), g), int8((d_out, d_in), g)
+    qs, ws = scales((T,), g), scales((d_out,), g)
+    ref = dense_ref(q, qs, W, ws)
+    for dtype in TYPES:
+        out = torch.full((T + 1, d_out), 7.0, device="cuda", dtype=dtype)
+        m.gemm_i8(q, qs, W, ws, out=out[:T])
+        close(out[:T], ref)
+        assert (out[T] == 7).all()
+
+
+@pytest.mark.parametrize("T,N,counts", [(4002, 8, [2624, 655, 291, 164, 105, 73, 53, 30]), (8192, 8, [5368, 1340, 595, 335, 214, 149, 100, 91]),
+                                        (4300, 3, [4296, 0, 1]), (9001, 28, [300] * 28), (4096, 8, [512] * 8)])
+def test_groups_with_a_last_round_of_few_tiles(T, N, counts):
+    g = gen(T + N)
+    d_in, d_out = 4096, 4096
+    q, qs, W, ws, off = grouped_case(T, N, d_in, d_out, counts, g)
+    out = torch.full((T, d_out), 7.0, device="cuda", dtype=torch.bfloat16)
+    m.gemm_i8(q, qs, W, ws, offsets=off.cuda(), out=out)
+    for e in range(N):
+        a, b = int(off[e]), int(off[e + 1])
+        close(out[a:b], dense_ref(q[a:b], qs[a:b], W[e], ws[e]))
+    assert (out[int(off[-1]):] == 7).all()
+
+
 @pytest.mark.parametrize("T", [1, 40, 300, 700])
 def test_the_largest_sums(T):
     """131056 inputs of -128 on both sides add up to just below 2^31; of -128 and 127 to the other end."""
