@@ -64,7 +64,7 @@ constexpr int kSortChunkPairs = 128;   // of the one-launch form, at most: 16 to
 
 struct SortShared {
     Counters before, rest;
-    int running[kMaxAdapters], wave_hist[4][kMaxAdapters];
+    int running[kMaxAdapters], wave_hist[2][4][kMaxAdapters];   // of the even and the odd steps: a step's is read into the next one
 };
 
 // The same for up to 256 pairs in all (decode), without a table: every wavefront holds all ids, and a place is the number of pairs
@@ -178,14 +178,15 @@ __device__ __forceinline__ void sort_positions(const SortArgs& a, SortShared& sh
             peers &= ((key >> bit) & 1) ? m : ~m;
         }
         const int rank = __popcll(peers & (lane == 0 ? 0ull : ~0ull >> (64 - lane)));
-        sh.wave_hist[wave][lane] = 0;
+        auto& hist = sh.wave_hist[i0 / kSortThreads & 1];
+        hist[wave][lane] = 0;
         __syncthreads();
-        if (valid && rank == 0) sh.wave_hist[wave][key] = __popcll(peers);
+        if (valid && rank == 0) hist[wave][key] = __popcll(peers);
         __syncthreads();
         int p = -1;
         if (valid) {
             p = sh.running[key] + rank;
-            for (int w = 0; w < wave; ++w) p += sh.wave_hist[w][key];
+            for (int w = 0; w < wave; ++w) p += hist[w][key];
         }
         if (in) {
             if (places != nullptr) places[i] = p;
@@ -193,8 +194,7 @@ __device__ __forceinline__ void sort_positions(const SortArgs& a, SortShared& sh
         }
         __syncthreads();
         if (i0 + kSortThreads < chunk_pairs && threadIdx.x < kMaxAdapters)
-            sh.running[threadIdx.x] += sh.wave_hist[0][threadIdx.x] + sh.wave_hist[1][threadIdx.x] +
-                                       sh.wave_hist[2][threadIdx.x] + sh.wave_hist[3][threadIdx.x];
+            sh.running[threadIdx.x] += hist[0][threadIdx.x] + hist[1][threadIdx.x] + hist[2][threadIdx.x] + hist[3][threadIdx.x];
     }
     __syncthreads();
 }

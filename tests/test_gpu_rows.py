@@ -101,6 +101,23 @@ def test_long_batches_agree_with_the_bucket_lists(T, N, k):
     assert all(torch.equal(a, b) for a, b in zip(few, want))
 
 
+@pytest.mark.parametrize("kind", ["uniform", "one", "padded"])
+def test_many_pairs_to_a_workgroup_again_and_again(kind):
+    T, N, k = 150000, 64, 8   # 4688 pairs to each of 256 workgroups, 256 at a time
+    g = gen(len(kind))
+    idx = routing(T, N, k, kind, g)
+    x = torch.zeros((T, 8), device="cuda", dtype=torch.bfloat16)
+    flat = idx.flatten()
+    order = torch.argsort(torch.where((flat >= 0) & (flat < N), flat, N).long(), stable=True)
+    want = torch.empty(T * k, device="cuda", dtype=torch.int32)
+    want[order] = torch.arange(T * k, device="cuda", dtype=torch.int32)
+    want[(flat < 0) | (flat >= N)] = -1
+    xs = torch.empty((T * k, 8), device="cuda", dtype=torch.bfloat16)
+    for _ in range(10):
+        _, pos, _ = m.sort_tokens(x, idx, N, out=xs)
+        assert torch.equal(pos.flatten(), want)
+
+
 # ---- back ----------------------------------------------------------------------------------------------------------------------
 def unsort_ref(ys, pos, w, scale, base):
     """(result, sum of magnitudes) in fp64."""
@@ -302,6 +319,35 @@ def test_graphs_that_share_a_workspace_and_another_stream():
         got = layer(x, idx, w, None, None)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got, out)
+
+
+def test_two_streams_at_once():
+    g = gen(37)
+    N, k, d_in, d_out = 8, 2, 1024, 520
+    E, esc = m.quantize_rows(torch.randn((N * d_out, d_in), generator=g, device="cuda"))
+    E, esc = E.view(N, d_out, d_in), esc.view(N, d_out)
+
+    def layer(x, idx, w, out):
+        xs, xsc, pos, off = m.sort_tokens(x, idx, N, quantize=True)
+        base = m.base_gemm_i8(x, E[0], esc[0])
+        return m.unsort_tokens(m.gemm_i8(xs, xsc, E, esc, offsets=off), pos, w, base=base, out=out)
+
+    work = []
+    for T in (2, 64, 777, 9000):
+        x = torch.randn((T, d_in), generator=g, device="cuda").bfloat16()
+        idx, w = routing(T, N, k, "padded", g), torch.rand((T, k), generator=g, device="cuda")
+        work.append((x, idx, w, layer(x, idx, w, None)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(4):
+        for a, b in zip(work, reversed(work)):
+            for stream, (x, idx, w, want) in zip(streams, (a, b)):
+                with torch.cuda.stream(stream):
+                    got.append((layer(x, idx, w, None), want))
+    torch.cuda.synchronize()
+    for y, want in got:
+        assert torch.equal(y, want)
 
 
 def test_gradients_inside_a_graph():
