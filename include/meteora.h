@@ -347,7 +347,8 @@ meteora_status meteora_base_gemm(const void* x, const void* W, int T, int d_in, 
  * Rows as 8-bit whole numbers with one scale each: the tokens of an activation, or the output channels of a weight
  * W[d_out, d_in] (its rows).  With a = max_i |x[t,i]|:
  *   scale[t] = a / 127,   q[t,i] = 127 * x[t,i] / a  rounded to the nearest whole number, halves to the even one
- * (the rounding of the exact quotient).  A row of zeros gives zeros and scale 0.  q lies in [-127, 127].
+ * (the rounding of the exact quotient).  A row of zeros gives zeros and scale 0.  q lies in [-127, 127].  A row that holds an
+ * infinity or a NaN gives zeros and scale infinity or NaN, so that its products are NaN and all others what they are.
  * Limits: d % 8 == 0, rows < 2^24.  x in dt; q, scale 16-byte aligned.
  */
 meteora_status meteora_quantize_rows(const void* x /*[rows,d]*/, int rows, int d, meteora_dtype dt,

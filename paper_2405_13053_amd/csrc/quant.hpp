@@ -1,5 +1,6 @@
 // Rows as 8-bit whole numbers with one scale each (device side, shared by quant.hip and sort.hip):
 //     a = max_i |x_i|,   q_i = 127 x_i / a rounded to the nearest whole number, halves to the even one,   scale = a / 127.
+// A row with an infinity or a NaN is zeros with that scale: a product of it is NaN, and no other row's.
 // The rounding is the exact quotient's: x_i = a / 2 is 63.5, and bf16 rows hold such values often (one in about 256 of the elements
 // of an octave), so whether a half is seen as one decides a whole step of the result.
 #pragma once
@@ -27,11 +28,14 @@ template <> struct Piece8<float> {
     __device__ __forceinline__ float at(int i) const { return v[i >> 2][i & 3]; }
 };
 
+// The larger one, NaN if either is: a row that holds a NaN must not come out as numbers.
+__device__ __forceinline__ float top2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 template <typename TX>
 __device__ __forceinline__ float piece_max(const Piece8<TX>& p) {
     float m = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(p.at(i)));
+    for (int i = 0; i < 8; ++i) m = top2(m, fabsf(p.at(i)));
     return m;
 }
 
@@ -39,7 +43,7 @@ __device__ __forceinline__ float piece_max(const Piece8<TX>& p) {
 struct Divisor { float a, up, by; };
 __device__ __forceinline__ Divisor divisor(float a) {
     const float up = a < 0x1p-100f ? 0x1p64f : 1.f;
-    return {a, up, 127.f / (a * up)};   // a = 0: infinity, and quantize8 writes zeros
+    return {a, up, 127.f / (a * up)};   // a = 0, infinity or NaN: quantize8 writes zeros
 }
 
 // Bits whose low byte is the whole number next to t, |t| < 128: 1.5 * 2^23 has steps of 1.
@@ -70,7 +74,7 @@ __device__ __forceinline__ uint2 quantize8(const Piece8<TX>& p, const Divisor& d
     for (int h = 0; h < 2; ++h)   // the low bytes of four
         w[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[h * 4 + 3], b[h * 4 + 2], 0x0c0c0400u),
                                      __builtin_amdgcn_perm(b[h * 4 + 1], b[h * 4], 0x0c0c0400u), 0x05040100u);
-    return d.a > 0.f ? make_uint2(w[0], w[1]) : make_uint2(0u, 0u);
+    return d.a > 0.f && d.a < INFINITY ? make_uint2(w[0], w[1]) : make_uint2(0u, 0u);
 }
 
 // A row by G threads (a wavefront, or the 4 of a workgroup).  HELD pieces a thread stay in registers between the two passes; 0: the row
@@ -93,19 +97,19 @@ struct QuantRow {
         if constexpr (HELD > 0) {
 #pragma unroll
             for (int i = 0; i < HELD; ++i)
-                if (i * G + lane < pieces) m = fmaxf(m, piece_max(held[i]));
+                if (i * G + lane < pieces) m = top2(m, piece_max(held[i]));
         } else {
             for (int i = lane; i < pieces; i += G) {
                 held[0].load(x + (size_t)i * 8);
-                m = fmaxf(m, piece_max(held[0]));
+                m = top2(m, piece_max(held[0]));
             }
         }
 #pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+        for (int off = 32; off >= 1; off >>= 1) m = top2(m, __shfl_xor(m, off));
         if constexpr (G == 64) return m;
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
         __syncthreads();
-        return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        return top2(top2(red[0], red[1]), top2(red[2], red[3]));
     }
     // store(i, q) takes the 8 bytes of piece i
     template <typename Store>

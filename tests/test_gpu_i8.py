@@ -93,6 +93,28 @@ def test_quantize_rows_of_zeros_and_of_the_smallest_and_largest(dtype):
     assert q[1, 5] == 127
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [16, 512, 1024, 2048, 4096, 8192, 16384, 20480])
+def test_infinities_and_nan_stay_visible_and_in_their_row(d, dtype):
+    for T in (3, 9, 2100) if d <= 4096 else (3, 9):
+        g = gen(d + T)
+        x = torch.randn((T, d), generator=g, device="cuda").to(dtype)
+        clean = m.quantize_rows(x)
+        x[0, d - 1], x[1, 0], x[1, d // 2] = float("nan"), float("inf"), -float("inf")
+        q, s = m.quantize_rows(x)
+        assert torch.isnan(s[0]) and s[1] == float("inf") and not q[:2].any()
+        assert torch.equal(q[2:], clean[0][2:]) and torch.equal(s[2:], clean[1][2:])
+        idx = torch.zeros((T, 1), device="cuda", dtype=torch.int32)
+        xs, xsc, _, _ = m.sort_tokens(x, idx, 1, quantize=True)
+        assert torch.equal(xs, q) and torch.equal(xsc[1:], s[1:]) and torch.isnan(xsc[0])
+        W, ws = m.quantize_rows(torch.randn((24, d), generator=g, device="cuda"))
+        y = m.base_gemm_i8(x, W, ws)
+        assert torch.isnan(y[:2]).all() and torch.equal(y[2:], m.gemm_i8(q, s, W, ws, dtype=dtype)[2:])
+        assert torch.isfinite(y[2:]).all()
+        one = m.base_gemm_i8(x[:1], W, ws)
+        assert torch.isnan(one).all()
+
+
 # ---- gemm_i8 -----------------------------------------------------------------------------------------------------------------
 def dense_ref(q, qs, W, ws):
     return (q.double() @ W.double().t()) * qs.double()[:, None] * ws.double()
