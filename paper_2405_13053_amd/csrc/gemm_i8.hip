@@ -771,8 +771,9 @@ static hipError_t launch_one_i8(GemmI8Args a, hipStream_t stream) {
 // nk K tiles, rounds of one (or per_cu) tiles per CU, bytes read and written once, 6 TB/s by the wavefront rings and 5.5 by the others.
 // The four times of a tile shape are fitted to 350 dense sizes (1 to 8192 rows, 256 to 14336 inputs and outputs, W not in the caches),
 // within 3 to 11% of them; on these sizes the choice is 1.1% slower on average than the best shape of each.  Groups: how their rows are
-// dealt is known on the device only, so two deals are weighed 7 to 3, an even one and 7/8 of the rows to an eighth of the groups: 1.7%
-// slower than the best on 216 even deals, 6.7% on as many that fall off as 1 / j^2 (2.1 and 11.9% by the even deal alone).
+// dealt is known on the device only, so two deals are weighed alike, a random one of equal chances (the mean and 1.22 standard deviations,
+// of a Poisson law, to either side of it) and one that falls off as 1 / j^2: on 999 random deals of chances 1, 1 / j and 1 / j^2 2.7% slower
+// than the best shape of each (an exactly even deal and one of 7/8 of the rows to 1/8 of the groups, 7 to 3: 4.7%).
 struct I8Shape {
     int rows, cols, per_cu;
     bool wave;              // gemm_i8_wave_kernel
@@ -811,23 +812,44 @@ static float shape_us(const GemmI8Args& a, const I8Shape& s, float row_tiles, in
     return cbrtf(own * own * own + mem * mem * mem);
 }
 
+// Rows of the groups of one deal, as far as tiles of 16 rows or more tell them apart
+struct Deal {
+    float groups = 0.f, weight = 1.f;   // with rows; each value below stands for `weight` groups
+    float small = 0.f;                  // of them with up to 16 rows
+    int n = 0, rows[kMaxAdapters];
+    void add(int r) {
+        if (r <= 0) return;
+        groups += weight;
+        if (r <= 16) small += weight;
+        else rows[n++] = r;
+    }
+    float tiles(int tile_rows) const {
+        int t = 0;
+        for (int i = 0; i < n; ++i) t += ceil_div(rows[i], tile_rows);
+        return small + weight * (float)t;
+    }
+};
+
 static int choose_shape(const GemmI8Args& a) {
-    const int N = a.T < a.N ? a.T : a.N, many = N / 8 > 1 ? N / 8 : 1, in_many = (int)((int64_t)a.T * 7 / 8), in_few = a.T - in_many;
-    const int few = N - many < in_few ? N - many : in_few;
+    const bool grouped = a.offsets != nullptr && a.N > 1;
+    Deal even, falling;
+    if (grouped) {
+        const int N = a.T < a.N ? a.T : a.N;
+        const float mean = (float)a.T / (float)N, spread = 1.22f * sqrtf(mean);
+        even.weight = (float)N / 3.f;
+        for (int i = -1; i <= 1; ++i) even.add((int)(mean + (float)i * spread + 0.5f));
+        float sum = 0.f;
+        for (int j = 1; j <= N; ++j) sum += 1.f / (float)(j * j);
+        for (int j = 1; j <= N; ++j) falling.add((int)((float)a.T / (sum * (float)(j * j)) + 0.5f));
+    }
     int best = 0;
     float least = 0.f;
     for (int i = 0; i < kI8ShapeCount; ++i) {
         const I8Shape& s = kI8Shapes[i];
         const int cols = s.wave ? wave_tile_cols(most_row_tiles(a, s.rows), a.d_out, s.cols) : s.cols;
-        float us;
-        if (a.offsets == nullptr || a.N == 1) {
-            us = shape_us(a, s, (float)ceil_div(a.T, s.rows), cols, 1.f);
-        } else {
-            const float even = (float)N * (float)ceil_div(ceil_div(a.T, N), s.rows);
-            const float skewed = (float)many * (float)ceil_div(ceil_div(in_many, many), s.rows) +
-                                 (few > 0 ? (float)few * (float)ceil_div(ceil_div(in_few, few), s.rows) : 0.f);
-            us = 0.7f * shape_us(a, s, even, cols, (float)N) + 0.3f * shape_us(a, s, skewed, cols, (float)(many + few));
-        }
+        const float us = !grouped ? shape_us(a, s, (float)ceil_div(a.T, s.rows), cols, 1.f)
+                                  : shape_us(a, s, even.tiles(s.rows), cols, even.groups) +
+                                        shape_us(a, s, falling.tiles(s.rows), cols, falling.groups);
         if (i == 0 || us < least) { least = us; best = i; }
     }
     return best;
