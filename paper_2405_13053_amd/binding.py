@@ -583,7 +583,7 @@ def sort_tokens(x, topk_idx, N: int, quantize: bool = False, out: Optional[torch
         _chk(x, "x"); _chk(topk_idx, "topk_idx", torch.int32, (T, k)); _chk(out, "out", dtype, (T * k, d))
     _chk(ws, "ws", torch.uint8)
     scale = torch.empty((T * k,), dtype=torch.float32, device=dev) if quantize else None
-    pos, offsets = topk_idx.new_empty((T, k)), topk_idx.new_empty((N + 1,))
+    pos, offsets = torch.empty_like(topk_idx), topk_idx.new_empty((N + 1,))
     ws = _ws(ws, lambda: sort_workspace_bytes(T, k, N), dev)
     _chk_device(x, topk_idx, out, ws)
     st = load_library().meteora_sort_tokens(_p(x), _p(topk_idx), T, k, N, d, _dt(x), _p(out), _p(scale), _p(pos), _p(offsets),
@@ -631,7 +631,9 @@ def unsort_backward(dy, ys, pos, w=None, scale: float = 1.0, out: Optional[torch
         _chk(dy, "dy", dtype, (T, d)); _chk(ys, "ys"); _chk(pos, "pos", torch.int32, (T, k)); _chk(w, "w", torch.float32, (T, k))
         _chk(out, "out", dtype, (rows, d))
     _chk_device(dy, ys, pos, w, out)
-    dw = torch.empty((T, k), dtype=torch.float32, device=dy.device) if want_dw else None
+    dw = None
+    if want_dw:
+        dw = torch.empty((T, k), dtype=torch.float32, device=dy.device) if w is None else torch.empty_like(w)
     st = load_library().meteora_unsort_backward(_p(dy), _p(ys), rows, _p(pos), _p(w), T, k, d, float(scale), _dt(ys), _p(out),
                                                 _p(dw), _stream())
     if st != 0:
