@@ -34,11 +34,15 @@ struct GemmI8Args {
     int tiles_m, tiles_n;   // row tiles of the grid (at least as many as there are), column tiles
     int tile_cols;          // columns of a tile (wave kernel)
     int tail;               // 1: the tiles of a last, half-empty round are left to gemm_i8_ring_kernel's TAIL form
+    int past_caches;        // 1: W is more than the caches keep from one call to the next
 };
 
 // The row tiles of all groups, each cut into tiles of BM rows, one group behind the other.  Whatever the offsets hold, the rows lie in
 // [0, T).  A lane holds a group; uniform results.
-struct RowTile { int e, row0, rows; };
+struct RowTile {
+    int e, row0, rows;
+    bool alone;   // its group has no other
+};
 
 template <int BM>
 struct RowTiles {
@@ -63,11 +67,12 @@ struct RowTiles {
         count = min(__builtin_amdgcn_readfirstlane(__shfl(end, 63)), a.tiles_m);
     }
     __device__ __forceinline__ RowTile at(const GemmI8Args& a, int tile) const {   // tile < count
-        if (a.offsets == nullptr) return {0, tile * BM, min(BM, a.T - tile * BM)};
+        if (a.offsets == nullptr) return {0, tile * BM, min(BM, a.T - tile * BM), count == 1};
         const int e = __ffsll(__ballot(end > tile)) - 1;
         const int first = __shfl(lo, e) + (tile - (__shfl(end, e) - __shfl(mine, e))) * BM;
         const int rows = min(BM, __shfl(hi, e) - first);
-        return {__builtin_amdgcn_readfirstlane(e), __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(rows)};
+        return {__builtin_amdgcn_readfirstlane(e), __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(rows),
+                __builtin_amdgcn_readfirstlane(__shfl(mine, e)) == 1};
     }
 };
 // The grid's row tiles: as many as T rows in N groups can make.  Workgroups past those that there are end at once.
@@ -449,40 +454,21 @@ __host__ __device__ constexpr int tail_start(int tiles) {
     return tiles > 256 && tiles % 256 <= kTailTiles ? tiles - tiles % 256 : tiles;
 }
 
-// PART: d_in may end in a partial K tile.  TAIL: this workgroup's tile is a part of one of 256 x 256 behind tail_start (the number of
-// tiles of groups is known here only).
-template <typename TO, int MB, int NB, int D, bool PART, bool TAIL = false>
-__global__ __launch_bounds__(256) void gemm_i8_ring_kernel(const GemmI8Args a) {
+// One tile.  PART: d_in may end in a partial K tile.  ONCE: no other workgroup reads these rows of W.
+template <typename TO, int MB, int NB, int D, bool PART, bool ONCE>
+__device__ __forceinline__ void ring_i8_tile(const GemmI8Args& a, unsigned char* smem, int e, int row0, int rows, int n0) {
     constexpr int BM = MB * 32, BN = NB * 32, PX = MB, PW = NB;   // 2 x 2 wavefronts; load instructions per wavefront and tile
     static_assert((NB % 2 == 0 || MB % 2 == 0) && D >= 2 && D <= 5 && (D - 1) * (PX + PW) < 64, "2 x 2 micro-blocks; vmcnt");
     constexpr int NR = MB + NB, NM = MB * NB;   // fragment reads and MFMAs per k-step of 64
     constexpr int RA = NM * 3 / 4 / NR > 0 ? NM * 3 / 4 / NR : 1, RB = NM / NR;   // MFMAs per read, see the bf16 kernel
     static_assert(RB >= 1, "a k-step needs one MFMA per fragment read");
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     bf16_t* ring = reinterpret_cast<bf16_t*>(smem);
     constexpr int kXElems = BM * kGemmBK, kWElems = BN * kGemmBK;   // in units of two bytes, as everything that is shared
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
-    const int l15 = lane & 15, kq = lane >> 4;
-    constexpr int PM = TAIL ? 256 / BM : 1, PN = TAIL ? 256 / BN : 1;   // tiles are dealt as PM x PN of them
-    const RowTiles<BM * PM> row_tiles(a, lane);
-    const int tiles = row_tiles.count * a.tiles_n;
-    const int id = TAIL ? tail_start(tiles) + (int)blockIdx.x / (PM * PN) : (int)blockIdx.x;
-    if (id >= (!TAIL && a.tail ? tail_start(tiles) : tiles)) return;
-    int tile_m, tile_n;
-    tile_of_workgroup(id, row_tiles.count, a.tiles_n, tile_m, tile_n);
-    RowTile rt = row_tiles.at(a, tile_m);
-    int n0 = tile_n * BN * PN;
-    if constexpr (TAIL) {
-        const int m0 = (int)blockIdx.x % PM * BM;
-        rt.row0 += m0;
-        rt.rows = min(BM, rt.rows - m0);
-        n0 += (int)blockIdx.x / PM % PN * BN;
-        if (rt.rows <= 0 || n0 >= a.d_out) return;
-    }
-    const int rows = rt.rows, e = rt.e, row0 = rt.row0, cols = min(BN, a.d_out - n0);
+    const int l15 = lane & 15, kq = lane >> 4, cols = min(BN, a.d_out - n0);
 
     const int nk_main = a.d_in / kI8Tile, nk = nk_main + (PART && a.d_in % kI8Tile != 0 ? 1 : 0);
     const int8_t* xb = a.q + (size_t)row0 * a.d_in;
@@ -500,7 +486,7 @@ __global__ __launch_bounds__(256) void gemm_i8_ring_kernel(const GemmI8Args a) {
     };
     auto request_w = [&](bf16_t* slot, int kt, int i, auto is_part) {
         if constexpr (decltype(is_part)::value) dma_piece_behind<true, false>(slot, ow, w_bytes, ow, part, -1, i, wave);
-        else dma_piece(slot, ow, kt, i, wave);
+        else dma_piece<ONCE ? kReadOnceI8 : 0>(slot, ow, kt, i, wave);
     };
     auto request_tile = [&](int it, auto is_part) {
 #pragma unroll
@@ -630,6 +616,39 @@ __global__ __launch_bounds__(256) void gemm_i8_ring_kernel(const GemmI8Args a) {
         for (int ni = 0; ni < NB; ++ni) asm volatile("" : "+a"(acc[mi][ni]));   // values from here on, not before
     __builtin_amdgcn_sched_barrier(0);
     ring_i8_epilogue<TO, MB, NB>(a, acc, smem, e, row0, rows, n0, wm, wn, wave, lane);
+}
+
+// TAIL: this workgroup's tile is a part of one of 256 x 256 behind tail_start (the number of tiles of groups is known here only).
+// W of a group with one row tile is read once, and where it comes from memory it is requested as such: 8 groups of 4096 -> 4096, 16 and 64 rows
+// each, 128 x 128 tiles 32.9 and 33.5 us against 35.7 and 35.6.  Where other row tiles read it again that policy costs 5 to 30%, and where it
+// is still in a cache too (28 groups of 4096 -> 64, 7 MB: 12.8 against 11.0).  So the workgroup chooses between two copies of the loop;
+// 256 x 256 tiles, which few rows do not come to, have one.
+template <typename TO, int MB, int NB, int D, bool PART, bool TAIL = false>
+__global__ __launch_bounds__(256) void gemm_i8_ring_kernel(const GemmI8Args a) {
+    constexpr int BM = MB * 32, BN = NB * 32;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    constexpr int PM = TAIL ? 256 / BM : 1, PN = TAIL ? 256 / BN : 1;   // tiles are dealt as PM x PN of them
+    const RowTiles<BM * PM> row_tiles(a, (int)threadIdx.x & 63);
+    const int tiles = row_tiles.count * a.tiles_n;
+    const int id = TAIL ? tail_start(tiles) + (int)blockIdx.x / (PM * PN) : (int)blockIdx.x;
+    if (id >= (!TAIL && a.tail ? tail_start(tiles) : tiles)) return;
+    int tile_m, tile_n;
+    tile_of_workgroup(id, row_tiles.count, a.tiles_n, tile_m, tile_n);
+    RowTile rt = row_tiles.at(a, tile_m);
+    int n0 = tile_n * BN * PN;
+    if constexpr (TAIL) {
+        const int m0 = (int)blockIdx.x % PM * BM;
+        rt.row0 += m0;
+        rt.rows = min(BM, rt.rows - m0);
+        n0 += (int)blockIdx.x / PM % PN * BN;
+        if (rt.rows <= 0 || n0 >= a.d_out) return;
+    }
+    if constexpr (!TAIL && MB * NB < 64)
+        if (rt.alone && a.past_caches) {
+            ring_i8_tile<TO, MB, NB, D, PART, true>(a, smem, rt.e, rt.row0, rt.rows, n0);
+            return;
+        }
+    ring_i8_tile<TO, MB, NB, D, PART, false>(a, smem, rt.e, rt.row0, rt.rows, n0);
 }
 
 // Up to 128 inputs (the expand of adapters): one K tile, and the output is what there is to move.  The same tiles without a ring, so
@@ -768,31 +787,31 @@ static hipError_t launch_one_i8(GemmI8Args a, hipStream_t stream) {
 
 // ---- which kernel and tile: the one that takes the least by
 //     us^3 = (launch + rounds * (round + nk * step) + tiles / 256 * nk * share)^3 + (bytes / rate)^3
-// nk K tiles, rounds of one (or per_cu) tiles per CU, bytes read and written once, 6 TB/s by the wavefront rings and 5.5 by the others.
-// The four times of a tile shape are fitted to 350 dense sizes (1 to 8192 rows, 256 to 14336 inputs and outputs, W not in the caches),
-// within 3 to 11% of them; on these sizes the choice is 1.1% slower on average than the best shape of each.  Groups: how their rows are
-// dealt is known on the device only, so two deals are weighed alike, a random one of equal chances (the mean and 1.22 standard deviations,
-// of a Poisson law, to either side of it) and one that falls off as 1 / j^2: on 999 random deals of chances 1, 1 / j and 1 / j^2 2.7% slower
-// than the best shape of each (an exactly even deal and one of 7/8 of the rows to 1/8 of the groups, 7 to 3: 4.7%).
+// nk K tiles, rounds of one (or per_cu) tiles per CU, bytes read and written once, 5.1 TB/s by the wavefront rings and 4.9 by the others.
+// The four times of a tile shape are fitted to 350 dense sizes (1 to 8192 rows, 256 to 14336 inputs and outputs) and 999 of groups (2 to 64 of
+// them, random deals of chances 1, 1 / j and 1 / j^2), W not in the caches: on the dense ones the choice is 0.6% slower on average than the
+// best shape of each, on the groups with their deals known 1.1%.  How rows are dealt is known on the device only, so two deals are weighed
+// alike, a random one of equal chances (the mean and 1.22 standard deviations, of a Poisson law, to either side) and one that falls off as
+// 1 / j^2: 2.6% slower than the best shape of each (an exactly even deal in place of the random one 3.1%).
 struct I8Shape {
     int rows, cols, per_cu;
     bool wave;              // gemm_i8_wave_kernel
     float launch, round, step, share;
 };
 constexpr I8Shape kI8Shapes[] = {
-    {16, 16, 1, true, 3.12f, 0.85f, 0.054f, 0.000f},
-    {16, 32, 1, true, 2.08f, 1.87f, 0.099f, 0.000f},
-    {16, 64, 1, true, 1.65f, 2.19f, 0.126f, 0.031f},
-    {32, 32, 1, true, 2.44f, 1.78f, 0.116f, 0.019f},
-    {64, 64, 1, false, 2.17f, 1.86f, 0.153f, 0.075f},
-    {96, 64, 1, false, 2.00f, 2.14f, 0.181f, 0.092f},
-    {128, 64, 1, false, 1.98f, 2.24f, 0.211f, 0.122f},
-    {128, 128, 1, false, 1.98f, 2.67f, 0.337f, 0.171f},
-    {128, 128, 2, false, 1.74f, 2.53f, 0.357f, 0.294f},
-    {192, 128, 1, false, 2.02f, 3.56f, 0.438f, 0.197f},
-    {224, 128, 1, false, 2.08f, 3.92f, 0.487f, 0.207f},
-    {256, 128, 1, false, 1.98f, 4.42f, 0.548f, 0.234f},
-    {256, 256, 1, false, 1.66f, 7.04f, 0.932f, 0.347f},
+    {16, 16, 1, true, 2.92f, 1.00f, 0.039f, 0.017f},
+    {16, 32, 1, true, 1.31f, 2.84f, 0.036f, 0.060f},
+    {16, 64, 1, true, 0.41f, 3.85f, 0.088f, 0.052f},
+    {32, 32, 1, true, 1.80f, 2.49f, 0.049f, 0.077f},
+    {64, 64, 1, false, 1.00f, 3.07f, 0.145f, 0.110f},
+    {96, 64, 1, false, 1.07f, 3.08f, 0.185f, 0.108f},
+    {128, 64, 1, false, 1.07f, 3.12f, 0.229f, 0.102f},
+    {128, 128, 1, false, 1.36f, 3.50f, 0.357f, 0.182f},
+    {128, 128, 2, false, 1.76f, 2.98f, 0.293f, 0.394f},
+    {192, 128, 1, false, 1.71f, 4.09f, 0.486f, 0.173f},
+    {224, 128, 1, false, 1.76f, 4.53f, 0.546f, 0.155f},
+    {256, 128, 1, false, 1.68f, 5.00f, 0.619f, 0.147f},
+    {256, 256, 1, false, 1.21f, 8.19f, 0.665f, 0.665f},
 };
 static_assert(kI8Shapes[4].rows * kI8Shapes[4].cols == 64 * 64 && kI8Shapes[6].rows * kI8Shapes[6].cols == 128 * 64 &&
               kI8Shapes[8].per_cu == 2, "tail_shape");
@@ -808,7 +827,7 @@ static float shape_us(const GemmI8Args& a, const I8Shape& s, float row_tiles, in
         tail = q.launch + q.round + nk * q.step + rest * (float)(256 * 256 / (q.rows * q.cols)) / 256.f * nk * q.share;
     }
     const float own = s.launch + rounds * (s.round + nk * s.step) + (tail > 0.f ? rounds : tiles / 256.f) * nk * s.share + tail;
-    const float mem = (groups * (float)a.d_out * (float)a.d_in + (float)a.T * ((float)a.d_in + 2.f * (float)a.d_out)) / (s.wave ? 6e6f : 5.5e6f);
+    const float mem = (groups * (float)a.d_out * (float)a.d_in + (float)a.T * ((float)a.d_in + 2.f * (float)a.d_out)) / (s.wave ? 5.1e6f : 4.9e6f);
     return cbrtf(own * own * own + mem * mem * mem);
 }
 
@@ -903,13 +922,16 @@ static hipError_t launch_base(const GemmI8Args& a, const TX* x, hipStream_t stre
 }
 hipError_t launch_base_gemm_i8_in_one(const void* x, const int8_t* W, const float* w_scale, int T, int d_in, int d_out, bool bf16,
                                       void* out, hipStream_t stream) {
-    const GemmI8Args a{nullptr, nullptr, W, w_scale, nullptr, out, T, d_in, d_out, 1, 1, 0, 0, 0};
+    const GemmI8Args a{nullptr, nullptr, W, w_scale, nullptr, out, T, d_in, d_out, 1, 1, 0, 0, 0, 0};
     return bf16 ? launch_base(a, (const bf16_t*)x, stream) : launch_base(a, (const float*)x, stream);
 }
 
 hipError_t launch_gemm_i8(const int8_t* q, const float* q_scale, const int8_t* W, const float* w_scale, const int32_t* offsets,
                           int T, int d_in, int d_out, int N, bool bf16, void* out, hipStream_t stream) {
-    const GemmI8Args a{q, q_scale, W, w_scale, offsets, out, T, d_in, d_out, N, 0, 0, 0, 0};
+    // The last cache holds 256 MB: from three such matrices in turn on none is still there.  Three in turn, 128 x 128 tiles, requested as kept and
+    // as read once, us: 67 MB 14.3 and 15.9, 84 MB 19.5 and 22.0, 101 MB 23.9 and 24.0, 117 MB 26.9 and 25.1, 134 MB 29.0 and 25.4.
+    const int past_caches = (int64_t)N * d_out * d_in >= 100000000;
+    const GemmI8Args a{q, q_scale, W, w_scale, offsets, out, T, d_in, d_out, N, 0, 0, 0, 0, past_caches};
     return bf16 ? launch_i8<bf16_t>(a, stream) : launch_i8<float>(a, stream);
 }
 

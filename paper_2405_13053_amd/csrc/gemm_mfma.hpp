@@ -317,10 +317,11 @@ __device__ __forceinline__ DmaOperand dma_operand(const bf16_t* base, int nrows,
     return o;
 }
 
+template <int POLICY = 0>   // of the caches
 __device__ __forceinline__ void dma_piece(bf16_t* lds_tile, const DmaOperand& o, int ktile, int j, int wave) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
         o.rsrc, (__attribute__((address_space(3))) void*)(lds_tile + (j * 4 + wave) * 8 * kGemmBK), 16, o.voff,
-        (int)(o.piece_step * (uint32_t)j + (uint32_t)ktile * (kGemmBK * 2)), 0, 0);
+        (int)(o.piece_step * (uint32_t)j + (uint32_t)ktile * (kGemmBK * 2)), 0, POLICY);
 }
 
 // The K tiles behind the whole ones: first, where d_in is no multiple of 64, the rest of the main operands' columns (kt < 0),
