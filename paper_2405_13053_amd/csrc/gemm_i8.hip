@@ -33,7 +33,7 @@ struct GemmI8Args {
     int T, d_in, d_out, N;
     int tiles_m, tiles_n;   // row tiles of the grid (at least as many as there are), column tiles
     int tile_cols;          // columns of a tile (wave kernel)
-    int tail;               // 1: the tiles of a last, half-empty round are left to gemm_i8_ring_kernel's TAIL form
+    int tail;               // 1: the tiles of a last, half-empty round are left to gemm_i8_tail_kernel
     int past_caches;        // 1: W is more than the caches keep from one call to the next
 };
 
@@ -618,37 +618,57 @@ __device__ __forceinline__ void ring_i8_tile(const GemmI8Args& a, unsigned char*
     ring_i8_epilogue<TO, MB, NB>(a, acc, smem, e, row0, rows, n0, wm, wn, wave, lane);
 }
 
-// TAIL: this workgroup's tile is a part of one of 256 x 256 behind tail_start (the number of tiles of groups is known here only).
 // W of a group with one row tile is read once, and where it comes from memory it is requested as such: 8 groups of 4096 -> 4096, 16 and 64 rows
 // each, 128 x 128 tiles 32.9 and 33.5 us against 35.7 and 35.6.  Where other row tiles read it again that policy costs 5 to 30%, and where it
 // is still in a cache too (28 groups of 4096 -> 64, 7 MB: 12.8 against 11.0).  So the workgroup chooses between two copies of the loop;
 // 256 x 256 tiles, which few rows do not come to, have one.
-template <typename TO, int MB, int NB, int D, bool PART, bool TAIL = false>
+template <typename TO, int MB, int NB, int D, bool PART>
 __global__ __launch_bounds__(256) void gemm_i8_ring_kernel(const GemmI8Args a) {
     constexpr int BM = MB * 32, BN = NB * 32;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    constexpr int PM = TAIL ? 256 / BM : 1, PN = TAIL ? 256 / BN : 1;   // tiles are dealt as PM x PN of them
-    const RowTiles<BM * PM> row_tiles(a, (int)threadIdx.x & 63);
+    const RowTiles<BM> row_tiles(a, (int)threadIdx.x & 63);
     const int tiles = row_tiles.count * a.tiles_n;
-    const int id = TAIL ? tail_start(tiles) + (int)blockIdx.x / (PM * PN) : (int)blockIdx.x;
-    if (id >= (!TAIL && a.tail ? tail_start(tiles) : tiles)) return;
+    if ((int)blockIdx.x >= (a.tail ? tail_start(tiles) : tiles)) return;
     int tile_m, tile_n;
-    tile_of_workgroup(id, row_tiles.count, a.tiles_n, tile_m, tile_n);
-    RowTile rt = row_tiles.at(a, tile_m);
-    int n0 = tile_n * BN * PN;
-    if constexpr (TAIL) {
-        const int m0 = (int)blockIdx.x % PM * BM;
-        rt.row0 += m0;
-        rt.rows = min(BM, rt.rows - m0);
-        n0 += (int)blockIdx.x / PM % PN * BN;
-        if (rt.rows <= 0 || n0 >= a.d_out) return;
-    }
-    if constexpr (!TAIL && MB * NB < 64)
+    tile_of_workgroup(blockIdx.x, row_tiles.count, a.tiles_n, tile_m, tile_n);
+    const RowTile rt = row_tiles.at(a, tile_m);
+    if constexpr (MB * NB < 64)
         if (rt.alone && a.past_caches) {
-            ring_i8_tile<TO, MB, NB, D, PART, true>(a, smem, rt.e, rt.row0, rt.rows, n0);
+            ring_i8_tile<TO, MB, NB, D, PART, true>(a, smem, rt.e, rt.row0, rt.rows, tile_n * BN);
             return;
         }
-    ring_i8_tile<TO, MB, NB, D, PART, false>(a, smem, rt.e, rt.row0, rt.rows, n0);
+    ring_i8_tile<TO, MB, NB, D, PART, false>(a, smem, rt.e, rt.row0, rt.rows, tile_n * BN);
+}
+
+// The 256 x 256 tiles behind tail_start, in smaller ones: as small as one to a CU allows, or two of the largest.  The number of tiles of
+// groups is known here only, and so is their size.
+template <typename TO, int MB, int NB, int D, bool PART>
+__device__ __forceinline__ void tail_i8_part(const GemmI8Args& a, const RowTiles<256>& row_tiles, unsigned char* smem, int first, int tiles) {
+    constexpr int BM = MB * 32, BN = NB * 32, PM = 256 / BM, PN = 256 / BN;
+    const int id = first + (int)blockIdx.x / (PM * PN), m0 = (int)blockIdx.x % PM * BM;
+    if (id >= tiles) return;
+    int tile_m, tile_n;
+    tile_of_workgroup(id, row_tiles.count, a.tiles_n, tile_m, tile_n);
+    const RowTile rt = row_tiles.at(a, tile_m);
+    const int rows = min(BM, rt.rows - m0), n0 = tile_n * 256 + (int)blockIdx.x / PM % PN * BN;
+    if (rows <= 0 || n0 >= a.d_out) return;
+    ring_i8_tile<TO, MB, NB, D, PART, false>(a, smem, rt.e, rt.row0 + m0, rows, n0);
+}
+constexpr int kTailSmall = 16, kTailMiddle = 32;   // tiles of 256 x 256 that are 256 of 64 x 64, and of 128 x 64
+constexpr int tail_i8_lds() {   // two workgroups to a CU
+    const int a = ring_i8_lds<2, 2, 4>(), b = ring_i8_lds<4, 2, 3>(), c = ring_i8_lds<4, 4, 2>();
+    return a > b ? (a > c ? a : c) : (b > c ? b : c);
+}
+static_assert(2 * tail_i8_lds() <= 160 * 1024, "LDS");
+
+template <typename TO, bool PART>
+__global__ __launch_bounds__(256) void gemm_i8_tail_kernel(const GemmI8Args a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const RowTiles<256> row_tiles(a, (int)threadIdx.x & 63);
+    const int tiles = row_tiles.count * a.tiles_n, first = tail_start(tiles);
+    if (tiles - first <= kTailSmall) tail_i8_part<TO, 2, 2, 4, PART>(a, row_tiles, smem, first, tiles);
+    else if (tiles - first <= kTailMiddle) tail_i8_part<TO, 4, 2, 3, PART>(a, row_tiles, smem, first, tiles);
+    else tail_i8_part<TO, 4, 4, 2, PART>(a, row_tiles, smem, first, tiles);
 }
 
 // Up to 128 inputs (the expand of adapters): one K tile, and the output is what there is to move.  The same tiles without a ring, so
@@ -737,38 +757,25 @@ static hipError_t launch_ring_i8(GemmI8Args a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// The tail of `rest` tiles of 256 x 256 at most
-template <typename TO, int MB, int NB, int D>
-static hipError_t launch_tail_i8(GemmI8Args a, int rest, hipStream_t stream) {
-    a.tiles_m = most_row_tiles(a, 256);
-    a.tiles_n = ceil_div(a.d_out, 256);
-    constexpr int lds = ring_i8_lds<MB, NB, D>();
-    const auto kern = a.d_in % kI8Tile != 0 ? &gemm_i8_ring_kernel<TO, MB, NB, D, true, true> : &gemm_i8_ring_kernel<TO, MB, NB, D, false, true>;
-    const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(kern), lds);
-    if (e != hipSuccess) return e;
-    kern<<<rest * (64 / (MB * NB)), 256, lds, stream>>>(a);
-    return hipGetLastError();
-}
-
-// Index in kI8Shapes of the tail's tiles: as small as one to a CU allows, two of the largest
-static int tail_shape(int rest) { return rest <= 16 ? 4 : rest <= 32 ? 6 : 8; }
-
 // 256 x 256 tiles, and the tail where there is, or (groups) may be, one.  As the best of the shapes with a round of their own for the rest,
-// and so, us: 4300, 5000, 6000 and 9000 x 4096 -> 4096 69.4, 77.7, 89.0, 141 and 69.2, 74.4, 83.8, 122; 5000 x 4096 -> 14336 247 and 235; 8
-// groups of 4096 -> 4096, 4002 and 8192 rows that fall off as 1 / j^2 92.5, 141 and 80.7, 123, dealt evenly (whole rounds: the second launch
-// finds nothing) 53.4, 102 and 55.1, 105.
+// and so, us: 4300, 5000 and 9000 x 4096 -> 4096 69.4, 77.7, 141 and 69.3, 74.7, 123; 5000 x 4096 -> 14336 247 and 228; 8 groups of 4096 ->
+// 4096, 4002 and 8192 rows that fall off as 1 / j^2 92.5, 141 and 81.4, 124, dealt evenly (whole rounds: the second launch finds nothing)
+// 53.4, 102 and 55.6, 103.  The size of the tail's tiles, 16 tiles of 8 groups of 4096 -> 4096 behind 256: 128 x 128 76.3, 64 x 64 68.3.
 template <typename TO>
 static hipError_t launch_largest_i8(GemmI8Args a, hipStream_t stream) {
     const int64_t tiles = (int64_t)most_row_tiles(a, 256) * ceil_div(a.d_out, 256);
     a.tail = tiles > 256 && (a.offsets != nullptr || tail_start((int)tiles) != tiles) ? 1 : 0;
     const hipError_t e = launch_ring_i8<TO, 8, 8, 2>(a, stream);
     if (e != hipSuccess || a.tail == 0) return e;
-    const int rest = a.offsets != nullptr ? kTailTiles : (int)tiles - tail_start((int)tiles);
-    switch (tail_shape(rest)) {
-        case 4: return launch_tail_i8<TO, 2, 2, 5>(a, rest, stream);
-        case 6: return launch_tail_i8<TO, 4, 2, 4>(a, rest, stream);
-        default: return launch_tail_i8<TO, 4, 4, 2>(a, rest, stream);
-    }
+    a.tiles_m = most_row_tiles(a, 256);
+    a.tiles_n = ceil_div(a.d_out, 256);
+    const auto kern = a.d_in % kI8Tile != 0 ? &gemm_i8_tail_kernel<TO, true> : &gemm_i8_tail_kernel<TO, false>;
+    const hipError_t f = ensure_lds_limit(reinterpret_cast<const void*>(kern), tail_i8_lds());
+    if (f != hipSuccess) return f;
+    const int rest = (int)tiles - tail_start((int)tiles);
+    const int wgs = a.offsets != nullptr ? kTailTiles * 4 : rest <= kTailSmall ? rest * 16 : rest <= kTailMiddle ? rest * 8 : rest * 4;
+    kern<<<wgs, 256, tail_i8_lds(), stream>>>(a);
+    return hipGetLastError();
 }
 
 template <typename TO, int MB, int NB>
@@ -814,7 +821,7 @@ constexpr I8Shape kI8Shapes[] = {
     {256, 256, 1, false, 1.21f, 8.19f, 0.665f, 0.665f},
 };
 static_assert(kI8Shapes[4].rows * kI8Shapes[4].cols == 64 * 64 && kI8Shapes[6].rows * kI8Shapes[6].cols == 128 * 64 &&
-              kI8Shapes[8].per_cu == 2, "tail_shape");
+              kI8Shapes[8].per_cu == 2, "of the tail");
 constexpr int kI8ShapeCount = sizeof(kI8Shapes) / sizeof(kI8Shapes[0]);
 
 static float shape_us(const GemmI8Args& a, const I8Shape& s, float row_tiles, int cols, float groups) {   // groups: with rows
@@ -822,7 +829,7 @@ static float shape_us(const GemmI8Args& a, const I8Shape& s, float row_tiles, in
     float rounds = ceilf(tiles / (float)(256 * s.per_cu)), tail = 0.f;
     const float rest = tiles - 256.f * (rounds - 1.f);
     if (s.rows * s.cols == 256 * 256 && rounds > 1.f && rest <= (float)kTailTiles) {
-        const I8Shape& q = kI8Shapes[tail_shape(a.offsets != nullptr ? kTailTiles : (int)rest)];
+        const I8Shape& q = kI8Shapes[rest <= (float)kTailSmall ? 4 : rest <= (float)kTailMiddle ? 6 : 8];   // much the same rings
         rounds -= 1.f;
         tail = q.launch + q.round + nk * q.step + rest * (float)(256 * 256 / (q.rows * q.cols)) / 256.f * nk * q.share;
     }
@@ -944,11 +951,10 @@ static hipError_t init_ring() {
     const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_ring_kernel<TO, MB, NB, D, true>), ring_i8_lds<MB, NB, D>());
     return e != hipSuccess ? e : ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_ring_kernel<TO, MB, NB, D, false>), ring_i8_lds<MB, NB, D>());
 }
-template <typename TO, int MB, int NB, int D>
+template <typename TO>
 static hipError_t init_tail() {
-    constexpr int lds = ring_i8_lds<MB, NB, D>();
-    const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_ring_kernel<TO, MB, NB, D, true, true>), lds);
-    return e != hipSuccess ? e : ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_ring_kernel<TO, MB, NB, D, false, true>), lds);
+    const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_tail_kernel<TO, true>), tail_i8_lds());
+    return e != hipSuccess ? e : ensure_lds_limit(reinterpret_cast<const void*>(&gemm_i8_tail_kernel<TO, false>), tail_i8_lds());
 }
 template <typename TX, int RB, int D>
 static hipError_t init_row() {
@@ -966,7 +972,7 @@ static hipError_t init_i8() {   // every kernel that launch_i8 and launch_base m
     for (hipError_t f : {init_wave<TO, 1, 1, 4, 5>(), init_wave<TO, 1, 2, 4, 5>(), init_wave<TO, 1, 4, 4, 3>(), init_wave<TO, 2, 2, 4, 4>(),
                          init_ring<TO, 2, 2, 5>(), init_ring<TO, 3, 2, 5>(), init_ring<TO, 4, 2, 4>(), init_ring<TO, 4, 4, 3>(),
                          init_ring<TO, 4, 4, 2>(), init_ring<TO, 6, 4, 3>(), init_ring<TO, 7, 4, 3>(), init_ring<TO, 8, 4, 3>(),
-                         init_ring<TO, 8, 8, 2>(), init_tail<TO, 2, 2, 5>(), init_tail<TO, 4, 2, 4>(), init_tail<TO, 4, 4, 2>(), init_row<TO, 1, 5>(), init_row<TO, 2, 3>()})
+                         init_ring<TO, 8, 8, 2>(), init_tail<TO>(), init_row<TO, 1, 5>(), init_row<TO, 2, 3>()})
         if (e == hipSuccess) e = f;
     return e;
 }

@@ -1,4 +1,4 @@
-"""Wait states around the matrix instructions that gemm_i8_ring_kernel has in assembly (see test_mfma_waits_host, whose walk through
+"""Wait states around the matrix instructions that gemm_i8_ring_kernel and gemm_i8_tail_kernel have in assembly (see test_mfma_waits_host, whose walk through
 the compiled code this is): v_mfma_i32_16x16x64_i8 reads and writes its registers as v_mfma_f32_16x16x32_bf16 does."""
 import os
 import re
@@ -19,7 +19,7 @@ def test_every_int8_ring_kernel_keeps_the_wait_states(tmp_path):
     subprocess.run(["hipcc", *flags, "--cuda-device-only", "-S", "-o", str(asm), src], check=True,
                    stdout=subprocess.DEVNULL, stderr=subprocess.DEVNULL)
     text = asm.read_text()
-    kernels = set(re.findall(r"^(_Z\S*gemm_i8_ring_kernel\S*):", text, re.M))
+    kernels = set(re.findall(r"^(_Z\S*gemm_i8_(?:ring|tail)_kernel\S*):", text, re.M))
     assert len(kernels) >= 30
     text = text.replace("v_mfma_i32_16x16x64_i8", waits.MFMA)
     code = [(fn, op) for fn, op, _ in waits._parse(text)[0] if op == waits.MFMA]
