@@ -219,6 +219,49 @@ def test_groups(T, N, counts, d_in, d_out, dtype):
     assert (out[int(off[-1]):] == 7).all()   # rows of no group
 
 
+@pytest.mark.parametrize("d_in,dtype", [(4096, torch.bfloat16), (4112, torch.float32)])
+@pytest.mark.parametrize("T,counts", [(4002, [1389, 778, 367, 201, 134, 104, 73, 58]), (4002, [1500, 800, 300, 300, 100, 100, 100, 100]),
+                                      (4050, [0, 1500, 513, 513, 513, 300, 257, 257]), (4200, [513] * 8), (4500, [4353, 0, 0, 0, 0, 0, 0, 1])],
+                         ids=lambda v: str(v)[:20])
+def test_tails_of_groups_of_every_size(T, counts, d_in, dtype):
+    """17, 18, 21, 24 and 19 row tiles of 256: 16, 32, 80, 128 and 48 tiles of 256 x 256 behind the first 256."""
+    g = gen(T + d_in)
+    q, qs, W, ws, off = grouped_case(T, 8, d_in, 4096, counts, g)
+    out = torch.full((T, 4096), 7.0, device="cuda", dtype=dtype)
+    m.gemm_i8(q, qs, W, ws, offsets=off.cuda(), out=out)
+    for e in range(8):
+        a, b = int(off[e]), int(off[e + 1])
+        close(out[a:b], dense_ref(q[a:b], qs[a:b], W[e], ws[e]))
+    assert (out[int(off[-1]):] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,d_in,d_out,most", [(8, 4096, 4096, 24), (8, 4096, 4096, 60), (8, 4096, 4096, 120), (8, 4096, 4096, 190),
+                                               (26, 1040, 4000, 64), (26, 1040, 4000, 130), (3, 6160, 5704, 100)])
+def test_groups_whose_weights_are_past_the_caches(N, d_in, d_out, most, dtype):
+    """Groups of one row tile, of several and of none beside each other; 134, 108 and 105 MB of weights."""
+    g = gen(N + d_in + most)
+    counts = [most - (e * 7) % most if e % 5 else (most * 2 + 3 if e % 2 else 0) for e in range(N)]
+    T = sum(counts) + 3
+    q, qs, W, ws, off = grouped_case(T, N, d_in, d_out, counts, g)
+    out = torch.full((T, d_out), 7.0, device="cuda", dtype=dtype)
+    m.gemm_i8(q, qs, W, ws, offsets=off.cuda(), out=out)
+    for e in range(N):
+        a, b = int(off[e]), int(off[e + 1])
+        close(out[a:b], dense_ref(q[a:b], qs[a:b], W[e], ws[e]))
+    assert (out[int(off[-1]):] == 7).all()
+
+
+@pytest.mark.parametrize("T", [1, 20, 64, 90, 128, 200, 300])
+def test_a_matrix_past_the_caches(T):
+    g = gen(T)
+    q, W = int8((T, 8208), g, -128), int8((12808, 8208), g, -128)
+    qs, ws = scales((T,), g), scales((12808,), g)
+    ref = dense_ref(q, qs, W, ws)
+    for dtype in TYPES:
+        close(m.gemm_i8(q, qs, W, ws, dtype=dtype), ref)
+
+
 def test_offsets_outside_the_rows_write_nothing_outside():
     g = gen(3)
     q, qs, W, ws, _ = grouped_case(100, 4, 64, 64, [25] * 4, g)
