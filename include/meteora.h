@@ -386,7 +386,8 @@ meteora_status meteora_base_gemm_i8(const void* x /*[T,d_in]*/, const int8_t* W 
  * Rows next to each other by adapter (the X_i of Sec. 3.3 as rows that are moved; meteora_bucket_tokens lists them):
  *   pos[t,j]   the place of pair (t, j) among all pairs whose topk_idx lies in [0, N), by adapter, then token, then slot;
  *              -1 for other ids (padding tokens, say with -1), which go nowhere
- *   offsets    the first place of every adapter; offsets[N] = the number of places taken, at most T*k
+ *   offsets    the first place of every adapter; offsets[N] = the number of places taken, at most T*k.  With T == 0 nothing is
+ *              launched and offsets are not written either (the caller clears them where something reads them)
  *   xs         row pos[t,j] is x[t].  Rows from offsets[N] on are left as they were.
  *   xs_scale == NULL: xs[T*k, d] in dt.  Otherwise xs is int8_t[T*k, d], quantised as in meteora_quantize_rows, and xs_scale[T*k]
  *              holds the rows' scales: the operand of meteora_gemm_i8.

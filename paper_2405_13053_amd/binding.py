@@ -481,6 +481,15 @@ def base_gemm(x, W, out: Optional[torch.Tensor] = None):
     return out
 
 
+# What stands for the address of an array without elements (T = 0), which has none: the library refuses NULL and reads nothing there.
+_EMPTY = 256
+
+
+def _pe(t: Optional[torch.Tensor]):
+    """_p of an array that has no elements where T = 0."""
+    return None if t is None else t.data_ptr() or _EMPTY
+
+
 def _chk_device(x: torch.Tensor, *others):
     """x lies on the current device, whose stream the call goes to, and the other tensors beside it."""
     dev = x.get_device()
@@ -502,7 +511,7 @@ def quantize_rows(x, out=None):
     q, scale = out
     _chk(q, "q", torch.int8, (rows, d)); _chk(scale, "scale", torch.float32, (rows,))
     _chk_device(x, q, scale)
-    st = load_library().meteora_quantize_rows(_p(x), rows, d, _dt(x), _p(q), _p(scale), _stream())
+    st = load_library().meteora_quantize_rows(_pe(x), rows, d, _dt(x), _pe(q), _pe(scale), _stream())
     if st != 0:
         raise MeteoraError(st, "meteora_quantize_rows")
     return q, scale
@@ -528,8 +537,8 @@ def gemm_i8(q, q_scale, W, w_scale, offsets=None, out: Optional[torch.Tensor] = 
         _chk(w_scale, "w_scale", torch.float32, (d_out,) if offsets is None else (N, d_out)); _chk(out, "out", None, (T, d_out))
     _chk(offsets, "offsets", torch.int32, (N + 1,))
     _chk_device(q, q_scale, W, w_scale, offsets, out)
-    st = load_library().meteora_gemm_i8(_p(q), _p(q_scale), _p(W), _p(w_scale), _p(offsets), T, d_in, d_out, N, _dt(out),
-                                        _p(out), _stream())
+    st = load_library().meteora_gemm_i8(_pe(q), _pe(q_scale), _p(W), _p(w_scale), _p(offsets), T, d_in, d_out, N, _dt(out),
+                                        _pe(out), _stream())
     if st != 0:
         raise MeteoraError(st, "meteora_gemm_i8")
     return out
@@ -557,7 +566,7 @@ def base_gemm_i8(x, W, w_scale, out: Optional[torch.Tensor] = None, ws: Optional
     _chk(ws, "ws", torch.uint8)
     ws = _ws(ws, lambda: base_gemm_i8_workspace_bytes(T, d_in), dev)
     _chk_device(x, W, w_scale, out, ws)
-    st = load_library().meteora_base_gemm_i8(_p(x), _p(W), _p(w_scale), T, d_in, d_out, _dt(x), _p(out), _p(ws), ws.numel(),
+    st = load_library().meteora_base_gemm_i8(_pe(x), _p(W), _p(w_scale), T, d_in, d_out, _dt(x), _pe(out), _p(ws), ws.numel(),
                                              _stream())
     if st != 0:
         raise MeteoraError(st, "meteora_base_gemm_i8")
@@ -570,7 +579,8 @@ def sort_workspace_bytes(T, k, N) -> int:
 
 def sort_tokens(x, topk_idx, N: int, quantize: bool = False, out: Optional[torch.Tensor] = None,
                 ws: Optional[torch.Tensor] = None):
-    """meteora_sort_tokens: (xs[T*k,d], pos[T,k], offsets[N+1]); with `quantize` (xs int8, xs_scale[T*k], pos, offsets)."""
+    """meteora_sort_tokens: (xs[T*k,d], pos[T,k], offsets[N+1]); with `quantize` (xs int8, xs_scale[T*k], pos, offsets).  Without
+    tokens offsets are zeros."""
     T, d = x.shape
     k = topk_idx.shape[1]
     dev = x.device
@@ -583,10 +593,10 @@ def sort_tokens(x, topk_idx, N: int, quantize: bool = False, out: Optional[torch
         _chk(x, "x"); _chk(topk_idx, "topk_idx", torch.int32, (T, k)); _chk(out, "out", dtype, (T * k, d))
     _chk(ws, "ws", torch.uint8)
     scale = torch.empty((T * k,), dtype=torch.float32, device=dev) if quantize else None
-    pos, offsets = torch.empty_like(topk_idx), topk_idx.new_empty((N + 1,))
+    pos, offsets = torch.empty_like(topk_idx), topk_idx.new_empty((N + 1,)) if T > 0 else topk_idx.new_zeros((N + 1,))
     ws = _ws(ws, lambda: sort_workspace_bytes(T, k, N), dev)
     _chk_device(x, topk_idx, out, ws)
-    st = load_library().meteora_sort_tokens(_p(x), _p(topk_idx), T, k, N, d, _dt(x), _p(out), _p(scale), _p(pos), _p(offsets),
+    st = load_library().meteora_sort_tokens(_pe(x), _pe(topk_idx), T, k, N, d, _dt(x), _pe(out), _pe(scale), _pe(pos), _p(offsets),
                                             _p(ws), ws.numel(), _stream())
     if st != 0:
         raise MeteoraError(st, "meteora_sort_tokens")
@@ -609,7 +619,7 @@ def unsort_tokens(ys, pos, w=None, scale: float = 1.0, base: Optional[torch.Tens
         _chk(ys, "ys"); _chk(pos, "pos", torch.int32, (T, k)); _chk(w, "w", torch.float32, (T, k))
         _chk(base, "base", ys.dtype, (T, d)); _chk(out, "out", ys.dtype, (T, d))
     _chk_device(ys, pos, w, base, out)
-    st = load_library().meteora_unsort_tokens(_p(ys), rows, _p(pos), _p(w), T, k, d, float(scale), _dt(ys), _p(base), _p(out),
+    st = load_library().meteora_unsort_tokens(_pe(ys), rows, _pe(pos), _pe(w), T, k, d, float(scale), _dt(ys), _pe(base), _pe(out),
                                               _stream())
     if st != 0:
         raise MeteoraError(st, "meteora_unsort_tokens")
@@ -634,8 +644,8 @@ def unsort_backward(dy, ys, pos, w=None, scale: float = 1.0, out: Optional[torch
     dw = None
     if want_dw:
         dw = torch.empty((T, k), dtype=torch.float32, device=dy.device) if w is None else torch.empty_like(w)
-    st = load_library().meteora_unsort_backward(_p(dy), _p(ys), rows, _p(pos), _p(w), T, k, d, float(scale), _dt(ys), _p(out),
-                                                _p(dw), _stream())
+    st = load_library().meteora_unsort_backward(_pe(dy), _pe(ys), rows, _pe(pos), _pe(w), T, k, d, float(scale), _dt(ys), _pe(out),
+                                                _pe(dw), _stream())
     if st != 0:
         raise MeteoraError(st, "meteora_unsort_backward")
     return out, dw

@@ -391,3 +391,41 @@ def test_binding_checks():
     with pytest.raises(ValueError):
         m.unsort_backward(x[:3], x, idx)
     assert m.unsort_tokens(x[:0], idx).abs().sum() == 0    # no rows: every place is outside
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_no_tokens(dtype):
+    """T = 0 (a step in which no sequence takes part): empty results, and no place taken."""
+    N, k, d, n = 4, 2, 64, 24
+    new = lambda *shape, dt=dtype: torch.empty(shape, device="cuda", dtype=dt)
+    x, idx, w = new(0, d), new(0, k, dt=torch.int32), new(0, k, dt=torch.float32)
+    W, ws = m.quantize_rows(torch.randn((N * n, d), device="cuda"))
+    W, ws = W.view(N, n, d), ws.view(N, n)
+    junk = torch.full((64,), 77, device="cuda", dtype=torch.int32)   # what the allocator may hand out for offsets
+    del junk
+    xs, pos, off = m.sort_tokens(x, idx, N)
+    assert xs.shape == (0, d) and pos.shape == (0, k) and torch.equal(off.cpu(), torch.zeros(N + 1, dtype=torch.int32))
+    xs, xsc, pos, off = m.sort_tokens(x, idx, N, quantize=True)
+    assert xs.shape == (0, d) and xsc.shape == (0,) and not off.cpu().any()
+    ys = m.gemm_i8(xs, xsc, W, ws, offsets=off, dtype=dtype)
+    assert ys.shape == (0, n) and m.gemm_i8(xs, xsc, W[0], ws[0], dtype=dtype).shape == (0, n)
+    base = m.base_gemm_i8(x, W[0], ws[0])
+    assert base.shape == (0, n)
+    assert m.unsort_tokens(ys, pos, w, 2.0, base=base, out=base) is base
+    dys, dw = m.unsort_backward(base, ys, pos, w, 2.0)
+    assert dys.shape == (0, n) and dw.shape == (0, k)
+    q, s = m.quantize_rows(x)
+    assert q.shape == (0, d) and s.shape == (0,)
+    # rows that no token asks for
+    ys = torch.randn((5, n), device="cuda").to(dtype)
+    kept = torch.full_like(ys, 7.0)
+    assert m.unsort_tokens(ys, pos, w).shape == (0, n)
+    _, dw = m.unsort_backward(base, ys, pos, w, out=kept)
+    assert dw.shape == (0, k) and (kept == 7).all()
+    # limits hold all the same
+    with pytest.raises(m.MeteoraError) as e:
+        m.sort_tokens(new(0, 12), idx, N)
+    assert e.value.status == 2
+    with pytest.raises(m.MeteoraError) as e:
+        m.quantize_rows(new(0, 12))
+    assert e.value.status == 2
