@@ -628,15 +628,18 @@ def unsort_tokens(ys, pos, w=None, scale: float = 1.0, base: Optional[torch.Tens
 
 def unsort_backward(dy, ys, pos, w=None, scale: float = 1.0, out: Optional[torch.Tensor] = None, want_dw: bool = True):
     """meteora_unsort_backward: (dys like ys, dw[T,k] f32 or None) for dy = dL/d(unsort_tokens).  Rows of dys that pos does not
-    name are left as they were in `out` (zeros if there is none)."""
-    rows, d = ys.shape
+    name are left as they were in `out` (zeros if there is none).  Without dw `ys` is not read: None, where there is an `out`."""
+    if ys is None and (want_dw or out is None):
+        raise ValueError("dw needs ys" if want_dw else "without ys an out says how many rows there are")
+    like = out if ys is None else ys
+    rows, d = like.shape
     T, k = pos.shape
-    dtype = ys.dtype
+    dtype = like.dtype
     if out is None:
         out = torch.zeros((rows, d), dtype=dtype, device=ys.device)
     # written out, as in linear_forward
     if not (dy.dtype == dtype and dy.shape == (T, d) and out.dtype == dtype and out.shape == (rows, d) and pos.dtype == torch.int32 and
-            ys.is_cuda and ys.is_contiguous() and dy.is_contiguous() and out.is_contiguous() and pos.is_contiguous() and
+            dy.is_cuda and like.is_contiguous() and dy.is_contiguous() and out.is_contiguous() and pos.is_contiguous() and
             (w is None or (w.dtype == torch.float32 and w.shape == (T, k) and w.is_contiguous()))):
         _chk(dy, "dy", dtype, (T, d)); _chk(ys, "ys"); _chk(pos, "pos", torch.int32, (T, k)); _chk(w, "w", torch.float32, (T, k))
         _chk(out, "out", dtype, (rows, d))
@@ -644,7 +647,7 @@ def unsort_backward(dy, ys, pos, w=None, scale: float = 1.0, out: Optional[torch
     dw = None
     if want_dw:
         dw = torch.empty((T, k), dtype=torch.float32, device=dy.device) if w is None else torch.empty_like(w)
-    st = load_library().meteora_unsort_backward(_pe(dy), _pe(ys), rows, _pe(pos), _pe(w), T, k, d, float(scale), _dt(ys), _pe(out),
+    st = load_library().meteora_unsort_backward(_pe(dy), _pe(ys), rows, _pe(pos), _pe(w), T, k, d, float(scale), _dt(out), _pe(out),
                                                 _pe(dw), _stream())
     if st != 0:
         raise MeteoraError(st, "meteora_unsort_backward")

@@ -429,3 +429,25 @@ def test_no_tokens(dtype):
     with pytest.raises(m.MeteoraError) as e:
         m.quantize_rows(new(0, 12))
     assert e.value.status == 2
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,k,d", [(1, 1, 8), (37, 3, 136), (40, 2, 5128), (600, 2, 4104)])
+def test_unsort_backward_without_the_rows(T, k, d, dtype):
+    """Frozen weights of the slots: no dw, and then the rows ys are not read and need not be there."""
+    g = gen(T + d)
+    pos, _ = places(routing(T, 5, k, "padded", g).cpu(), 5)
+    dy, w = torch.randn((T, d), generator=g, device="cuda").to(dtype), torch.randn((T, k), generator=g, device="cuda")
+    ys = torch.randn((T * k, d), generator=g, device="cuda").to(dtype)
+    want, _ = m.unsort_backward(dy, ys, pos.cuda(), w, 1.5, out=torch.full_like(ys, 7.0))
+    out = torch.full_like(ys, 7.0)
+    dys, dw = m.unsort_backward(dy, None, pos.cuda(), w, 1.5, out=out, want_dw=False)
+    assert dys is out and dw is None and torch.equal(dys, want)
+    with pytest.raises(ValueError):
+        m.unsort_backward(dy, None, pos.cuda(), w, 1.5, out=out)            # dw is a product with ys
+    with pytest.raises(ValueError):
+        m.unsort_backward(dy, None, pos.cuda(), w, 1.5, want_dw=False)      # nothing says how many rows there are
+    with pytest.raises(TypeError):
+        m.unsort_backward(dy, None, pos.cuda(), w, 1.5, out=out.double(), want_dw=False)
+    with pytest.raises(ValueError):
+        m.unsort_backward(dy, None, pos.cuda(), w, 1.5, out=out[:, :d - 1], want_dw=False)
