@@ -357,14 +357,18 @@ meteora_status meteora_quantize_rows(const void* x /*[rows,d]*/, int rows, int d
 /*
  * Product of 8-bit whole numbers with a scale per token and per output channel, over groups of consecutive rows:
  *   out[t,c] = q_scale[t] * w_scale[e,c] * sum_i q[t,i] * W[e,c,i],   e = the group with offsets[e] <= t < offsets[e+1]
- * The sum is exact (whole numbers); fp32 scaling, one rounding where dt (the type of out) is METEORA_BF16.
+ * The sum is exact (whole numbers); fp32 scaling, by q_scale first, one rounding where dt (the type of out) is METEORA_BF16.
  *   offsets == NULL: N = 1, all rows are one group: a base projection (the 8-bit counterpart of meteora_base_gemm on rows
  *                    that are quantised already).
  *   offsets[N+1] (device): groups as meteora_sort_tokens and meteora_bucket_tokens return them, one matrix per adapter;
  *                    groups may be empty.  Rows outside every group (t >= offsets[N]) are left as they were in out.
  *                    Offsets must lie in [0, T] and not fall; whatever they hold, only rows in [0, T) are read and written.
- * Integer weights are frozen: there is no gradient for W.  The gradient with respect to the rows is a call of this entry point
- * on the weight transposed and quantised anew.
+ * Integer weights are frozen: there is no gradient for W.  The gradient with respect to the rows that were quantised (the rounding passed
+ * by) is dx[t,i] = sum_c dy[t,c] * w_scale[e,c] * W[e,c,i], whose scales lie along the sum: no call of this entry point computes it.  In
+ * bf16 it is meteora_base_gemm of dy on the matrix V[i,c] = w_scale[e,c] * W[e,c,i].  In 8 bits it is approximated by this entry point on
+ * dy and V quantised anew, each with a rounding of its own: with a = max_c |dy[t,c]| and b = max_c |V[i,c]| off by up to
+ *   sum_c (|V[i,c]| * a + |dy[t,c]| * b + a * b / 254) / 254
+ * before the output's rounding.
  * Limits: d_in % 16 == 0, d_in <= 131056, d_out % 8 == 0, d_out <= 2^20, N <= 64, T < 2^24, T * d_out < 2^33.
  */
 meteora_status meteora_gemm_i8(const int8_t* q /*[T,d_in]*/, const float* q_scale /*[T]*/, const int8_t* W /*[N,d_out,d_in]*/,

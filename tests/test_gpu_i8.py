@@ -378,3 +378,35 @@ def test_binding_checks():
         m.base_gemm_i8(torch.zeros((4, 64), device="cuda"), torch.zeros((8, 64), dtype=torch.int8, device="cuda"),
                        torch.zeros(8, device="cuda"), ws=torch.empty(64, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 3
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,d_in,d_out", [(1, 64, 16), (33, 272, 528), (300, 1024, 1040), (1000, 528, 256)])
+def test_gradient_of_the_rows(T, d_in, d_out, dtype):
+    """dx = dy V with V[c,i] = w_scale[c] W[c,i], as an 8-bit product of dy and V^T quantised anew: each element of dy is off by half a step,
+    a / 254, each of V by b / 254, and the product by what the two add up to.  Rounded beyond that: V and both scales (2^-24 each), the two
+    scalings, and the output.  And as a bf16 product on V rounded to bf16: 2^-8 of each product, and fp32 sums."""
+    g = gen(T + d_in)
+    W, ws = m.quantize_rows(torch.randn((d_out, d_in), generator=g, device="cuda") * d_in ** -0.5)
+    dy = torch.randn((T, d_out), generator=g, device="cuda").to(dtype)
+    V = (W.float() * ws[:, None]).t().contiguous()      # [d_in, d_out]
+    exact = dy.double() @ (W.double() * ws.double()[:, None])
+    Vq, vs = m.quantize_rows(V)
+    q, s = m.quantize_rows(dy)
+    dx = m.gemm_i8(q, s, Vq, vs, dtype=dtype)
+    a, b = dy.double().abs().amax(1)[:, None], V.double().abs().amax(1)[None, :]
+    size = dy.double().abs() @ V.double().abs().t()
+    off = (V.double().abs().sum(1)[None, :] * a + dy.double().abs().sum(1)[:, None] * b + d_out * a * b / 254) / 254
+    tol = off * (1 + 8 * U32) + 8 * U32 * (size + off)
+    tol = tol + half_step(dtype) * 1.001 * (exact.abs() + tol)
+    assert ((dx.double() - exact).abs() <= tol).all()
+    if dtype == torch.bfloat16:
+        dx = m.base_gemm(dy, V.bfloat16())
+        tol = (2.0 ** -8 * 1.001 + (d_out + 2) * U32) * size
+        assert ((dx.double() - exact).abs() <= tol + half_step(dtype) * 1.001 * (exact.abs() + tol)).all()
+    # against differences: the product is linear in its rows, and a row of the identity gives a column of V
+    eye, es = m.quantize_rows(torch.eye(d_in, device="cuda")[:16].contiguous())
+    col = m.gemm_i8(eye, es, W, ws, dtype=torch.float32)    # [16, d_out]: V's first rows
+    assert ((col - V[:16]).abs() <= 4 * U32 * V[:16].abs()).all()
+    part = dy.double() @ col.double().t()
+    assert ((part - exact[:, :16]).abs() <= 5 * U32 * size[:, :16]).all()
