@@ -60,7 +60,10 @@ struct SortArgs {
     float* xs_scale;               // [T*k]
 };
 
-constexpr int kSortChunkPairs = 128;   // of the one-launch form, at most: 16 tokens of 8 pairs
+// The one-launch form: every workgroup counts all pairs, so it takes few of them and up to 1024 workgroups.  ceil(T / 1024) tokens to a
+// workgroup, T * k <= kOneLaunchPairs: at most T * k / 1024 + k pairs.
+constexpr int kOneLaunchPairs = 16384, kOneLaunchChunks = 1024;
+constexpr int kSortChunkPairs = kOneLaunchPairs / kOneLaunchChunks + kMaxTopK;
 
 struct SortShared {
     Counters before, rest;
@@ -315,10 +318,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_quantize_kernel(const SortA
 // 4096 20.2 and 28.9 / 23.6 and 25.6, 8192 x 4096 40.4 and 43.0 / 42.6 and 35.6, 8192 x 1024 16.3 and 18.5 / 16.8 and 18.5; top-8 2048 x
 // 1024 14.7 and 21.0 / 15.1 and 22.2, 4096 x 1024 31.8 and 22.0 / 31.1 and 20.2 (as 256 workgroups 20.7 / 22.2).
 static bool sort_in_one(int64_t pairs, int64_t elements, bool quantised) {
-    return pairs <= 16384 && !(quantised && elements > (int64_t)1 << 24);
+    return pairs <= kOneLaunchPairs && !(quantised && elements > (int64_t)1 << 24);
 }
-// With few pairs every workgroup of the one launch counts all of them: up to 1024 workgroups.
-static int sort_chunk_tokens(int T) { return ceil_div(T, 1024); }
+static int sort_chunk_tokens(int T) { return ceil_div(T, kOneLaunchChunks); }
 // With many, a launch of histograms, one of places, which adds up those of all chunks, and one of rows.
 constexpr int kCountChunks = 256;
 static int count_chunk_tokens(int T) { return ceil_div(T, kCountChunks); }
@@ -356,6 +358,7 @@ hipError_t launch_sort_tokens(const void* x, const int32_t* topk_idx, int T, int
     const int row16 = d / (bf16 ? 8 : 4), lanes = lanes_log2_for(row16);
     if (sort_in_one(a.pairs, (int64_t)T * d, xs_scale != nullptr)) {
         a.chunk_tokens = sort_chunk_tokens(T);
+        if (a.chunk_tokens * k > kSortChunkPairs) return hipErrorInvalidValue;   // places[] of the kernels
         a.nchunks = ceil_div(T, a.chunk_tokens);
         if (xs_scale != nullptr)
             return bf16 ? launch_sort_quantize(a, (const bf16_t*)x, (int8_t*)xs, stream)

@@ -451,3 +451,37 @@ def test_unsort_backward_without_the_rows(T, k, d, dtype):
         m.unsort_backward(dy, None, pos.cuda(), w, 1.5, out=out.double(), want_dw=False)
     with pytest.raises(ValueError):
         m.unsort_backward(dy, None, pos.cuda(), w, 1.5, out=out[:, :d - 1], want_dw=False)
+
+
+def places_sorted(idx, N):
+    """pos, offsets by a stable sort, on the GPU."""
+    flat = idx.flatten()
+    valid = (flat >= 0) & (flat < N)
+    key = torch.where(valid, flat, N).long()
+    pos = torch.empty_like(flat)
+    pos[torch.argsort(key, stable=True)] = torch.arange(flat.numel(), device=idx.device, dtype=torch.int32)
+    counts = torch.bincount(key, minlength=N + 1)[:N]
+    offsets = torch.cat([counts.new_zeros(1), counts.cumsum(0)]).to(torch.int32)
+    return torch.where(valid, pos, -1).view_as(idx), offsets
+
+
+# as many pairs as the one launch takes with the most to a workgroup (21 of them with k = 7), and one token more
+BORDER = [(2340, 64, 7), (2341, 64, 7), (3276, 28, 5), (3277, 28, 5), (16384, 28, 1), (16385, 28, 1), (2048, 64, 8), (2049, 64, 8), (8192, 4, 2)]
+
+
+@pytest.mark.parametrize("kind", ["uniform", "one", "padded"])
+@pytest.mark.parametrize("T,N,k", BORDER)
+def test_sort_either_side_of_the_one_launch(T, N, k, kind):
+    g = gen(T + 23 * k)
+    idx = routing(T, N, k, kind, g)
+    pos, off = places_sorted(idx, N)
+    for dtype, d in ((torch.bfloat16, 8), (torch.float32, 72), (torch.bfloat16, 2056)):
+        x = torch.randn((T, d), generator=g, device="cuda").to(dtype)
+        xs = torch.full((T * k + 1, d), 7.0, device="cuda", dtype=dtype)
+        _, gpos, goff = m.sort_tokens(x, idx, N, out=xs[:T * k])
+        assert torch.equal(gpos, pos) and torch.equal(goff, off)
+        want = torch.full_like(xs, 7.0)
+        for j in range(k):
+            there = pos[:, j] >= 0
+            want[pos[there, j].long()] = x[there]
+        assert torch.equal(xs, want)
