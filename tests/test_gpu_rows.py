@@ -485,3 +485,37 @@ def test_sort_either_side_of_the_one_launch(T, N, k, kind):
             there = pos[:, j] >= 0
             want[pos[there, j].long()] = x[there]
         assert torch.equal(xs, want)
+
+
+# rows in a launch of their own: every width at which a wavefront or a workgroup holds another number of pieces, and rows that are read
+# twice; the last ones have few pairs and more than 2^24 elements
+MOVED = [(2049, 64, 8, 16), (2049, 64, 8, 512), (2341, 64, 7, 520), (8200, 28, 2, 2048), (2049, 5, 8, 2056), (16385, 28, 1, 1032),
+         (2060, 64, 8, 4096), (2050, 7, 8, 4104), (2049, 4, 8, 8200), (2049, 4, 8, 16392), (1030, 4, 2, 16400), (5000, 28, 2, 4096)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", ["uniform", "padded"])
+@pytest.mark.parametrize("T,N,k,d", MOVED)
+def test_sort_quantised_with_the_rows_in_a_launch_of_their_own(T, N, k, d, kind, dtype):
+    g = gen(T + d)
+    idx = routing(T, N, k, kind, g)
+    pos, off = places_sorted(idx, N)
+    x = torch.randn((T, d), generator=g, device="cuda").to(dtype)
+    x[T // 2] = 0
+    x[1, d - 1], x[T - 1, 0], x[T - 1, d // 2] = float("nan"), float("inf"), -float("inf")
+    good = torch.isfinite(x).all(1)
+    finite = torch.where(good[:, None], x, torch.zeros_like(x))
+    q, _ = rows_ref(finite)
+    # by a tensor: fp32 tensors of a GPU are divided by a number by its reciprocal, which is an ulp off
+    s = finite.abs().amax(1).float() / torch.full((T,), 127.0, device="cuda")
+    s[1], s[T - 1] = float("nan"), float("inf")
+    xs = torch.full((T * k + 1, d), 7, device="cuda", dtype=torch.int8)
+    _, sc, gpos, goff = m.sort_tokens(x, idx, N, quantize=True, out=xs[:T * k])
+    assert torch.equal(gpos, pos) and torch.equal(goff, off)
+    want = torch.full_like(xs, 7)
+    for j in range(k):
+        there = pos[:, j] >= 0
+        at = pos[there, j].long()
+        want[at] = q[there]
+        assert torch.equal(torch.nan_to_num(sc[at], nan=-1.0), torch.nan_to_num(s[there], nan=-1.0))
+    assert torch.equal(xs, want)
