@@ -376,6 +376,16 @@ meteora_status meteora_gemm_i8(const int8_t* q /*[T,d_in]*/, const float* q_scal
                                int d_out, int N, meteora_dtype dt, void* out /*[T,d_out]*/, meteora_stream stream);
 
 /*
+ * The kernel that meteora_gemm_i8 starts for these sizes, for tests that mean to reach every one.  Host only, no HIP call.  grouped:
+ * offsets are given.  The host pointers (each may be NULL) receive its name (a static string: "one" for up to 128 inputs, "wave" for few
+ * rows, "ring" for many), the rows and columns of its tiles, the workgroups that share a CU, whether the weights of a group with a
+ * single row tile are requested as read once, and whether a second launch takes the tiles of a last, nearly empty round.  Returns 0, or -1
+ * for arguments outside the limits of meteora_gemm_i8 and for T == 0.
+ */
+int meteora_gemm_i8_kernel(int T, int d_in, int d_out, int N, int grouped, const char** name /*host*/, int* tile_rows /*host*/,
+                           int* tile_cols /*host*/, int* per_cu /*host*/, int* read_once /*host*/, int* tail /*host*/);
+
+/*
  * Base projection with the weight in 8 bits: meteora_quantize_rows of x, then meteora_gemm_i8 with one group.  x and out in dt.
  * ws: meteora_base_gemm_i8_workspace_bytes(T, d_in) bytes (the quantised rows and their scales), which also holds any smaller T;
  * 0 for arguments outside the limits of meteora_gemm_i8.

@@ -88,6 +88,8 @@ def load_library():
     lib.meteora_quantize_rows.argtypes = [vp, i, i, i, vp, vp, vp]
     lib.meteora_gemm_i8.restype = i
     lib.meteora_gemm_i8.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, i, vp, vp]
+    lib.meteora_gemm_i8_kernel.restype = i
+    lib.meteora_gemm_i8_kernel.argtypes = [i, i, i, i, i, vp, vp, vp, vp, vp, vp]
     lib.meteora_base_gemm_i8_workspace_bytes.restype = sz
     lib.meteora_base_gemm_i8_workspace_bytes.argtypes = [i, i]
     lib.meteora_base_gemm_i8.restype = i
@@ -542,6 +544,17 @@ def gemm_i8(q, q_scale, W, w_scale, offsets=None, out: Optional[torch.Tensor] = 
     if st != 0:
         raise MeteoraError(st, "meteora_gemm_i8")
     return out
+
+
+def gemm_i8_kernel(T: int, d_in: int, d_out: int, N: Optional[int] = None):
+    """meteora_gemm_i8_kernel: (name, tile_rows, tile_cols, per_cu, read_once, tail) of the kernel that gemm_i8 starts, for N groups or for
+    none; None outside the limits."""
+    name, ints = ctypes.c_char_p(), [ctypes.c_int() for _ in range(5)]
+    if load_library().meteora_gemm_i8_kernel(T, d_in, d_out, 1 if N is None else N, int(N is not None), ctypes.byref(name),
+                                             *(ctypes.byref(v) for v in ints)) != 0:
+        return None
+    rows, cols, per_cu, once, tail = (v.value for v in ints)
+    return name.value.decode(), rows, cols, per_cu, bool(once), bool(tail)
 
 
 def base_gemm_i8_workspace_bytes(T, d_in) -> int:

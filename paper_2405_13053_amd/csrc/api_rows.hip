@@ -39,12 +39,15 @@ meteora_status meteora_quantize_rows(const void* x, int rows, int d, meteora_dty
     return status(launch_quantize_rows(x, rows, d, dt == METEORA_BF16, q, scale, static_cast<hipStream_t>(stream)));
 }
 
+static bool i8_sizes_supported(int T, int d_in, int d_out) {
+    return d_in % 16 == 0 && d_in <= kI8MaxInputs && d_out % 8 == 0 && d_out <= kI8MaxOutputs && T <= kRowsMax &&
+           (int64_t)T * d_out < (int64_t)1 << 33;
+}
+
 static meteora_status check_i8_weights(const int8_t* W, const float* w_scale, int T, int d_in, int d_out, meteora_dtype dt,
                                        const void* out) {
     if (!W || !w_scale || !out || T < 0 || d_in < 1 || d_out < 1) return METEORA_ERR_INVALID_ARG;
-    if (!known(dt) || d_in % 16 != 0 || d_in > kI8MaxInputs || d_out % 8 != 0 || d_out > kI8MaxOutputs || T > kRowsMax ||
-        (int64_t)T * d_out >= (int64_t)1 << 33)
-        return METEORA_ERR_UNSUPPORTED;
+    if (!known(dt) || !i8_sizes_supported(T, d_in, d_out)) return METEORA_ERR_UNSUPPORTED;
     if (!aligned(W, 16) || !aligned(w_scale, 16) || !aligned(out, 16)) return METEORA_ERR_UNSUPPORTED;
     return METEORA_OK;
 }
@@ -60,6 +63,20 @@ meteora_status meteora_gemm_i8(const int8_t* q, const float* q_scale, const int8
     if (T == 0) return METEORA_OK;
     return status(launch_gemm_i8(q, q_scale, W, w_scale, offsets, T, d_in, d_out, N, dt == METEORA_BF16, out,
                                  static_cast<hipStream_t>(stream)));
+}
+
+int meteora_gemm_i8_kernel(int T, int d_in, int d_out, int N, int grouped, const char** name, int* tile_rows, int* tile_cols,
+                           int* per_cu, int* read_once, int* tail) {
+    if (T < 1 || d_in < 1 || d_out < 1 || N < 1 || N > kMaxAdapters || (!grouped && N != 1) || !i8_sizes_supported(T, d_in, d_out))
+        return -1;
+    const I8Plan p = gemm_i8_plan(T, d_in, d_out, N, grouped != 0);
+    if (name) *name = p.kernel;
+    if (tile_rows) *tile_rows = p.rows;
+    if (tile_cols) *tile_cols = p.cols;
+    if (per_cu) *per_cu = p.per_cu;
+    if (read_once) *read_once = p.once;
+    if (tail) *tail = p.tail;
+    return 0;
 }
 
 size_t meteora_base_gemm_i8_workspace_bytes(int T, int d_in) {

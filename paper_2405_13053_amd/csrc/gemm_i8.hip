@@ -761,10 +761,13 @@ static hipError_t launch_ring_i8(GemmI8Args a, hipStream_t stream) {
 // and so, us: 4300, 5000 and 9000 x 4096 -> 4096 69.4, 77.7, 141 and 69.3, 74.7, 123; 5000 x 4096 -> 14336 247 and 228; 8 groups of 4096 ->
 // 4096, 4002 and 8192 rows that fall off as 1 / j^2 92.5, 141 and 81.4, 124, dealt evenly (whole rounds: the second launch finds nothing)
 // 53.4, 102 and 55.6, 103.  The size of the tail's tiles, 16 tiles of 8 groups of 4096 -> 4096 behind 256: 128 x 128 76.3, 64 x 64 68.3.
+static bool may_have_tail(const GemmI8Args& a, int64_t tiles) {   // the most that there may be, of 256 x 256
+    return tiles > 256 && (a.offsets != nullptr || tail_start((int)tiles) != tiles);
+}
 template <typename TO>
 static hipError_t launch_largest_i8(GemmI8Args a, hipStream_t stream) {
     const int64_t tiles = (int64_t)most_row_tiles(a, 256) * ceil_div(a.d_out, 256);
-    a.tail = tiles > 256 && (a.offsets != nullptr || tail_start((int)tiles) != tiles) ? 1 : 0;
+    a.tail = may_have_tail(a, tiles) ? 1 : 0;
     const hipError_t e = launch_ring_i8<TO, 8, 8, 2>(a, stream);
     if (e != hipSuccess || a.tail == 0) return e;
     a.tiles_m = most_row_tiles(a, 256);
@@ -933,13 +936,27 @@ hipError_t launch_base_gemm_i8_in_one(const void* x, const int8_t* W, const floa
     return bf16 ? launch_base(a, (const bf16_t*)x, stream) : launch_base(a, (const float*)x, stream);
 }
 
-hipError_t launch_gemm_i8(const int8_t* q, const float* q_scale, const int8_t* W, const float* w_scale, const int32_t* offsets,
-                          int T, int d_in, int d_out, int N, bool bf16, void* out, hipStream_t stream) {
+static GemmI8Args i8_args(const int8_t* q, const float* q_scale, const int8_t* W, const float* w_scale, const int32_t* offsets,
+                          int T, int d_in, int d_out, int N, void* out) {
     // The last cache holds 256 MB: from three such matrices in turn on none is still there.  Three in turn, 128 x 128 tiles, requested as kept and
     // as read once, us: 67 MB 14.3 and 15.9, 84 MB 19.5 and 22.0, 101 MB 23.9 and 24.0, 117 MB 26.9 and 25.1, 134 MB 29.0 and 25.4.
     const int past_caches = (int64_t)N * d_out * d_in >= 100000000;
-    const GemmI8Args a{q, q_scale, W, w_scale, offsets, out, T, d_in, d_out, N, 0, 0, 0, 0, past_caches};
+    return {q, q_scale, W, w_scale, offsets, out, T, d_in, d_out, N, 0, 0, 0, 0, past_caches};
+}
+hipError_t launch_gemm_i8(const int8_t* q, const float* q_scale, const int8_t* W, const float* w_scale, const int32_t* offsets,
+                          int T, int d_in, int d_out, int N, bool bf16, void* out, hipStream_t stream) {
+    const GemmI8Args a = i8_args(q, q_scale, W, w_scale, offsets, T, d_in, d_out, N, out);
     return bf16 ? launch_i8<bf16_t>(a, stream) : launch_i8<float>(a, stream);
+}
+
+I8Plan gemm_i8_plan(int T, int d_in, int d_out, int N, bool grouped) {
+    static const int32_t some = 0;   // offsets, which the host does not read
+    const GemmI8Args a = i8_args(nullptr, nullptr, nullptr, nullptr, grouped ? &some : nullptr, T, d_in, d_out, N, nullptr);
+    if (d_in <= kI8Tile) return {"one", 64, 128, 1, false, false};
+    const I8Shape& s = kI8Shapes[choose_shape(a)];
+    const bool largest = s.rows * s.cols == 256 * 256;
+    return {s.wave ? "wave" : "ring", s.rows, s.cols, s.per_cu, !s.wave && !largest && a.past_caches != 0,
+            largest && may_have_tail(a, (int64_t)most_row_tiles(a, 256) * ceil_div(d_out, 256))};
 }
 
 template <typename TO, int TB, int RB, int WV, int D>

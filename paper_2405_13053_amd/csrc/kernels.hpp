@@ -229,6 +229,13 @@ hipError_t launch_gemm(const void* x, const void* W, int T, int d_in, int d_out,
 hipError_t launch_quantize_rows(const void* x, int rows, int d, bool bf16, int8_t* q, float* scale, hipStream_t stream);
 hipError_t launch_gemm_i8(const int8_t* q, const float* q_scale, const int8_t* W, const float* w_scale, const int32_t* offsets,
                           int T, int d_in, int d_out, int N, bool bf16, void* out, hipStream_t stream);
+// What it starts: kernel, tiles, workgroups that share a CU; weights of a single row tile requested as read once; a tail of smaller tiles.
+struct I8Plan {
+    const char* kernel;
+    int rows, cols, per_cu;
+    bool once, tail;
+};
+I8Plan gemm_i8_plan(int T, int d_in, int d_out, int N, bool grouped);
 // the quantisation and the product of a few tokens in one launch
 bool base_gemm_i8_in_one(int T, int d_in);
 hipError_t launch_base_gemm_i8_in_one(const void* x, const int8_t* W, const float* w_scale, int T, int d_in, int d_out, bool bf16,

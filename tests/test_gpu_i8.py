@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import paper_2405_13053_amd as m
+from tests import i8_kernels
 
 pytestmark = pytest.mark.gpu
 U32 = 2.0 ** -24
@@ -410,3 +411,38 @@ def test_gradient_of_the_rows(T, d_in, d_out, dtype):
     assert ((col - V[:16]).abs() <= 4 * U32 * V[:16].abs()).all()
     part = dy.double() @ col.double().t()
     assert ((part - exact[:, :16]).abs() <= 5 * U32 * size[:, :16]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,d_in,d_out,N", i8_kernels.PRODUCTS)
+def test_every_kernel_of_the_product(T, d_in, d_out, N, dtype):
+    """Sizes that lead to each tile shape and copy of its loop, dense and over groups, with whole K tiles and with a partial one."""
+    g = gen(T + d_in + d_out)
+    out = torch.full((T + 1, d_out), 7.0, device="cuda", dtype=dtype)
+    if N is None:
+        q, W = int8((T, d_in), g, -128), int8((d_out, d_in), g, -128)
+        qs, ws = scales((T,), g), scales((d_out,), g)
+        m.gemm_i8(q, qs, W, ws, out=out[:T])
+        close(out[:T], dense_ref(q, qs, W, ws))
+        assert (out[T] == 7).all()
+        return
+    counts = i8_kernels.deal(T, N)
+    q, qs, W, ws, off = grouped_case(T, N, d_in, d_out, counts, g)
+    m.gemm_i8(q, qs, W, ws, offsets=off.cuda(), out=out[:T])
+    for e in range(N):
+        a, b = int(off[e]), int(off[e + 1])
+        close(out[a:b], dense_ref(q[a:b], qs[a:b], W[e], ws[e]))
+    assert (out[int(off[-1]):] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,d_in,d_out", [case for cases in i8_kernels.TAILS.values() for case in cases])
+def test_tails_of_a_dense_product_at_their_borders(T, d_in, d_out, dtype):
+    """1, 16, 17, 32, 33 and 128 tiles of 256 x 256 behind a whole round, which the largest tiles then leave to smaller ones."""
+    g = gen(T + d_in)
+    q, W = int8((T, d_in), g), int8((d_out, d_in), g)
+    qs, ws = scales((T,), g), scales((d_out,), g)
+    out = torch.full((T + 1, d_out), 7.0, device="cuda", dtype=dtype)
+    m.gemm_i8(q, qs, W, ws, out=out[:T])
+    close(out[:T], dense_ref(q, qs, W, ws))
+    assert (out[T] == 7).all()
