@@ -519,3 +519,40 @@ def test_sort_quantised_with_the_rows_in_a_launch_of_their_own(T, N, k, d, kind,
         want[at] = q[there]
         assert torch.equal(torch.nan_to_num(sc[at], nan=-1.0), torch.nan_to_num(s[there], nan=-1.0))
     assert torch.equal(xs, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,d_in,d_out,N,r,k", [(1, 512, 264, 4, 8, 2), (4, 1024, 1032, 28, 8, 2), (40, 528, 776, 8, 16, 2),
+                                                (300, 1040, 512, 28, 8, 1), (1100, 512, 1032, 28, 8, 2)])
+def test_a_layer_on_an_8_bit_base(T, d_in, d_out, N, r, k, dtype):
+    """The frozen base projection in 8 bits and the layer's own adapters on it: base_gemm_i8, gate_topk, lora_forward onto its output.
+    Rounded: the base's scales and scalings (4 * 2^-24) and its output; s w h, in bf16 as the operand of the expand; fp32 sums over d_in and
+    over the k r products; the sum of the two as the output."""
+    g = gen(T + d_out)
+    x = torch.randn((T, d_in), generator=g, device="cuda").to(dtype)
+    W, wsc = m.quantize_rows(torch.randn((d_out, d_in), generator=g, device="cuda") * d_in ** -0.5)
+    Wg = torch.randn((d_in, N), generator=g, device="cuda") * d_in ** -0.5
+    A = (torch.randn((N, d_in, r), generator=g, device="cuda") * d_in ** -0.5).to(dtype)
+    B = (torch.randn((N, r, d_out), generator=g, device="cuda") * r ** -0.5).to(dtype)
+    out = m.base_gemm_i8(x, W, wsc)
+    idx, w, _ = m.gate_topk(x, Wg, None, k)
+    assert m.lora_forward(x, A, B, idx, w, 2.0, out=out, accumulate=True) is out
+    q, _ = rows_ref(x.cpu())
+    base = dense_ref(q, x.cpu().abs().amax(1).double() / 127, W.cpu(), wsc.cpu())
+    xd, A, B, idx, w = x.cpu().double(), A.cpu().double(), B.cpu().double(), idx.cpu().long(), w.cpu().double()
+    logits = xd @ Wg.cpu().double()
+    top = logits.topk(k, 1).values[:, -1:]
+    assert (logits.gather(1, idx) >= top - 1e-4).all()
+    want, mag = base.clone(), torch.zeros_like(base)
+    for j in range(k):
+        for e in range(N):
+            t = idx[:, j] == e
+            want[t] += 2.0 * w[t, j, None] * ((xd[t] @ A[e]) @ B[e])
+            mag[t] += 2.0 * w[t, j, None] * ((xd[t].abs() @ A[e].abs()) @ B[e].abs())
+            if dtype == torch.bfloat16:
+                half = 2.0 * w[t, j, None] * ((xd[t] @ A[e]).abs() @ B[e].abs())
+                mag[t] += half * half_step(dtype) / ((d_in + k * r + 8) * U32)
+    u = half_step(dtype) * 1.01
+    tol = (u + 4 * U32) * base.abs() + 1.01 * (d_in + k * r + 8) * U32 * mag
+    tol = tol + (u + U32) * (want.abs() + tol)
+    assert ((out.cpu().double() - want).abs() <= tol).all()
