@@ -94,7 +94,12 @@ __device__ __forceinline__ int xcd_order(int wg, int total) {
     return xcd * per + min(xcd, rest) + wg / 8;
 }
 
-constexpr int kReadOnceI8 = 2;   // cache policy of the weights of few rows: "nt", what a call reads is gone before its next
+// Cache policy of the weights of few rows: "nt", for weights that come from memory, as a model's layers in turn do; what it costs where they
+// are still in a cache, or where many row tiles read long rows again, is accepted.  Read once and kept, us, weights in turn: 8 groups of
+// 4096 -> 4096, 16 rows 25.8 and 29.0, 16 x 4096 -> 4096 5.7 and 6.0, 64 x 4096 -> 4096 7.9 and 8.2, 16 x 5120 -> 13824 13.7 and 15.2, 64 x
+// 14336 -> 4096 22.8 and 22.1, 64 and 700 x 131056 -> 264 106 and 79, 215 and 146; the same weights again and again: 26.9 and 23.8, 4.0
+// and 4.0, 5.8 and 5.8, 12.9 and 12.9, 21.2 and 13.5, 110 and 59, 216 and 134.
+constexpr int kReadOnceI8 = 2;
 constexpr uint32_t kOutside = 0x80000000u;   // past every resource here, also with a K offset added
 
 template <typename TO>
@@ -760,7 +765,8 @@ static hipError_t launch_ring_i8(GemmI8Args a, hipStream_t stream) {
 // 256 x 256 tiles, and the tail where there is, or (groups) may be, one.  As the best of the shapes with a round of their own for the rest,
 // and so, us: 4300, 5000 and 9000 x 4096 -> 4096 69.4, 77.7, 141 and 69.3, 74.7, 123; 5000 x 4096 -> 14336 247 and 228; 8 groups of 4096 ->
 // 4096, 4002 and 8192 rows that fall off as 1 / j^2 92.5, 141 and 81.4, 124, dealt evenly (whole rounds: the second launch finds nothing)
-// 53.4, 102 and 55.6, 103.  The size of the tail's tiles, 16 tiles of 8 groups of 4096 -> 4096 behind 256: 128 x 128 76.3, 64 x 64 68.3.
+// 53.4, 102 and 55.6, 103.  The size of the tail's tiles, 16 tiles of 8 groups of 4096 -> 4096 behind 256: 128 x 128 76.3, 64 x 64 68.3; 32 tiles:
+// 128 x 128 78, 128 x 64 74, 64 x 64 76; dense, 17 tiles of 5263 x 4096 -> 3176 69, 64 and 69, 32 of 4600 x 4096 -> 4096 71, 68 and 71.
 static bool may_have_tail(const GemmI8Args& a, int64_t tiles) {   // the most that there may be, of 256 x 256
     return tiles > 256 && (a.offsets != nullptr || tail_start((int)tiles) != tiles);
 }
@@ -802,7 +808,10 @@ static hipError_t launch_one_i8(GemmI8Args a, hipStream_t stream) {
 // them, random deals of chances 1, 1 / j and 1 / j^2), W not in the caches: on the dense ones the choice is 0.6% slower on average than the
 // best shape of each, on the groups with their deals known 1.1%.  How rows are dealt is known on the device only, so two deals are weighed
 // alike, a random one of equal chances (the mean and 1.22 standard deviations, of a Poisson law, to either side) and one that falls off as
-// 1 / j^2: 2.6% slower than the best shape of each (an exactly even deal in place of the random one 3.1%).
+// 1 / j^2: 2.6% slower than the best shape of each (an exactly even deal in place of the random one 3.1%).  That holds for those two laws.
+// 23 sizes (4, 8 and 28 groups, 16 to 16384 rows) of other deals: 1 / j 3.5% on average and 20% at worst, half of the rows in no group 7 and
+// 52%, all rows in one group 21 and 123% (8 groups of 4096 -> 4096, 128 rows: 21 us against 9.5, since the tile is chosen for
+// eight matrices), and of single deals of the two laws 4.6 and 32%, 1.9 and 14%.
 struct I8Shape {
     int rows, cols, per_cu;
     bool wave;              // gemm_i8_wave_kernel
@@ -940,6 +949,7 @@ static GemmI8Args i8_args(const int8_t* q, const float* q_scale, const int8_t* W
                           int T, int d_in, int d_out, int N, void* out) {
     // The last cache holds 256 MB: from three such matrices in turn on none is still there.  Three in turn, 128 x 128 tiles, requested as kept and
     // as read once, us: 67 MB 14.3 and 15.9, 84 MB 19.5 and 22.0, 101 MB 23.9 and 24.0, 117 MB 26.9 and 25.1, 134 MB 29.0 and 25.4.
+    // All N matrices count, also where the rows are in few of them: which have rows is known on the device only.
     const int past_caches = (int64_t)N * d_out * d_in >= 100000000;
     return {q, q_scale, W, w_scale, offsets, out, T, d_in, d_out, N, 0, 0, 0, 0, past_caches};
 }

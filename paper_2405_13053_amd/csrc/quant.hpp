@@ -50,7 +50,8 @@ __device__ __forceinline__ Divisor divisor(float a) {
 __device__ __forceinline__ uint32_t whole_bits(float t) { return __float_as_uint(t + 12582912.f); }
 
 // bf16: x = m 2^e and a = n 2^f of 8-bit m, n make 127 x / a a half exactly or leave it 1 / (254 m) > 2^-16 of itself away from one.
-// x * by is within 2^-23 of it, so with 17 bits kept, 2^-18 at most moved, halves are halves and nothing else is or crosses one.
+// x * by is within 2^-23 of it, so with 17 bits kept, 2^-17 at most moved (2^-17 + 2^-23 < 2^-16), halves are halves and nothing else is or
+// crosses one.
 __device__ __forceinline__ uint32_t quantize1(bf16_t, float x, const Divisor& d) {
     const uint32_t t = __float_as_uint(x * d.by);
     return whole_bits(__uint_as_float((t + 0x40u) & 0xffffff80u));

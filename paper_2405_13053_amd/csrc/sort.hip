@@ -534,8 +534,9 @@ hipError_t launch_unsort_backward(const void* dy, const void* ys, int64_t rows, 
                                                                                                (u32x4*)dys, dw);
         return hipGetLastError();
     };
-    // 256 threads to a row and 1024, top-2: 64 x 4096 7.5 and 6.8 us, 64 x 14336 14.4 and 9.3, 512 x 4096 10.0 and 10.1, 512 x 14336 25.8
-    // and 18.2, 1024 x 4096 12.3 and 16.9; top-8 300 x 5120 24.6 and 15.9
+    // 256 threads to a row and 1024, us, top-2: 64 x 4096 7.4 and 6.4, 64 x 14336 14.8 and 9.0, 512 x 4096 12.0 and 10.4, 512 x 14336 25.4 and
+    // 19.3, 640 x 4096 13.1 and 16.1, 640 x 8192 19.9 and 20.6, 520 x 14336 25.8 and 24.7, 768 x 14336 31.6 and 31.2, 1024 x 14336 36.0 and
+    // 37.0; top-8 300 x 5120 36.2 and 21.4, 640 x 5120 43.7 and 38.0, 640 x 14336 99.7 and 81.6: the border is that of top-2
     if (a.row16 >= 512 && T <= 512) {
         a.lanes_log2 = 10;
         return bf16 ? go(&unsort_backward_kernel<bf16_t, 1024>, 1024) : go(&unsort_backward_kernel<float, 1024>, 1024);
