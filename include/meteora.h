@@ -365,10 +365,10 @@ meteora_status meteora_quantize_rows(const void* x /*[rows,d]*/, int rows, int d
  *                    Offsets must lie in [0, T] and not fall; whatever they hold, only rows in [0, T) are read and written.
  * Integer weights are frozen: there is no gradient for W.  The gradient with respect to the rows that were quantised (the rounding passed
  * by) is dx[t,i] = sum_c dy[t,c] * w_scale[e,c] * W[e,c,i], whose scales lie along the sum: no call of this entry point computes it.  In
- * bf16 it is meteora_base_gemm of dy on the matrix V[i,c] = w_scale[e,c] * W[e,c,i].  In 8 bits it is approximated by this entry point on
+ * bf16 it is meteora_base_gemm of a group's dy on the matrix V[i,c] = w_scale[e,c] * W[e,c,i].  In 8 bits it is approximated by this entry point on
  * dy and V quantised anew, each with a rounding of its own: with a = max_c |dy[t,c]| and b = max_c |V[i,c]| off by up to
  *   sum_c (|V[i,c]| * a + |dy[t,c]| * b + a * b / 254) / 254
- * before the output's rounding.
+ * before the roundings of fp32 and of the output.
  * Limits: d_in % 16 == 0, d_in <= 131056, d_out % 8 == 0, d_out <= 2^20, N <= 64, T < 2^24, T * d_out < 2^33.
  */
 meteora_status meteora_gemm_i8(const int8_t* q /*[T,d_in]*/, const float* q_scale /*[T]*/, const int8_t* W /*[N,d_out,d_in]*/,
@@ -379,7 +379,7 @@ meteora_status meteora_gemm_i8(const int8_t* q /*[T,d_in]*/, const float* q_scal
  * The kernel that meteora_gemm_i8 starts for these sizes, for tests that mean to reach every one.  Host only, no HIP call.  grouped:
  * offsets are given.  The host pointers (each may be NULL) receive its name (a static string: "one" for up to 128 inputs, "wave" for few
  * rows, "ring" for many), the rows and columns of its tiles, the workgroups that share a CU, whether the weights of a group with a
- * single row tile are requested as read once, and whether a second launch takes the tiles of a last, nearly empty round.  Returns 0, or -1
+ * single row tile are requested as read once, and whether a second launch may take the tiles of a last, nearly empty round.  Returns 0, or -1
  * for arguments outside the limits of meteora_gemm_i8 and for T == 0.
  */
 int meteora_gemm_i8_kernel(int T, int d_in, int d_out, int N, int grouped, const char** name /*host*/, int* tile_rows /*host*/,
