@@ -397,6 +397,66 @@ meteora_status meteora_base_gemm_i8(const void* x /*[T,d_in]*/, const int8_t* W 
                                     size_t ws_bytes, meteora_stream stream);
 
 /*
+ * Rows as 4-bit values with a power of two for every 32 consecutive inputs (a block): the tokens of an activation, or the output
+ * channels of a weight W[d_out, d_in].  A code c stands for (-1)^(c >> 3) times 0, 0.5, 1, 1.5, 2, 3, 4, 6 (by c & 7; E2M1), a scale byte E
+ * for 2^(E - 127), 255 for NaN (E8M0).  With a = max |x[t,i]| over a block:
+ *   E = max(0, floor(log2 a) - 2 + 127),   q[t,i] = the value nearest to x[t,i] * 2^(127 - E), ties to the even code, at most 6,
+ * the sign kept.  A block of zeros has E = 0.  A block that holds an infinity or a NaN is zeros with E = 255: products of its row are NaN,
+ * all others what they are.
+ *   q[rows, d/2]   input 2j of a row in the low, 2j + 1 in the high half of byte j
+ *   scale          meteora_mx4_scale_bytes(rows, d) = ceil(d/512) * rows * 16 bytes: block b of row t has its byte at
+ *                  [b / 16][t][(b % 4) * 4 + b % 16 / 4]; bytes of no block are zeros (quantising writes them; the products count on it)
+ * meteora_dequantize_mx4 gives the values back, out[rows, d], or out[d, rows] with transpose (rows % 8 == 0 then).  They are exact in
+ * fp32 and bf16 but for those of 2^128 and more, which are infinite, and in bf16 those below 2^-133, of which there are none in a
+ * block that was quantised.
+ * Limits: d % 32 == 0, d <= 131072, rows < 2^24, rows * d < 2^36 (0 from meteora_mx4_scale_bytes outside).  x, out in dt.
+ */
+size_t meteora_mx4_scale_bytes(int rows, int d);
+
+meteora_status meteora_quantize_mx4(const void* x /*[rows,d]*/, int rows, int d, meteora_dtype dt, uint8_t* q /*[rows,d/2]*/,
+                                    uint8_t* scale, meteora_stream stream);
+
+meteora_status meteora_dequantize_mx4(const uint8_t* q /*[rows,d/2]*/, const uint8_t* scale, int rows, int d, meteora_dtype dt,
+                                      int transpose, void* out /*[rows,d] or [d,rows]*/, meteora_stream stream);
+
+/*
+ * Product of such rows and such weights, over groups of consecutive rows:
+ *   out[t,c] = sum_i V(q[t,i]) * V(W[e,c,i]),   e = the group with offsets[e] <= t < offsets[e+1],   V: the values stood for
+ * Products of two values are exact, sums fp32 in an order that depends on the sizes, one rounding where dt (the type of out) is
+ * METEORA_BF16.  offsets, N, groups and rows of no group as in meteora_gemm_i8.  w_scale: the N matrices' scales one behind the other, each
+ * meteora_mx4_scale_bytes(d_out, d_in); q_scale: meteora_mx4_scale_bytes(T, d_in).
+ * Limits: those of the rows for both operands, d_out % 8 == 0, d_out <= 2^20, N <= 64, T * d_out < 2^33.
+ *
+ * meteora_gemm_mx4_kernel: the kernel that these sizes lead to, as meteora_gemm_i8_kernel ("one" for up to 256 inputs).
+ */
+meteora_status meteora_gemm_mx4(const uint8_t* q /*[T,d_in/2]*/, const uint8_t* q_scale, const uint8_t* W /*[N,d_out,d_in/2]*/,
+                                const uint8_t* w_scale, const int32_t* offsets /*[N+1] or NULL*/, int T, int d_in, int d_out, int N,
+                                meteora_dtype dt, void* out /*[T,d_out]*/, meteora_stream stream);
+
+int meteora_gemm_mx4_kernel(int T, int d_in, int d_out, int N, int grouped, const char** name /*host*/, int* tile_rows /*host*/,
+                            int* tile_cols /*host*/, int* per_cu /*host*/, int* read_once /*host*/, int* tail /*host*/);
+
+/*
+ * Base projection with the weight in 4 bits: meteora_quantize_mx4 of x, then meteora_gemm_mx4 with one group.  x and out in dt.
+ * ws: meteora_base_gemm_mx4_workspace_bytes(T, d_in) bytes, which also holds any smaller T; 0 outside the limits.
+ *
+ * meteora_base_gemm_mx4_backward: its gradient with respect to x, the rounding of x passed by (the weight is frozen and has none):
+ *   dx[t,i] = sum_c dy[t,c] * V(W[c,i])
+ * dy and dx in dt, dy as it is (not quantised), fp32 sums, one rounding.  The weight's values are laid out transposed in ws, in dt, on
+ * every call: meteora_base_gemm_mx4_backward_workspace_bytes(d_in, d_out, dt), whatever T.
+ */
+size_t meteora_base_gemm_mx4_workspace_bytes(int T, int d_in);
+
+meteora_status meteora_base_gemm_mx4(const void* x /*[T,d_in]*/, const uint8_t* W /*[d_out,d_in/2]*/, const uint8_t* w_scale, int T, int d_in,
+                                     int d_out, meteora_dtype dt, void* out /*[T,d_out]*/, void* ws, size_t ws_bytes, meteora_stream stream);
+
+size_t meteora_base_gemm_mx4_backward_workspace_bytes(int d_in, int d_out, meteora_dtype dt);
+
+meteora_status meteora_base_gemm_mx4_backward(const void* dy /*[T,d_out]*/, const uint8_t* W /*[d_out,d_in/2]*/, const uint8_t* w_scale, int T,
+                                              int d_in, int d_out, meteora_dtype dt, void* dx /*[T,d_in]*/, void* ws, size_t ws_bytes,
+                                              meteora_stream stream);
+
+/*
  * Rows next to each other by adapter (the X_i of Sec. 3.3 as rows that are moved; meteora_bucket_tokens lists them):
  *   pos[t,j]   the place of pair (t, j) among all pairs whose topk_idx lies in [0, N), by adapter, then token, then slot;
  *              -1 for other ids (padding tokens, say with -1), which go nowhere

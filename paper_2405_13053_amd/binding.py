@@ -94,6 +94,24 @@ def load_library():
     lib.meteora_base_gemm_i8_workspace_bytes.argtypes = [i, i]
     lib.meteora_base_gemm_i8.restype = i
     lib.meteora_base_gemm_i8.argtypes = [vp, vp, vp, i, i, i, i, vp, vp, sz, vp]
+    lib.meteora_mx4_scale_bytes.restype = sz
+    lib.meteora_mx4_scale_bytes.argtypes = [i, i]
+    lib.meteora_quantize_mx4.restype = i
+    lib.meteora_quantize_mx4.argtypes = [vp, i, i, i, vp, vp, vp]
+    lib.meteora_dequantize_mx4.restype = i
+    lib.meteora_dequantize_mx4.argtypes = [vp, vp, i, i, i, i, vp, vp]
+    lib.meteora_gemm_mx4.restype = i
+    lib.meteora_gemm_mx4.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, i, vp, vp]
+    lib.meteora_gemm_mx4_kernel.restype = i
+    lib.meteora_gemm_mx4_kernel.argtypes = [i, i, i, i, i, vp, vp, vp, vp, vp, vp]
+    lib.meteora_base_gemm_mx4_workspace_bytes.restype = sz
+    lib.meteora_base_gemm_mx4_workspace_bytes.argtypes = [i, i]
+    lib.meteora_base_gemm_mx4.restype = i
+    lib.meteora_base_gemm_mx4.argtypes = [vp, vp, vp, i, i, i, i, vp, vp, sz, vp]
+    lib.meteora_base_gemm_mx4_backward_workspace_bytes.restype = sz
+    lib.meteora_base_gemm_mx4_backward_workspace_bytes.argtypes = [i, i, i]
+    lib.meteora_base_gemm_mx4_backward.restype = i
+    lib.meteora_base_gemm_mx4_backward.argtypes = [vp, vp, vp, i, i, i, i, vp, vp, sz, vp]
     lib.meteora_sort_workspace_bytes.restype = sz
     lib.meteora_sort_workspace_bytes.argtypes = [i, i, i]
     lib.meteora_sort_tokens.restype = i
@@ -583,6 +601,134 @@ def base_gemm_i8(x, W, w_scale, out: Optional[torch.Tensor] = None, ws: Optional
                                              _stream())
     if st != 0:
         raise MeteoraError(st, "meteora_base_gemm_i8")
+    return out
+
+
+def mx4_scale_shape(rows: int, d: int):
+    """Shape of the scales of rows in 4 bits: (ceil(d / 512), rows, 16)."""
+    return ((d + 511) // 512, rows, 16)
+
+
+def quantize_mx4(x, out=None):
+    """meteora_quantize_mx4: (q[rows,d/2] uint8, scale[ceil(d/512),rows,16] uint8), the rows of x as 4-bit values with a power of two
+    for every 32 inputs.  `out` = the two result tensors if the caller has them already."""
+    rows, d = x.shape
+    _chk(x, "x")
+    if out is None:
+        out = (torch.empty((rows, d // 2), dtype=torch.uint8, device=x.device),
+               torch.empty(mx4_scale_shape(rows, d), dtype=torch.uint8, device=x.device))
+    q, scale = out
+    _chk(q, "q", torch.uint8, (rows, d // 2)); _chk(scale, "scale", torch.uint8, mx4_scale_shape(rows, d))
+    _chk_device(x, q, scale)
+    st = load_library().meteora_quantize_mx4(_pe(x), rows, d, _dt(x), _pe(q), _pe(scale), _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_quantize_mx4")
+    return q, scale
+
+
+def dequantize_mx4(q, scale, transpose: bool = False, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16):
+    """meteora_dequantize_mx4: the values of rows in 4 bits, out[rows,d], or out[d,rows] with `transpose`.  `dtype`: of the output, if
+    there is no `out`."""
+    rows, d = q.shape[0], q.shape[1] * 2
+    shape = (d, rows) if transpose else (rows, d)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+    _chk(q, "q", torch.uint8); _chk(scale, "scale", torch.uint8, mx4_scale_shape(rows, d)); _chk(out, "out", None, shape)
+    _chk_device(q, scale, out)
+    st = load_library().meteora_dequantize_mx4(_pe(q), _pe(scale), rows, d, _dt(out), int(transpose), _pe(out), _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_dequantize_mx4")
+    return out
+
+
+def gemm_mx4(q, q_scale, W, w_scale, offsets=None, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16):
+    """meteora_gemm_mx4: out[t,c] = sum_i of the values of q[t,i] and W[e,c,i].  W[d_out,d_in/2] and w_scale as quantize_mx4 gives them
+    without offsets, with offsets[N+1] the same for every group: W[N,d_out,d_in/2], w_scale[N,ceil(d_in/512),d_out,16].  `dtype`: of the
+    output, if there is no `out`."""
+    T, half = q.shape
+    d_in = half * 2
+    if W.dim() != (2 if offsets is None else 3):
+        raise ValueError("a W of one matrix per group needs offsets, a single matrix none")
+    d_out = W.shape[-2]
+    N = 1 if offsets is None else W.shape[0]
+    if out is None:
+        out = torch.empty((T, d_out), dtype=dtype, device=q.device)
+    lead = () if offsets is None else (N,)
+    chunks = (d_in + 511) // 512
+    # written out, as in linear_forward
+    if not (q.dtype == torch.uint8 and W.dtype == torch.uint8 and q_scale.dtype == torch.uint8 and w_scale.dtype == torch.uint8 and
+            q_scale.shape == (chunks, T, 16) and W.shape[-1] == half and w_scale.shape == (*lead, chunks, d_out, 16) and
+            out.shape == (T, d_out) and q.is_cuda and q.is_contiguous() and q_scale.is_contiguous() and W.is_contiguous() and
+            w_scale.is_contiguous() and out.is_contiguous()):
+        _chk(q, "q", torch.uint8); _chk(q_scale, "q_scale", torch.uint8, (chunks, T, 16))
+        _chk(W, "W", torch.uint8, (*lead, d_out, half)); _chk(w_scale, "w_scale", torch.uint8, (*lead, chunks, d_out, 16))
+        _chk(out, "out", None, (T, d_out))
+    _chk(offsets, "offsets", torch.int32, (N + 1,))
+    _chk_device(q, q_scale, W, w_scale, offsets, out)
+    st = load_library().meteora_gemm_mx4(_pe(q), _pe(q_scale), _p(W), _p(w_scale), _p(offsets), T, d_in, d_out, N, _dt(out), _pe(out),
+                                         _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_gemm_mx4")
+    return out
+
+
+def gemm_mx4_kernel(T: int, d_in: int, d_out: int, N: Optional[int] = None):
+    """meteora_gemm_mx4_kernel: (name, tile_rows, tile_cols, per_cu, read_once, tail) of the kernel that gemm_mx4 starts, for N groups or
+    for none; None outside the limits."""
+    name, ints = ctypes.c_char_p(), [ctypes.c_int() for _ in range(5)]
+    if load_library().meteora_gemm_mx4_kernel(T, d_in, d_out, 1 if N is None else N, int(N is not None), ctypes.byref(name),
+                                              *(ctypes.byref(v) for v in ints)) != 0:
+        return None
+    rows, cols, per_cu, once, tail = (v.value for v in ints)
+    return name.value.decode(), rows, cols, per_cu, bool(once), bool(tail)
+
+
+def base_gemm_mx4_workspace_bytes(T, d_in) -> int:
+    return int(load_library().meteora_base_gemm_mx4_workspace_bytes(T, d_in))
+
+
+def base_gemm_mx4(x, W, w_scale, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """meteora_base_gemm_mx4: out = x W^T with W[d_out,d_in/2], w_scale (quantize_mx4 of the weight), the rows of x quantised on the way."""
+    T, d_in = x.shape
+    d_out = W.shape[0]
+    dev, dtype = x.device, x.dtype
+    if out is None:
+        _chk(x, "x")
+        out = torch.empty((T, d_out), dtype=dtype, device=dev)
+    # written out, as in linear_forward
+    if not (W.dtype == torch.uint8 and w_scale.dtype == torch.uint8 and out.dtype == dtype and W.shape == (d_out, d_in // 2) and
+            w_scale.shape == ((d_in + 511) // 512, d_out, 16) and out.shape == (T, d_out) and x.is_cuda and x.is_contiguous() and
+            W.is_contiguous() and w_scale.is_contiguous() and out.is_contiguous()):
+        _chk(x, "x"); _chk(W, "W", torch.uint8, (d_out, d_in // 2)); _chk(w_scale, "w_scale", torch.uint8, mx4_scale_shape(d_out, d_in))
+        _chk(out, "out", dtype, (T, d_out))
+    _chk(ws, "ws", torch.uint8)
+    ws = _ws(ws, lambda: base_gemm_mx4_workspace_bytes(T, d_in), dev)
+    _chk_device(x, W, w_scale, out, ws)
+    st = load_library().meteora_base_gemm_mx4(_pe(x), _p(W), _p(w_scale), T, d_in, d_out, _dt(x), _pe(out), _p(ws), ws.numel(), _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_base_gemm_mx4")
+    return out
+
+
+def base_gemm_mx4_backward_workspace_bytes(d_in, d_out, dtype) -> int:
+    dt = BF16 if dtype in (torch.bfloat16, BF16, "bf16") else F32
+    return int(load_library().meteora_base_gemm_mx4_backward_workspace_bytes(d_in, d_out, dt))
+
+
+def base_gemm_mx4_backward(dy, W, w_scale, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """meteora_base_gemm_mx4_backward: dx[T,d_in] = dy W, the gradient of base_gemm_mx4 with respect to x (its rounding passed by)."""
+    T, d_out = dy.shape
+    d_in = W.shape[1] * 2
+    _chk(dy, "dy"); _chk(W, "W", torch.uint8, (d_out, d_in // 2)); _chk(w_scale, "w_scale", torch.uint8, mx4_scale_shape(d_out, d_in))
+    if out is None:
+        out = torch.empty((T, d_in), dtype=dy.dtype, device=dy.device)
+    _chk(out, "out", dy.dtype, (T, d_in)); _chk(ws, "ws", torch.uint8)
+    ws = _ws(ws, lambda: base_gemm_mx4_backward_workspace_bytes(d_in, d_out, dy.dtype), dy.device)
+    _chk_device(dy, W, w_scale, out, ws)
+    st = load_library().meteora_base_gemm_mx4_backward(_pe(dy), _p(W), _p(w_scale), T, d_in, d_out, _dt(dy), _pe(out), _p(ws), ws.numel(),
+                                                       _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_base_gemm_mx4_backward")
     return out
 
 

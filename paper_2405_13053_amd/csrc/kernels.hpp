@@ -19,6 +19,7 @@ hipError_t shrink_init_kernels();
 hipError_t gate_bwd_init_kernels();
 hipError_t bucket_init_scratch();
 hipError_t gemm_i8_init_kernels();
+hipError_t gemm_mx4_init_kernels();
 
 // ---- weight repacking, one launch: W_gate -> split bf16 fragments (bf16 gate), A -> MFMA fragments,
 // stacked B -> its transpose Bt[d_out, N*r rounded up to 64] (zero-padded) for the GEMM's K-extension.
@@ -240,6 +241,14 @@ I8Plan gemm_i8_plan(int T, int d_in, int d_out, int N, bool grouped);
 bool base_gemm_i8_in_one(int T, int d_in);
 hipError_t launch_base_gemm_i8_in_one(const void* x, const int8_t* W, const float* w_scale, int T, int d_in, int d_out, bool bf16,
                                       void* out, hipStream_t stream);
+
+// ---- 4-bit products (quant_mx4.hpp has the format): d, d_in % 32 == 0, d_out % 8 == 0; groups as above.  turned: out[d, rows].
+hipError_t launch_quantize_mx4(const void* x, int rows, int d, bool bf16, uint8_t* q, uint8_t* scale, hipStream_t stream);
+hipError_t launch_dequantize_mx4(const uint8_t* q, const uint8_t* scale, int rows, int d, bool turned, bool bf16, void* out,
+                                 hipStream_t stream);
+hipError_t launch_gemm_mx4(const uint8_t* q, const uint8_t* q_scale, const uint8_t* W, const uint8_t* w_scale, const int32_t* offsets,
+                           int T, int d_in, int d_out, int N, bool bf16, void* out, hipStream_t stream);
+I8Plan gemm_mx4_plan(int T, int d_in, int d_out, int N, bool grouped);
 
 // ---- rows sorted by adapter: pos[T,k], offsets[N+1], xs[pos[t,j]] = x[t] (with xs_scale: as 8-bit whole numbers), and back
 // (rows: those of ys; base, w, dw may be nullptr).  chunk_counts: sort_count_bytes, whatever T.

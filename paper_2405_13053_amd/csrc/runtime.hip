@@ -52,6 +52,8 @@ hipError_t init_kernels() {
     if (e != hipSuccess) return e;
     e = gemm_i8_init_kernels();
     if (e != hipSuccess) return e;
+    e = gemm_mx4_init_kernels();
+    if (e != hipSuccess) return e;
     return bucket_init_scratch();
 }
 
