@@ -499,6 +499,39 @@ meteora_status meteora_unsort_backward(const void* dy /*[T,d]*/, const void* ys 
                                        meteora_stream stream);
 
 /*
+ * Gated MLPs of experts for a few tokens (T <= 64: a decode step, drafted tokens), routing given:
+ *   h[t,j] = silu(W1[e, 0:f] x[t]) * (W1[e, f:2f] x[t]),   e = topk_idx[t,j],   silu(g) = g / (1 + exp(-g))
+ *   out[t] = base[t] + scale * sum_j topk_w[t,j] * (W2[e] h[t,j])
+ * Ids outside [0, N) (padding tokens, say with -1) give nothing: such a token is base[t], or zeros.  An id may stand twice in a token's
+ * row.  base == NULL: zeros; base may be out itself.  x, base, out in dt, which must be METEORA_BF16.  Weights:
+ *   w1_scale == w2_scale == NULL:  W1[N,2f,d] and W2[N,d,f] in dt
+ *   otherwise                      in 4 bits as meteora_quantize_mx4 gives them, a matrix behind the other: W1 [N,2f,d/2] with N times
+ *                                  meteora_mx4_scale_bytes(2f, d), W2 [N,d,f/2] with N times meteora_mx4_scale_bytes(d, f).  Their values
+ *                                  enter the products as bf16, exactly; x is not quantised.
+ * fp32 sums; h is rounded to bf16, as the operand of the second product, and out once.  The weights of the experts in use are read once (where
+ * more than 16 or 32 tokens share an expert, again from the caches).  Without tokens nothing is launched.
+ * Limits: T <= 64, N <= 64, k <= 8, d % 8 == 0, f % 8 == 0 (in 4 bits % 32), d, f <= 131072.
+ * ws: meteora_experts_workspace_bytes(T, d, f, N, k) bytes, which also holds any smaller T; 0 outside the limits.
+ *
+ * meteora_moe_forward: the same behind its gate, as meteora_gate_topk routes (k <= N; the logits' sums in an order of their own, so that
+ * two that are equal to fp32 accuracy may rank the other way there).  topk_idx_out / topk_w_out receive the routing if they are not NULL.
+ * These two have no gradients.
+ */
+size_t meteora_experts_workspace_bytes(int T, int d, int f, int N, int k);
+
+meteora_status meteora_experts_forward(const void* x /*[T,d]*/, const int32_t* topk_idx /*[T,k]*/, const float* topk_w /*[T,k]*/,
+                                       const void* W1, const uint8_t* w1_scale /*or NULL*/, const void* W2,
+                                       const uint8_t* w2_scale /*or NULL*/, int T, int d, int f, int N, int k, float scale, meteora_dtype dt,
+                                       const void* base /*[T,d] or NULL*/, void* out /*[T,d]*/, void* ws, size_t ws_bytes,
+                                       meteora_stream stream);
+
+meteora_status meteora_moe_forward(const void* x /*[T,d]*/, const float* W_gate /*[d,N]*/, const float* gate_bias /*[N] or NULL*/,
+                                   const void* W1, const uint8_t* w1_scale /*or NULL*/, const void* W2, const uint8_t* w2_scale /*or NULL*/,
+                                   int T, int d, int f, int N, int k, float scale, float inv_temperature, meteora_dtype dt,
+                                   const void* base /*[T,d] or NULL*/, void* out /*[T,d]*/, int32_t* topk_idx_out /*[T,k] or NULL*/,
+                                   float* topk_w_out /*[T,k] or NULL*/, void* ws, size_t ws_bytes, meteora_stream stream);
+
+/*
  * Optional per-stage timing, for benchmarks.  Host only; off by default.
  * While enabled, meteora_lora_forward and meteora_linear_forward record
  * hipEvents on `stream` around each stage (prep, gate_logits, gate_topk,

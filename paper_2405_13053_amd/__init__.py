@@ -10,5 +10,6 @@ from .binding import (MeteoraError, base_gemm, bucket_tokens, bucket_tokens_noal
                       base_gemm_i8, base_gemm_i8_workspace_bytes, gemm_i8, gemm_i8_kernel, quantize_rows, sort_tokens, sort_workspace_bytes,
                       unsort_backward, unsort_tokens,
                       base_gemm_mx4, base_gemm_mx4_backward, base_gemm_mx4_backward_workspace_bytes, base_gemm_mx4_workspace_bytes,
+                      experts_forward, experts_workspace_bytes, moe_forward,
                       dequantize_mx4, gemm_mx4, gemm_mx4_kernel, mx4_scale_shape, quantize_mx4,
                       BMM_GATHER, LOOP_ORIGINAL, variant_forward, variant_workspace_bytes)

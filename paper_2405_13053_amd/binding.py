@@ -112,6 +112,12 @@ def load_library():
     lib.meteora_base_gemm_mx4_backward_workspace_bytes.argtypes = [i, i, i]
     lib.meteora_base_gemm_mx4_backward.restype = i
     lib.meteora_base_gemm_mx4_backward.argtypes = [vp, vp, vp, i, i, i, i, vp, vp, sz, vp]
+    lib.meteora_experts_workspace_bytes.restype = sz
+    lib.meteora_experts_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.meteora_experts_forward.restype = i
+    lib.meteora_experts_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, f, i, vp, vp, vp, sz, vp]
+    lib.meteora_moe_forward.restype = i
+    lib.meteora_moe_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, f, f, i, vp, vp, vp, vp, vp, sz, vp]
     lib.meteora_sort_workspace_bytes.restype = sz
     lib.meteora_sort_workspace_bytes.argtypes = [i, i, i]
     lib.meteora_sort_tokens.restype = i
@@ -730,6 +736,75 @@ def base_gemm_mx4_backward(dy, W, w_scale, out: Optional[torch.Tensor] = None, w
     if st != 0:
         raise MeteoraError(st, "meteora_base_gemm_mx4_backward")
     return out
+
+
+def experts_workspace_bytes(T, d, f, N, k) -> int:
+    return int(load_library().meteora_experts_workspace_bytes(T, d, f, N, k))
+
+
+def _chk_experts(x, W1, W2, w1_scale, w2_scale, base, out):
+    """Checks what experts_forward and moe_forward share; (d, f, N)."""
+    T, d = x.shape
+    N, d2, cols = W2.shape
+    mx4 = w1_scale is not None
+    f = cols * 2 if mx4 else cols
+    if (w1_scale is None) != (w2_scale is None):
+        raise ValueError("W1 and W2 are both in 4 bits, with scales, or neither")
+    # written out, as in linear_forward
+    if not (x.is_cuda and x.is_contiguous() and W1.is_contiguous() and W2.is_contiguous() and out.is_contiguous() and out.dtype == x.dtype and
+            out.shape == (T, d) and d2 == d and W1.shape == (N, 2 * f, d // 2 if mx4 else d) and
+            W1.dtype == W2.dtype == (torch.uint8 if mx4 else x.dtype) and
+            (base is None or (base.dtype == x.dtype and base.shape == (T, d) and base.is_contiguous()))):
+        wt = torch.uint8 if mx4 else x.dtype
+        _chk(x, "x"); _chk(W1, "W1", wt, (N, 2 * f, d // 2 if mx4 else d)); _chk(W2, "W2", wt, (N, d, cols))
+        _chk(base, "base", x.dtype, (T, d)); _chk(out, "out", x.dtype, (T, d))
+    if mx4:
+        _chk(w1_scale, "w1_scale", torch.uint8, (N, *mx4_scale_shape(2 * f, d)))
+        _chk(w2_scale, "w2_scale", torch.uint8, (N, *mx4_scale_shape(d, f)))
+    return d, f, N
+
+
+def experts_forward(x, topk_idx, topk_w, W1, W2, w1_scale=None, w2_scale=None, scale: float = 1.0,
+                    base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """meteora_experts_forward: out[t] = base[t] + scale * sum_j topk_w[t,j] * MLP_e(x[t]), e = topk_idx[t,j], for up to 64 tokens.
+    W1[N,2f,d], W2[N,d,f] in x's dtype; with w1_scale, w2_scale in 4 bits, quantize_mx4 of every matrix: W1[N,2f,d/2], W2[N,d,f/2]."""
+    T, k = topk_idx.shape
+    if out is None:
+        out = torch.empty_like(x)
+    d, f, N = _chk_experts(x, W1, W2, w1_scale, w2_scale, base, out)
+    _chk(topk_idx, "topk_idx", torch.int32, (x.shape[0], k)); _chk(topk_w, "topk_w", torch.float32, (x.shape[0], k)); _chk(ws, "ws", torch.uint8)
+    ws = _ws(ws, lambda: experts_workspace_bytes(T, d, f, N, k), x.device)
+    _chk_device(x, topk_idx, topk_w, W1, W2, w1_scale, w2_scale, base, out, ws)
+    st = load_library().meteora_experts_forward(_pe(x), _pe(topk_idx), _pe(topk_w), _p(W1), _p(w1_scale), _p(W2), _p(w2_scale), T, d, f, N, k,
+                                                float(scale), _dt(x), None if base is None else _pe(base), _pe(out), _p(ws), ws.numel(),
+                                                _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_experts_forward")
+    return out
+
+
+def moe_forward(x, W_gate, gate_bias, W1, W2, k: int, w1_scale=None, w2_scale=None, scale: float = 1.0, inv_temperature: float = 1.0,
+                base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                return_routing: bool = False):
+    """meteora_moe_forward: experts_forward behind its gate, W_gate[d,N] f32 and gate_bias[N] f32 or None; with `return_routing`
+    (out, topk_idx[T,k], topk_w[T,k])."""
+    T = x.shape[0]
+    if out is None:
+        out = torch.empty_like(x)
+    d, f, N = _chk_experts(x, W1, W2, w1_scale, w2_scale, base, out)
+    _chk(W_gate, "W_gate", torch.float32, (d, N)); _chk(gate_bias, "gate_bias", torch.float32, (N,)); _chk(ws, "ws", torch.uint8)
+    idx = w = None
+    if return_routing:
+        idx = torch.empty((T, k), dtype=torch.int32, device=x.device)
+        w = torch.empty((T, k), dtype=torch.float32, device=x.device)
+    ws = _ws(ws, lambda: experts_workspace_bytes(T, d, f, N, k), x.device)
+    _chk_device(x, W_gate, gate_bias, W1, W2, w1_scale, w2_scale, base, out, ws)
+    st = load_library().meteora_moe_forward(_pe(x), _p(W_gate), _p(gate_bias), _p(W1), _p(w1_scale), _p(W2), _p(w2_scale), T, d, f, N, k,
+                                            float(scale), float(inv_temperature), _dt(x), None if base is None else _pe(base), _pe(out),
+                                            None if idx is None else _pe(idx), None if w is None else _pe(w), _p(ws), ws.numel(), _stream())
+    if st != 0:
+        raise MeteoraError(st, "meteora_moe_forward")
+    return (out, idx, w) if return_routing else out
 
 
 def sort_workspace_bytes(T, k, N) -> int:

@@ -38,20 +38,6 @@ __device__ __forceinline__ void mfma16_mx4(f32x4& acc, const bf16x8& w, const bf
                      : "+a"(acc) : "v"(w), "v"(x), "v"(sw), "v"(sx));
 }
 
-// The scales of `rows` consecutive rows of an operand with `all` rows, a chunk at a time.  Rows past the last give 0, which stands for
-// 2^-127, and so does a chunk past the last.
-struct ScaleRows {
-    const uint8_t* first;
-    size_t step;          // bytes from chunk to chunk
-    int bytes, chunks;
-    __device__ __forceinline__ ScaleRows(const uint8_t* scale, int all, int row0, int rows, int row_bytes)
-        : first(scale + (size_t)row0 * 16), step((size_t)all * 16), bytes(rows * 16), chunks((row_bytes + 255) / 256) {}
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk(int c) const {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(first + (size_t)c * step), 0, c < chunks ? (uint32_t)bytes : 0u,
-                                                 0x00020000);
-    }
-};
-
 template <int TB, int RB, int WV, int D>
 constexpr int wave_mx4_lds() {
     constexpr int ring = WV * D * (TB + RB) * 2304, sums = WV * TB * RB * 1024;
@@ -81,10 +67,6 @@ __device__ __forceinline__ void wave_mx4_sums(const GemmMx4Args& a, const f32x4 
         const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
         store4((TO*)a.out + (size_t)(row0 + row) * a.d_out + n0 + col, v);
     }
-}
-
-__device__ __forceinline__ void mx4_scale_lds(__amdgpu_buffer_rsrc_t rsrc, unsigned char* dst, uint32_t voff) {   // a word to each lane
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)dst, 4, voff, 0, 0, 0);
 }
 
 // Few rows: TB x 16 rows of q, RB x 16 rows of W, WV wavefronts, each with every WV-th K tile of 256 inputs and a ring of its own of

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "common.hpp"
+
 namespace meteora {
 
 // ---- process state (runtime.hip): raise a kernel's dynamic-LDS limit once per device (thread-safe), and the
@@ -249,6 +251,27 @@ hipError_t launch_dequantize_mx4(const uint8_t* q, const uint8_t* scale, int row
 hipError_t launch_gemm_mx4(const uint8_t* q, const uint8_t* q_scale, const uint8_t* W, const uint8_t* w_scale, const int32_t* offsets,
                            int T, int d_in, int d_out, int N, bool bf16, void* out, hipStream_t stream);
 I8Plan gemm_mx4_plan(int T, int d_in, int d_out, int N, bool grouped);
+
+// ---- gated MLPs of experts for a few tokens (T <= kExpertsMaxTokens) and the gate in front of them
+constexpr int kExpertsMaxTokens = 64;
+struct ExpertsArgs {
+    const bf16_t* x;                     // [T, d]
+    const int32_t* idx;                  // [T, k]; ids outside [0, N): nothing
+    const float* w;                      // [T, k]
+    const uint8_t *W1, *s1, *W2, *s2;    // [N, 2f, d], [N, d, f]: bf16 (scales nullptr), or 4 bits (quant_mx4.hpp)
+    const bf16_t* base;                  // [T, d] or nullptr; may be out
+    bf16_t* out;                         // [T, d]
+    bf16_t* h;                           // scratch: experts_h_bytes, experts_y_bytes
+    float* y;
+    float scale;
+    int T, k, N, d, f;
+};
+size_t experts_h_bytes(int T, int k, int f);
+size_t experts_y_bytes(int T, int k, int d);
+hipError_t launch_experts(const ExpertsArgs& a, hipStream_t stream);
+hipError_t launch_gate_few(const void* x, const float* W_gate, const float* bias, int T, int d, int N, int k, float inv_temperature,
+                           int32_t* topk_idx, float* topk_w, hipStream_t stream);
+hipError_t experts_init_kernels();
 
 // ---- rows sorted by adapter: pos[T,k], offsets[N+1], xs[pos[t,j]] = x[t] (with xs_scale: as 8-bit whole numbers), and back
 // (rows: those of ys; base, w, dw may be nullptr).  chunk_counts: sort_count_bytes, whatever T.

@@ -79,4 +79,22 @@ __device__ __forceinline__ u32x4 mx4_bf16x8(uint32_t q, float s) {
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, s, 3))};
 }
 
+// The scales of `rows` consecutive rows of an operand with `all` rows, a chunk at a time.  Rows past the last give 0, which stands for
+// 2^-127, and so does a chunk past the last.
+struct ScaleRows {
+    const uint8_t* first;
+    size_t step;          // bytes from chunk to chunk
+    int bytes, chunks;
+    __device__ __forceinline__ ScaleRows(const uint8_t* scale, int all, int row0, int rows, int row_bytes)
+        : first(scale + (size_t)row0 * 16), step((size_t)all * 16), bytes(rows * 16), chunks((row_bytes + 255) / 256) {}
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t chunk(int c) const {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(first + (size_t)c * step), 0, c < chunks ? (uint32_t)bytes : 0u,
+                                                 0x00020000);
+    }
+};
+
+__device__ __forceinline__ void mx4_scale_lds(__amdgpu_buffer_rsrc_t rsrc, unsigned char* dst, uint32_t voff) {   // a word to each lane
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)dst, 4, voff, 0, 0, 0);
+}
+
 }  // namespace meteora
