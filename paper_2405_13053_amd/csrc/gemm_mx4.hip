@@ -180,11 +180,15 @@ __global__ __launch_bounds__(WV * 64) void gemm_mx4_wave_kernel(const GemmMx4Arg
 
 
 // Many rows: the schedule of gemm_i8_ring_kernel.  The instruction is in assembly with its accumulator tied, with the same care
-// (tests/test_mfma_waits_mx4_host.py reads the compiled code).  The rings take all of LDS with 256 x 256 tiles, so the scales are words in
-// registers, MB + NB a lane for two K tiles, loaded ahead; the second tile's are shifted down.
+// (tests/test_mfma_waits_mx4_host.py reads the compiled code).  Scales: with rings of two slots, which take all of LDS with 256 x 256 tiles, words in
+// registers, MB + NB a lane for two K tiles, loaded a tile and a half ahead; the second tile's are shifted down.  Loads complete in order, so in
+// deeper rings those words would wait for every K tile requested before them; there the scales are part of the slots, 16 bytes a row
+// (those of two K tiles, in either's slot), 64 rows a load instruction.
+template <int BLOCKS, int D>
+constexpr int mx4_slot_bytes() { return BLOCKS * 32 * kI8Tile + (D > 2 ? ceil_div(BLOCKS, 2) * 1024 : 0); }
 template <int MB, int NB, int D>
 constexpr int ring_mx4_lds() {
-    constexpr int ring = (D * MB + (D + 1) * NB) * 32 * kI8Tile, stage = 4 * 32 * (NB * 64 + 16);
+    constexpr int ring = D * mx4_slot_bytes<MB, D>() + (D + 1) * mx4_slot_bytes<NB, D>(), stage = 4 * 32 * (NB * 64 + 16);
     return ring > stage ? ring : stage;
 }
 
@@ -235,12 +239,14 @@ __device__ __forceinline__ void ring_mx4_epilogue(const GemmMx4Args& a, f32x4 (&
 template <typename TO, int MB, int NB, int D, bool PART, bool ONCE>
 __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned char* smem, int e, int row0, int rows, int n0) {
     constexpr int BM = MB * 32, BN = NB * 32, PX = MB, PW = NB;   // 2 x 2 wavefronts; load instructions per wavefront and tile
-    static_assert((NB % 2 == 0 || MB % 2 == 0) && D >= 2 && D <= 5 && (D - 1) * (PX + PW) < 64, "2 x 2 micro-blocks; vmcnt");
-    constexpr int NR = MB + NB, NM = MB * NB;   // fragment reads and MFMAs per k-step of 64
+    constexpr bool SLOTS = D > 2;                                 // scales in the slots
+    constexpr int GX = ceil_div(BM, 64), GW = ceil_div(BN, 64), PS = SLOTS ? ceil_div(GX + GW, 4) : 0, P = PX + PW + PS;
+    static_assert((NB % 2 == 0 || MB % 2 == 0) && D >= 2 && D <= 5 && (D - 1) * P < 64, "2 x 2 micro-blocks; vmcnt");
+    constexpr int NR = MB + NB, NM = MB * NB;   // fragment reads and MFMAs per k-step of 128
     constexpr int RA = NM * 3 / 4 / NR > 0 ? NM * 3 / 4 / NR : 1, RB = NM / NR;   // MFMAs per read, see the bf16 kernel
     static_assert(RB >= 1, "a k-step needs one MFMA per fragment read");
     bf16_t* ring = reinterpret_cast<bf16_t*>(smem);
-    constexpr int kXElems = BM * kGemmBK, kWElems = BN * kGemmBK;   // in units of two bytes, as everything that is shared
+    constexpr int kXElems = mx4_slot_bytes<MB, D>() / 2, kWElems = mx4_slot_bytes<NB, D>() / 2;   // of two bytes, as everything that is shared
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -255,8 +261,7 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
     const PartTile part = part_tile(a.d_in / 2, wave, lane);
     const uint32_t x_bytes = (uint32_t)rows * (uint32_t)a.d_in, w_bytes = (uint32_t)cols * (uint32_t)a.d_in;
 
-    // Scales: words of the chunk of two K tiles that is multiplied, of which the lower half is the current one's, and of the next chunk,
-    // requested a tile and a half ahead
+    // Scales: the low half of a word is the tile's that is multiplied; next: of the chunk of two tiles behind it, or of the tile
     const ScaleRows xsc(a.q_scale, a.T, row0, rows, a.d_in);
     const ScaleRows wsc(a.w_scale + (size_t)e * mx4_scale_bytes(a.d_out, a.d_in * 2), a.d_out, n0, cols, a.d_in);
     const uint32_t sx_at = (uint32_t)(wm + l15) * 16 + kq * 4, sw_at = (uint32_t)(wn + l15) * 16 + kq * 4;
@@ -268,7 +273,7 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
 #pragma unroll
         for (int i = 0; i < NB; ++i) tw[i] = __builtin_amdgcn_raw_buffer_load_b32(rw, sw_at + i * 256, 0, 0);
     };
-    request_scales(sx, sw, 0);
+    if constexpr (!SLOTS) request_scales(sx, sw, 0);
     auto xslot = [&](int it) { return ring + (it % D) * kXElems; };
     auto wslot = [&](int it) { return ring + D * kXElems + (it % (D + 1)) * kWElems; };
     auto request_x = [&](bf16_t* slot, int kt, int i, auto is_part) {
@@ -279,11 +284,31 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
         if constexpr (decltype(is_part)::value) dma_piece_behind<true, false>(slot, ow, w_bytes, ow, part, -1, i, wave);
         else dma_piece<ONCE ? kReadOnceI8 : 0>(slot, ow, kt, i, wave);
     };
+    auto request_s = [&](bf16_t* xsl, bf16_t* wsl, int kt) {   // 64 rows each; fewer than there are wavefronts: some twice
+#pragma unroll
+        for (int j = 0; j < PS; ++j) {
+            const int g = (j * 4 + wave) % (GX + GW), r = g < GX ? g : g - GX;
+            const __amdgpu_buffer_rsrc_t rsrc = (g < GX ? xsc : wsc).chunk(kt >> 1);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rsrc, (__attribute__((address_space(3))) void*)((g < GX ? xsl + BM * kGemmBK : wsl + BN * kGemmBK) + r * 512), 16,
+                (uint32_t)(r * 64 + lane) * 16, 0, 0, 0);
+        }
+    };
+    auto read_scales = [&](uint32_t (&tx)[MB], uint32_t (&tw)[NB], const bf16_t* xsl, const bf16_t* wsl, int kt) {
+        const int half = kt & 1;
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+            tx[i] = *reinterpret_cast<const uint16_t*>(xsl + BM * kGemmBK + (wm + i * 16 + l15) * 8 + kq * 2 + half);
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            tw[i] = *reinterpret_cast<const uint16_t*>(wsl + BN * kGemmBK + (wn + i * 16 + l15) * 8 + kq * 2 + half);
+    };
     auto request_tile = [&](int it, auto is_part) {
 #pragma unroll
         for (int i = 0; i < PX; ++i) request_x(xslot(it), it, i, is_part);
 #pragma unroll
         for (int i = 0; i < PW; ++i) request_w(wslot(it), it, i, is_part);
+        request_s(xslot(it), wslot(it), it);
     };
 #pragma unroll
     for (int t = 0; t < D; ++t)
@@ -302,15 +327,16 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
 
     Frags16<MB, NB> f0, f1;
     auto wait_tiles = [&](int left) {   // the loads of at most `left` tiles may still be in flight
-        if (D > 4 && left >= 4) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(D > 4 ? 4 * (PX + PW) : 0) : "memory");
-        else if (D > 3 && left == 3) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(D > 3 ? 3 * (PX + PW) : 0) : "memory");
-        else if (D > 2 && left == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(D > 2 ? 2 * (PX + PW) : 0) : "memory");
-        else if (left == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PX + PW) : "memory");
+        if (D > 4 && left >= 4) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(D > 4 ? 4 * P : 0) : "memory");
+        else if (D > 3 && left == 3) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(D > 3 ? 3 * P : 0) : "memory");
+        else if (D > 2 && left == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(D > 2 ? 2 * P : 0) : "memory");
+        else if (left == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(P) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     };
     wait_tiles(min(nk, D) - 1);   // d_in >= 16: one K tile at least
 #pragma unroll
     for (int i = 0; i < NR; ++i) load_frag16<MB, NB>(f0, xslot(0), wslot(0), wm, wn, l15, kq, 0, i);
+    if constexpr (SLOTS) read_scales(sx, sw, xslot(0), wslot(0), 0);
 
     using K0 = std::integral_constant<int, 0>;
     using K1 = std::integral_constant<int, 1>;
@@ -356,11 +382,12 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
         __builtin_amdgcn_sched_barrier(0);
         // tile it + 1 must have landed, and every wavefront's reads of tile it must be complete
         if constexpr (REQ < 2)
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PW + (D - 2) * (PX + PW)) : "memory");
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PW + (D - 2) * P) : "memory");
         else
             wait_tiles(nk - 2 - it);
         const bool odd = PH >= 0 ? PH % 2 != 0 : (it & 1) != 0;
-        if (!odd) request_scales(sx_next, sw_next, (it >> 1) + 1);
+        if constexpr (SLOTS) read_scales(sx_next, sw_next, xsl(1), wsl(1), it + 1);   // behind the last tile: of no use
+        else if (!odd) request_scales(sx_next, sw_next, (it >> 1) + 1);
         __builtin_amdgcn_sched_barrier(0);
         // k-step 1: its MFMAs, the first fragments of tile it + 1 and the row pieces of tile it + D into the slot just drained
         const bf16_t* xn = xsl(1);
@@ -375,6 +402,8 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
                 for (int c = 0; c < pieces_after_read(i, PX, NR); ++c) request_x(xreq, it + D, issued++, IsPart{});
                 __builtin_amdgcn_sched_barrier(0);
             }
+            request_s(xreq, wreq, it + D);
+            __builtin_amdgcn_sched_barrier(0);
             mfmas(f1, NR * RB, NM, K1{});
         } else {
             if (it + 1 < nk) {   // reads only: MFMAs in both arms of a branch make the compiler copy accumulators
@@ -384,7 +413,7 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
             __builtin_amdgcn_sched_barrier(0);
             mfmas(f1, 0, NM, K1{});
         }
-        if (odd) {
+        if (SLOTS || odd) {
 #pragma unroll
             for (int i = 0; i < MB; ++i) sx[i] = sx_next[i];
 #pragma unroll
@@ -462,7 +491,7 @@ __device__ __forceinline__ void tail_mx4_part(const GemmMx4Args& a, const RowTil
     ring_mx4_tile<TO, MB, NB, D, PART, false>(a, smem, rt.e, rt.row0 + m0, rows, n0);
 }
 constexpr int tail_mx4_lds() {   // two workgroups to a CU
-    const int a = ring_mx4_lds<2, 2, 4>(), b = ring_mx4_lds<4, 2, 3>(), c = ring_mx4_lds<4, 4, 2>();
+    const int a = ring_mx4_lds<2, 2, 3>(), b = ring_mx4_lds<4, 2, 2>(), c = ring_mx4_lds<4, 4, 2>();
     return a > b ? (a > c ? a : c) : (b > c ? b : c);
 }
 static_assert(2 * tail_mx4_lds() <= 160 * 1024, "LDS");
@@ -472,8 +501,8 @@ __global__ __launch_bounds__(256) void gemm_mx4_tail_kernel(const GemmMx4Args a)
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const RowTiles<256> row_tiles(a, (int)threadIdx.x & 63);
     const int tiles = row_tiles.count * a.tiles_n, first = tail_start(tiles);
-    if (tiles - first <= kTailSmall) tail_mx4_part<TO, 2, 2, 4, PART>(a, row_tiles, smem, first, tiles);
-    else if (tiles - first <= kTailMiddle) tail_mx4_part<TO, 4, 2, 3, PART>(a, row_tiles, smem, first, tiles);
+    if (tiles - first <= kTailSmall) tail_mx4_part<TO, 2, 2, 3, PART>(a, row_tiles, smem, first, tiles);
+    else if (tiles - first <= kTailMiddle) tail_mx4_part<TO, 4, 2, 2, PART>(a, row_tiles, smem, first, tiles);
     else tail_mx4_part<TO, 4, 4, 2, PART>(a, row_tiles, smem, first, tiles);
 }
 
@@ -633,8 +662,8 @@ static hipError_t launch_mx4(const GemmMx4Args& a, hipStream_t stream) {
         case 7: return launch_ring_mx4<TO, 4, 4, 3>(a, stream);
         case 8: return launch_ring_mx4<TO, 4, 4, 2>(a, stream);
         case 9: return launch_ring_mx4<TO, 6, 4, 3>(a, stream);
-        case 10: return launch_ring_mx4<TO, 7, 4, 3>(a, stream);
-        case 11: return launch_ring_mx4<TO, 8, 4, 3>(a, stream);
+        case 10: return launch_ring_mx4<TO, 7, 4, 2>(a, stream);
+        case 11: return launch_ring_mx4<TO, 8, 4, 2>(a, stream);
         default: return launch_largest_mx4<TO>(a, stream);
     }
 }
@@ -679,7 +708,7 @@ static hipError_t init_mx4() {   // every kernel that launch_mx4 may start
     hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_one_kernel<TO, 2, 4>), one_mx4_lds<TO, 2, 4>());
     for (hipError_t f : {init_wave<TO, 1, 1, 4, 5>(), init_wave<TO, 1, 2, 4, 5>(), init_wave<TO, 1, 4, 4, 3>(), init_wave<TO, 2, 2, 4, 4>(),
                          init_ring<TO, 2, 2, 5>(), init_ring<TO, 3, 2, 5>(), init_ring<TO, 4, 2, 4>(), init_ring<TO, 4, 4, 3>(),
-                         init_ring<TO, 4, 4, 2>(), init_ring<TO, 6, 4, 3>(), init_ring<TO, 7, 4, 3>(), init_ring<TO, 8, 4, 3>(),
+                         init_ring<TO, 4, 4, 2>(), init_ring<TO, 6, 4, 3>(), init_ring<TO, 7, 4, 2>(), init_ring<TO, 8, 4, 2>(),
                          init_ring<TO, 8, 8, 2>(), init_tail<TO>()})
         if (e == hipSuccess) e = f;
     return e;
