@@ -11,6 +11,7 @@
 // gemm_mx4_ring_kernel   many rows: tiles of 64 x 64 to 256 x 256, rings of LDS slots, scales in registers
 // gemm_mx4_wave_kernel   few rows: a ring to every wavefront, scales in its slots
 // gemm_mx4_one_kernel    up to 256 inputs: no ring
+// gemm_mx4_row_kernel    up to 4 tokens of meteora_base_gemm_mx4: their quantisation too
 #include "common.hpp"
 #include "gemm_mfma.hpp"
 #include "gemm_rows.hpp"
@@ -178,6 +179,107 @@ __global__ __launch_bounds__(WV * 64) void gemm_mx4_wave_kernel(const GemmMx4Arg
     wave_mx4_sums<TO, TB, RB, WV>(a, acc, smem, row0, rows, n0, cols, wave, lane);
 }
 
+// ------------------------------------------------------------------------------------------
+// A few tokens and their quantisation in one launch (meteora_base_gemm_mx4): every workgroup quantises all of x itself, into LDS, while its
+// first tiles of W are on their way, which costs less than a launch in front.  W goes through the wavefronts' rings as above; a lane
+// without a row of its own multiplies another's, and its result is not kept.
+// ------------------------------------------------------------------------------------------
+constexpr int kRowThreads = 256, kRowMaxTokens = 4, kRowMaxInputs = 16384;   // of all tokens
+constexpr int row_mx4_stride(int d) { return (d / 2 + 127) / 128 * 128 + 16; }   // bytes; rows start 4 banks apart
+constexpr int row_mx4_bytes(int T, int d) { return T * (row_mx4_stride(d) + mx4_chunks(d) * 16); }
+template <int RB, int D>
+constexpr int row_mx4_ring_bytes() { return 4 * D * RB * 2304; }   // and the sums in its place
+template <int RB, int D>
+constexpr int row_mx4_lds_most() { return row_mx4_ring_bytes<RB, D>() + kRowMaxInputs / 2 + kRowMaxTokens * (127 + 16) + kRowMaxInputs / 32 + kRowMaxTokens * 16; }
+
+// HELD: pieces of 8 inputs to a thread.  kRowHeld: of tokens whose last chunks are padded
+constexpr int kRowHeld = 9;
+static_assert(kRowMaxInputs + kRowMaxTokens * (kMxChunk - 32) <= kRowHeld * kRowThreads * 8, "pieces");
+template <typename TX, int RB, int D, int HELD>
+__global__ __launch_bounds__(kRowThreads) void gemm_mx4_row_kernel(const GemmMx4Args a, const TX* __restrict__ x) {
+    constexpr int WV = 4, NL = 3 * RB;
+    static_assert(D >= 2 && (D - 1) * NL < 64, "vmcnt");
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l15 = lane & 15, kq = lane >> 4;
+    const int n0 = xcd_order(blockIdx.x, a.tiles_n) * a.tile_cols, cols = min(a.tile_cols, a.d_out - n0);
+    const uint32_t ld = (uint32_t)a.d_in;
+    unsigned char* const ring = smem + wave * D * RB * 2304;
+    unsigned char* const xq = smem + row_mx4_ring_bytes<RB, D>();
+    const int inputs = a.d_in * 2, per = inputs / 8, chunks = mx4_chunks(inputs), stride = row_mx4_stride(inputs);
+    unsigned char* const xs = xq + a.T * stride;   // [T][chunks][16]
+
+    // whole chunks of 64 pieces, a block to a quad of threads; those past the last input are zeros with scale 0, since whatever LDS held there
+    // might be a NaN
+    Piece8<TX> held[HELD];
+    const int pieces = chunks * 64;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int p = i * kRowThreads + tid, t = p / pieces, j = p - t * pieces;
+        held[i] = Piece8<TX>{};
+        if (t < a.T && j < per) held[i].load(x + (size_t)t * inputs + j * 8);
+    }
+    WaveOperand<RB> w(a.W + (size_t)n0 * ld, cols, ld, lane);
+    const ScaleRows ws(a.w_scale, a.d_out, n0, cols, a.d_in);
+    const uint32_t at_scale = (uint32_t)l15 * 16 + kq * 4;
+    const int nk = ceil_div(a.d_in, 128), n = wave < nk ? (nk - 1 - wave) / WV + 1 : 0;
+    auto request = [&](unsigned char* slot, int kt) {
+        w.at_tile(kt, nk);
+        const auto scales = ws.chunk(kt >> 1);
+#pragma unroll
+        for (int i = 0; i < 2 * RB; ++i) w.template request<kReadOnceI8>(slot, i);
+#pragma unroll
+        for (int r = 0; r < RB; ++r) mx4_scale_lds(scales, slot + RB * 2048 + r * 256, at_scale + r * 256);
+    };
+#pragma unroll
+    for (int d = 0; d < D; ++d) request(ring + d * RB * 2304, wave + d * WV);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int p = i * kRowThreads + tid, t = p / pieces, j = p - t * pieces, b = j >> 2;
+        const uint32_t E = mx4_exponent(held[i]), v = mx4_quantize8(held[i], E);
+        if (t >= a.T) continue;
+        if (j < per) *reinterpret_cast<uint32_t*>(xq + t * stride + j * 4) = v;
+        if ((j & 3) == 0) xs[t * chunks * 16 + (b >> 4) * 16 + (b & 3) * 4 + ((b & 15) >> 2)] = (uint8_t)E;
+    }
+    __syncthreads();
+    const unsigned char* const mine = xq + (l15 % a.T) * stride;
+    const unsigned char* const my_scales = xs + (l15 % a.T) * chunks * 16 + kq * 4 + (wave & 1) * 2;   // a wavefront's K tiles are all even or all odd
+    const int half = (wave & 1) * 16;
+
+    f32x4 acc[1][RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) acc[0][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int slot = 0;
+    for (int i = 0; i < n; ++i) {
+        const int kt = wave + i * WV;
+        const unsigned char* const at = ring + slot * RB * 2304;
+        // of the loads only those of the D - 1 tiles behind this one may be in flight
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * NL) : "memory");
+        u32x4 wf[2][RB], xf[2];
+        uint32_t sw[RB];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r) wf[ks][r] = *reinterpret_cast<const u32x4*>(at + r * 2048 + l15 * 128 + swz(l15, ks * 4 + kq) * 16);
+            xf[ks] = *reinterpret_cast<const u32x4*>(mine + kt * 128 + (ks * 4 + kq) * 16);   // past the last input: any codes, times zeros
+        }
+#pragma unroll
+        for (int r = 0; r < RB; ++r) sw[r] = *reinterpret_cast<const uint32_t*>(at + RB * 2048 + r * 256 + lane * 4) >> half;
+        const uint32_t sx = *reinterpret_cast<const uint16_t*>(my_scales + (kt >> 1) * 16);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot is read
+        request(ring + slot * RB * 2304, kt + D * WV);
+        slot = slot + 1 == D ? 0 : slot + 1;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            acc[0][r] = mfma_mx4<0>(wf[0][r], xf[0], acc[0][r], sw[r], sx);
+            acc[0][r] = mfma_mx4<1>(wf[1][r], xf[1], acc[0][r], sw[r], sx);
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land in what follows
+    __syncthreads();
+    wave_mx4_sums<TX, 1, RB, WV>(a, acc, smem, 0, a.T, n0, cols, wave, lane);
+}
 
 // Many rows: the schedule of gemm_i8_ring_kernel.  The instruction is in assembly with its accumulator tied, with the same care
 // (tests/test_mfma_waits_mx4_host.py reads the compiled code).  Scales: with rings of two slots, which take all of LDS with 256 x 256 tiles, words in
@@ -668,6 +770,31 @@ static hipError_t launch_mx4(const GemmMx4Args& a, hipStream_t stream) {
     }
 }
 
+template <typename TX, int RB, int D>
+static hipError_t launch_row(GemmMx4Args a, const TX* x, hipStream_t stream) {
+    a.tile_cols = wave_tile_cols(1, a.d_out, RB * 16);
+    a.tiles_n = ceil_div(a.d_out, a.tile_cols);
+    const int lds = row_mx4_ring_bytes<RB, D>() + row_mx4_bytes(a.T, a.d_in * 2);
+    auto go = [&](auto kern) {
+        const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(kern), row_mx4_lds_most<RB, D>());
+        if (e != hipSuccess) return e;
+        kern<<<a.tiles_n, kRowThreads, lds, stream>>>(a, x);
+        return hipGetLastError();
+    };
+    return a.T * mx4_chunks(a.d_in * 2) * kMxChunk <= 4096 ? go(&gemm_mx4_row_kernel<TX, RB, D, 2>) : go(&gemm_mx4_row_kernel<TX, RB, D, kRowHeld>);
+}
+bool base_gemm_mx4_in_one(int T, int d_in) { return T <= kRowMaxTokens && T * d_in <= kRowMaxInputs; }
+
+template <typename TX>
+static hipError_t launch_base(const GemmMx4Args& a, const TX* x, hipStream_t stream) {
+    return a.d_out <= 4096 ? launch_row<TX, 1, 5>(a, x, stream) : launch_row<TX, 2, 4>(a, x, stream);
+}
+hipError_t launch_base_gemm_mx4_in_one(const void* x, const uint8_t* W, const uint8_t* w_scale, int T, int d_in, int d_out, bool bf16, void* out,
+                                       hipStream_t stream) {
+    const GemmMx4Args a{nullptr, nullptr, (const int8_t*)W, w_scale, nullptr, out, T, d_in / 2, d_out, 1, 1, 0, 0, 0, 0};
+    return bf16 ? launch_base(a, (const bf16_t*)x, stream) : launch_base(a, (const float*)x, stream);
+}
+
 static GemmMx4Args mx4_args(const uint8_t* q, const uint8_t* q_scale, const uint8_t* W, const uint8_t* w_scale, const int32_t* offsets,
                             int T, int d_in, int d_out, int N, void* out) {
     const int past_caches = (int64_t)N * d_out * (d_in / 2) >= 100000000;
@@ -703,13 +830,18 @@ static hipError_t init_tail() {
     const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_tail_kernel<TO, true>), tail_mx4_lds());
     return e != hipSuccess ? e : ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_tail_kernel<TO, false>), tail_mx4_lds());
 }
+template <typename TX, int RB, int D>
+static hipError_t init_row() {
+    const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_row_kernel<TX, RB, D, 2>), row_mx4_lds_most<RB, D>());
+    return e != hipSuccess ? e : ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_row_kernel<TX, RB, D, kRowHeld>), row_mx4_lds_most<RB, D>());
+}
 template <typename TO>
-static hipError_t init_mx4() {   // every kernel that launch_mx4 may start
+static hipError_t init_mx4() {   // every kernel that launch_mx4 and launch_base may start
     hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_one_kernel<TO, 2, 4>), one_mx4_lds<TO, 2, 4>());
     for (hipError_t f : {init_wave<TO, 1, 1, 4, 5>(), init_wave<TO, 1, 2, 4, 5>(), init_wave<TO, 1, 4, 4, 3>(), init_wave<TO, 2, 2, 4, 4>(),
                          init_ring<TO, 2, 2, 5>(), init_ring<TO, 3, 2, 5>(), init_ring<TO, 4, 2, 4>(), init_ring<TO, 4, 4, 3>(),
                          init_ring<TO, 4, 4, 2>(), init_ring<TO, 6, 4, 3>(), init_ring<TO, 7, 4, 2>(), init_ring<TO, 8, 4, 2>(),
-                         init_ring<TO, 8, 8, 2>(), init_tail<TO>()})
+                         init_ring<TO, 8, 8, 2>(), init_tail<TO>(), init_row<TO, 1, 5>(), init_row<TO, 2, 4>()})
         if (e == hipSuccess) e = f;
     return e;
 }
