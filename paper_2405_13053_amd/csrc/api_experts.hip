@@ -21,13 +21,15 @@ bool sizes_supported(int T, int d, int f, int N, int k) {
     return T <= kExpertsMaxTokens && N <= kMaxAdapters && k <= kMaxTopK && d % 8 == 0 && f % 8 == 0 && d <= kExpertsMaxWidth &&
            f <= kExpertsMaxWidth;
 }
-struct Scratch { size_t h, y, idx, w, total; };
-Scratch carve(int T, int d, int f, int k) {   // idx, w: the routing of meteora_moe_forward
+struct Scratch { size_t h, y, plan, idx, w, part, total; };
+Scratch carve(int T, int d, int f, int N, int k) {   // idx, w, part: the routing of meteora_moe_forward
     Scratch s{};
     s.y = align_up(experts_h_bytes(T, k, f), 256);
-    s.idx = s.y + align_up(experts_y_bytes(T, k, d), 256);
+    s.plan = s.y + align_up(experts_y_bytes(T, k, d), 256);
+    s.idx = s.plan + align_up(experts_plan_bytes(), 256);
     s.w = s.idx + align_up((size_t)T * k * sizeof(int32_t), 256);
-    s.total = s.w + align_up((size_t)T * k * sizeof(float), 256);
+    s.part = s.w + align_up((size_t)T * k * sizeof(float), 256);
+    s.total = s.part + align_up(experts_part_bytes(T, d, N), 256);
     return s;
 }
 // Everything but the routing's pointers
@@ -39,16 +41,16 @@ meteora_status check(const void* x, const void* W1, const uint8_t* s1, const voi
         return METEORA_ERR_UNSUPPORTED;
     for (const void* p : {x, W1, (const void*)s1, W2, (const void*)s2, base, out})
         if (!aligned(p, 16)) return METEORA_ERR_UNSUPPORTED;
-    if (!ws || !aligned(ws, 256) || ws_bytes < carve(T, d, f, k).total) return METEORA_ERR_WORKSPACE;
+    if (!ws || !aligned(ws, 256) || ws_bytes < carve(T, d, f, N, k).total) return METEORA_ERR_WORKSPACE;
     return METEORA_OK;
 }
-ExpertsArgs arguments(const void* x, const int32_t* idx, const float* w, const void* W1, const uint8_t* s1, const void* W2, const uint8_t* s2,
+ExpertsArgs arguments(const void* x, int32_t* idx, float* w, const void* W1, const uint8_t* s1, const void* W2, const uint8_t* s2,
                       int T, int d, int f, int N, int k, float scale, const void* base, void* out, void* ws) {
-    const Scratch s = carve(T, d, f, k);
+    const Scratch s = carve(T, d, f, N, k);
     char* const p = static_cast<char*>(ws);
     return {static_cast<const bf16_t*>(x), idx, w, static_cast<const uint8_t*>(W1), s1, static_cast<const uint8_t*>(W2), s2,
-            static_cast<const bf16_t*>(base), static_cast<bf16_t*>(out), reinterpret_cast<bf16_t*>(p), reinterpret_cast<float*>(p + s.y), scale,
-            T, k, N, d, f};
+            static_cast<const bf16_t*>(base), static_cast<bf16_t*>(out), reinterpret_cast<bf16_t*>(p), reinterpret_cast<float*>(p + s.y), p + s.plan, scale,
+            T, k, N, d, f, nullptr, nullptr, 1.f};
 }
 
 }  // namespace
@@ -57,7 +59,7 @@ extern "C" {
 
 size_t meteora_experts_workspace_bytes(int T, int d, int f, int N, int k) {
     if (!sizes_ok(T, d, f, N, k) || !sizes_supported(T, d, f, N, k)) return 0;
-    return carve(T, d, f, k).total + 256;
+    return carve(T, d, f, N, k).total + 256;
 }
 
 meteora_status meteora_experts_forward(const void* x, const int32_t* topk_idx, const float* topk_w, const void* W1, const uint8_t* w1_scale,
@@ -68,7 +70,7 @@ meteora_status meteora_experts_forward(const void* x, const int32_t* topk_idx, c
     if (s != METEORA_OK) return s;
     if (!aligned(topk_idx, 4) || !aligned(topk_w, 4)) return METEORA_ERR_UNSUPPORTED;
     if (T == 0) return METEORA_OK;
-    return status(launch_experts(arguments(x, topk_idx, topk_w, W1, w1_scale, W2, w2_scale, T, d, f, N, k, scale, base, out, ws),
+    return status(launch_experts(arguments(x, const_cast<int32_t*>(topk_idx), const_cast<float*>(topk_w), W1, w1_scale, W2, w2_scale, T, d, f, N, k, scale, base, out, ws),
                                  static_cast<hipStream_t>(stream)));
 }
 
@@ -82,12 +84,15 @@ meteora_status meteora_moe_forward(const void* x, const float* W_gate, const flo
     if (!aligned(W_gate, 16) || !aligned(gate_bias, 4) || !aligned(topk_idx_out, 4) || !aligned(topk_w_out, 4)) return METEORA_ERR_UNSUPPORTED;
     if (T == 0) return METEORA_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const Scratch c = carve(T, d, f, k);
+    const Scratch c = carve(T, d, f, N, k);
     int32_t* idx = topk_idx_out ? topk_idx_out : reinterpret_cast<int32_t*>(static_cast<char*>(ws) + c.idx);
     float* w = topk_w_out ? topk_w_out : reinterpret_cast<float*>(static_cast<char*>(ws) + c.w);
-    const hipError_t e = launch_gate_few(x, W_gate, gate_bias, T, d, N, k, inv_temperature, idx, w, st);
-    if (e != hipSuccess) return METEORA_ERR_HIP;
-    return status(launch_experts(arguments(x, idx, w, W1, w1_scale, W2, w2_scale, T, d, f, N, k, scale, base, out, ws), st));
+    ExpertsArgs a = arguments(x, idx, w, W1, w1_scale, W2, w2_scale, T, d, f, N, k, scale, base, out, ws);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + c.part);
+    a.bias = gate_bias;
+    a.inv_temperature = inv_temperature;
+    const hipError_t e = launch_experts_gate(a, W_gate, st);
+    return e != hipSuccess ? METEORA_ERR_HIP : status(launch_experts(a, st));
 }
 
 }  // extern "C"

@@ -16,6 +16,8 @@
 //   through the experts in use one after the other, so that the weighted sum is in registers and nothing is added in memory.
 // more: an expert's tokens are columns, 16 or 32 at a time, read once for the four wavefronts of a workgroup, which have rows of W of
 //   their own.  experts_up_kernel and experts_down_kernel; experts_sum_kernel adds the rows of a token.
+#include <stddef.h>
+
 #include <type_traits>
 
 #include "common.hpp"
@@ -29,27 +31,124 @@ namespace meteora {
 
 constexpr int kFewTokens = 4;
 
-// ---- routing: bit t of masks[e]: token t goes to expert e, by however many slots.  LDS; all threads of the workgroup.
+// ---- the gate: logits[j] = sum_i x[i] W_gate[i,j] + bias[j], top-k and softmax.  gate_part_kernel: a slice of the rows of W_gate, 16 values to a
+// thread, for 8 tokens; part[t][slice][NP], NP = N rounded up to a power of two.  The slices are added where they are needed, by whoever
+// needs the routing: a wavefront to a token.
+constexpr int kGateSlices = 32, kGateTokens = 8, kGateHeld = 16;
+__host__ __device__ constexpr int gate_columns(int N) { return N <= 8 ? 8 : N <= 16 ? 16 : N <= 32 ? 32 : 64; }
+__host__ __device__ constexpr int gate_slice_rows(int NP) { return 256 * kGateHeld / NP; }
+__host__ __device__ constexpr int gate_slices(int d, int N) {
+    const int n = (d + gate_slice_rows(gate_columns(N)) - 1) / gate_slice_rows(gate_columns(N));
+    return n < kGateSlices ? n : kGateSlices;
+}
+
+template <int NP>
+__global__ __launch_bounds__(256) void gate_part_kernel(const bf16_t* __restrict__ x, const float* __restrict__ W_gate, int T, int d, int N,
+                                                        float* __restrict__ part) {
+    constexpr int SUB = 64 / NP, STEP = 4 * SUB, R = STEP * kGateHeld;   // rows of a wavefront's load, of the workgroup's, of a slice
+    static_assert(R == gate_slice_rows(NP), "slice");
+    __shared__ float xs[kGateTokens][R];
+    __shared__ float sums[kGateTokens][4][NP];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane % NP, sub = wave * SUB + lane / NP;
+    const int t0 = blockIdx.y * kGateTokens, tokens = min(kGateTokens, T - t0);
+    float sum[kGateTokens] = {};
+    for (int r0 = blockIdx.x * R; r0 < d; r0 += gridDim.x * R) {
+        float w[kGateHeld];
+#pragma unroll
+        for (int i = 0; i < kGateHeld; ++i) {
+            const int r = r0 + i * STEP + sub;
+            w[i] = r < d && col < N ? W_gate[(size_t)r * N + col] : 0.f;
+        }
+        __syncthreads();
+        for (int p = tid; p < tokens * (R / 8); p += 256) {   // d % 8 == 0
+            const int t = p / (R / 8), c = p % (R / 8) * 8;
+            Piece8<bf16_t> v{};
+            if (r0 + c < d) v.load(x + (size_t)(t0 + t) * d + r0 + c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) xs[t][c + i] = v.at(i);
+        }
+        __syncthreads();
+        for (int t = 0; t < tokens; ++t) {
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < kGateHeld; ++i) s = fmaf(xs[t][i * STEP + sub], w[i], s);
+#pragma unroll
+            for (int u = 0; u < kGateTokens; ++u) sum[u] += u == t ? s : 0.f;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < kGateTokens; ++t) {
+        float s = sum[t];
+#pragma unroll
+        for (int off = NP; off < 64; off <<= 1) s += __shfl_xor(s, off);
+        if (lane < NP) sums[t][wave][lane] = s;
+    }
+    __syncthreads();
+    for (int p = tid; p < tokens * NP; p += 256) {
+        const int t = p / NP, c = p % NP;
+        part[((size_t)(t0 + t) * gridDim.x + blockIdx.x) * NP + c] = sums[t][0][c] + sums[t][1][c] + (sums[t][2][c] + sums[t][3][c]);
+    }
+}
+
+// Token t by a wavefront: lane j < k has its j-th choice and weight.
+__device__ __forceinline__ void route_token(const ExpertsArgs& a, int t, int lane, int& expert, float& weight) {
+    const int NP = gate_columns(a.N), slices = gate_slices(a.d, a.N), each = 64 / NP, col = lane % NP;
+    const float* p = a.part + (size_t)t * slices * NP + col;
+    float g[1] = {0.f};
+    for (int s = lane / NP; s < slices; s += 4 * each) {
+        float v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = s + u * each < slices ? p[(size_t)(s + u * each) * NP] : 0.f;
+        g[0] += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    const float b = a.bias != nullptr && lane < a.N ? a.bias[lane] : 0.f;
+    for (int off = NP; off < 64; off <<= 1) g[0] += __shfl_xor(g[0], off);
+    g[0] += b;
+    if (g[0] == 0.f) g[0] = 0.f;   // -0 -> +0 so equal logits have equal keys
+    int sel[1];
+    float w[1];
+    wave_topk_softmax<64, 1>(g, lane, a.N, a.k, a.inv_temperature, sel, w);
+    expert = sel[0];
+    weight = w[0];
+}
+__global__ __launch_bounds__(256) void experts_route_kernel(const ExpertsArgs a) {
+    const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= a.T) return;
+    int e;
+    float w;
+    route_token(a, t, lane, e, w);
+    if (lane < a.k) {
+        a.idx[t * a.k + lane] = e;
+        a.w[t * a.k + lane] = w;
+    }
+}
+
+// ---- which tokens an expert has: bit t of word[e], by however many of the token's slots.  LDS; all threads of the workgroup.
 struct ExpertMasks { uint32_t word[kMaxAdapters][2]; };
 
 __device__ __forceinline__ void find_masks(const ExpertsArgs& a, ExpertMasks& m) {
+    int e = -1;   // T * k <= 512: up to two pairs to a thread, on their way first
+    const int pairs = a.T * a.k, p0 = threadIdx.x, p1 = p0 + blockDim.x;
+    if (p0 < pairs) e = a.idx[p0];
+    const int e1 = p1 < pairs ? a.idx[p1] : -1;
     for (int i = threadIdx.x; i < 2 * kMaxAdapters; i += blockDim.x) m.word[i >> 1][i & 1] = 0;
     __syncthreads();
-    for (int p = threadIdx.x; p < a.T * a.k; p += blockDim.x) {
-        const int e = a.idx[p], t = p / a.k;
-        if ((unsigned)e < (unsigned)a.N) atomicOr(&m.word[e][t >> 5], 1u << (t & 31));
-    }
+    if ((unsigned)e < (unsigned)a.N) atomicOr(&m.word[e][p0 / a.k >> 5], 1u << (p0 / a.k & 31));
+    if ((unsigned)e1 < (unsigned)a.N) atomicOr(&m.word[e1][p1 / a.k >> 5], 1u << (p1 / a.k & 31));
     __syncthreads();
 }
 __device__ __forceinline__ uint64_t mask_of(const ExpertMasks& m, int e) { return (uint64_t)m.word[e][1] << 32 | m.word[e][0]; }
 __device__ __forceinline__ int rank_in(uint64_t mask, int t) { return __popcll(mask & (((uint64_t)1 << t) - 1)); }
-// an inclusive sum over the lanes
-__device__ __forceinline__ int wave_sums(int v, int lane) {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int n = __shfl_up(v, off);
-        if (lane >= off) v += n;
-    }
+// an inclusive sum over the lanes (DPP: within rows of 16, then across them)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_rows(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_sums(int v) {
+    v += dpp_rows<kDppRowShr + 1, 0xf>(v);
+    v += dpp_rows<kDppRowShr + 2, 0xf>(v);
+    v += dpp_rows<kDppRowShr + 4, 0xf>(v);
+    v += dpp_rows<kDppRowShr + 8, 0xf>(v);
+    v += dpp_rows<kDppBcast15, 0xa>(v);
+    v += dpp_rows<kDppBcast31, 0xc>(v);
     return v;
 }
 
@@ -75,6 +174,7 @@ struct WeightRing {
     __device__ __forceinline__ WeightRing(const uint8_t* W, const uint8_t* scale, int all, int row0, int n, int bytes, int lane)
         : rows(reinterpret_cast<const int8_t*>(W), n, (uint32_t)bytes, lane), scales(scale, all, row0, n, bytes),
           at_scale((uint32_t)(lane & 15) * 16 + (lane >> 4) * 4) {}
+    __device__ __forceinline__ WeightRing(int bytes, int lane) : WeightRing(nullptr, nullptr, 0, 0, 0, bytes, lane) {}
     __device__ __forceinline__ void point(const uint8_t* W, const uint8_t* scale, int all, int row0, int n, int bytes) {
         rows.mat = i8_operand(reinterpret_cast<const int8_t*>(W), n, (uint32_t)bytes);
         scales = ScaleRows(scale, all, row0, n, bytes);
@@ -181,7 +281,23 @@ __global__ __launch_bounds__(256) void experts_few_up_kernel(const ExpertsArgs a
     __shared__ ExpertMasks masks;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l15 = lane & 15, kq = lane >> 4;
-    find_masks(a, masks);
+    if (a.part != nullptr) {   // every workgroup routes; the first one says how
+        int e = -1;
+        float w = 0.f;
+        if (wave < a.T) route_token(a, wave, lane, e, w);
+        if (tid < 2 * kMaxAdapters) masks.word[tid >> 1][tid & 1] = 0;
+        __syncthreads();
+        if (wave < a.T && lane < a.k) {
+            if ((unsigned)e < (unsigned)a.N) atomicOr(&masks.word[e][0], 1u << wave);
+            if (blockIdx.x == 0) {
+                a.idx[wave * a.k + lane] = e;
+                a.w[wave * a.k + lane] = w;
+            }
+        }
+        __syncthreads();
+    } else {
+        find_masks(a, masks);
+    }
     const uint64_t mine = lane < a.N ? mask_of(masks, lane) : 0;
     const uint64_t active = __ballot(mine != 0);
     const int tiles = ceil_div(a.f, CH), total = __popcll(active) * tiles;
@@ -189,7 +305,7 @@ __global__ __launch_bounds__(256) void experts_few_up_kernel(const ExpertsArgs a
     const int id = xcd_order(blockIdx.x, total);
     const int which = id / tiles;
     const int e = __builtin_amdgcn_readfirstlane(__ffsll(__ballot(mine != 0 && rank_in(active, lane) == which)) - 1);
-    const int sums = wave_sums(__popcll(mine), lane);
+    const int sums = wave_sums(__popcll(mine));
     const int first = __builtin_amdgcn_readfirstlane(__shfl(sums, e) - __popcll(mask_of(masks, e)));   // row of h
     const uint32_t tokens = masks.word[e][0];
     const int c0 = (id - which * tiles) * CH + (KS == 1 ? wave * 16 : 0), n = min(16, a.f - c0);   // this wavefront's channels; n <= 0: none
@@ -268,14 +384,20 @@ __global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const Experts
     __shared__ ExpertMasks masks;
     __shared__ int list[kMaxAdapters][2];                  // the experts in use and their first rows of h
     __shared__ float weight[kMaxAdapters][kFewTokens];
+    __shared__ int ids[kFewTokens * kMaxTopK];
+    __shared__ float ws[kFewTokens * kMaxTopK];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l15 = lane & 15, kq = lane >> 4;
+    if (tid < a.T * a.k) {
+        ids[tid] = a.idx[tid];
+        ws[tid] = a.w[tid];
+    }
     find_masks(a, masks);
     const uint64_t mine = lane < a.N ? mask_of(masks, lane) : 0;
     const uint64_t active = __ballot(mine != 0);
     const int count = __popcll(active);
     if (wave == 0) {
-        const int sums = wave_sums(__popcll(mine), lane);
+        const int sums = wave_sums(__popcll(mine));
         if (mine != 0) {
             const int i = rank_in(active, lane);
             list[i][0] = lane;
@@ -283,7 +405,7 @@ __global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const Experts
             for (int t = 0; t < kFewTokens; ++t) {
                 float w = 0.f;
                 for (int j = 0; j < a.k && t < a.T; ++j)
-                    if (a.idx[t * a.k + j] == lane) w += a.w[t * a.k + j];
+                    if (ids[t * a.k + j] == lane) w += ws[t * a.k + j];
                 weight[i][t] = w;
             }
         }
@@ -371,91 +493,90 @@ __global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const Experts
 }
 
 // ---- more tokens -----------------------------------------------------------------------------------------------------------------
-// Blocks of R = 16 TB tokens of an expert, tiles of channels; the four wavefronts share the tokens' rows.
-struct Block {
-    int e, begin, count, first;   // expert, its tokens begin .. begin + count - 1, and the row of h and y of the first of these
-};
-template <int R>
-struct Blocks {
-    uint64_t mine;
-    int sums, blocks, end, total;
-    __device__ __forceinline__ Blocks(const ExpertsArgs& a, const ExpertMasks& m, int lane) {
-        mine = lane < a.N ? mask_of(m, lane) : 0;
-        sums = wave_sums(__popcll(mine), lane);
-        blocks = (__popcll(mine) + R - 1) / R;
-        end = wave_sums(blocks, lane);
-        total = __builtin_amdgcn_readfirstlane(__shfl(end, 63));
-    }
-    __device__ __forceinline__ Block at(int b) const {
-        const int e = __ffsll(__ballot(end > b)) - 1;
-        const int n = __shfl(__popcll(mine), e), begin = (b - (__shfl(end, e) - __shfl(blocks, e))) * R;
-        return {__builtin_amdgcn_readfirstlane(e), __builtin_amdgcn_readfirstlane(begin), __builtin_amdgcn_readfirstlane(min(R, n - begin)),
-                __builtin_amdgcn_readfirstlane(__shfl(sums, e) - n + begin)};
-    }
-};
+// Blocks of R = 16 TB tokens of an expert; w wavefronts of a workgroup's 8 take 16 rows of gate and up (32 rows of W2) each, and all share the
+// tokens' rows.  A workgroup has every grid-th (tile, block), and its loads run on from one into the next.
+constexpr int kManyWaves = 8, kManySplits = 4;
 
-template <typename WT, int TB, int RB>
-constexpr int many_slot_bytes() { return 4 * RB * WT::kBlockBytes + TB * 16 * kTokenBytes<WT>; }
+// What a launch of 256 workgroups does: w, and (down) the parts that K is cut into.  The choice is the one that takes the least by
+//   rounds * K tiles of a part * time of one + parts
+// us.  A K tile of w wavefronts took, 4 bits and blocks of 16 tokens (20 tokens of 16 experts, 4096 and 2048 wide), 0.76, 0.81, 0.86, 0.90, 1.09, 1.15,
+// 1.18, 1.4 us for w = 1 to 8, and with blocks of 32 (64 tokens of 8 experts, 4096 and 14336) 0.92, 0.97, 1.02, 1.08, 1.37, 1.45, 1.53, 1.73: up to 4, one
+// wavefront to a SIMD, mostly the way from the barrier through LDS and the MFMAs to the next one.
+// Calls of 33 tokens of 28 experts, 2080 and 1376 wide, with w = 4, 5 and 8 for the first product 53.9, 53.8, 62.3; of 64 of 8, 4096 and 14336, w = 4, 7, 8
+// 181, 158, 171, and the second product with w = 8 whole and in two and four parts 195, 158, 162.
+struct Tiling { int waves, splits; };
+template <typename WT>
+__device__ __forceinline__ Tiling choose_tiling(int blocks, int units, int nk, bool may_split, int lane) {   // a wavefront; units: of channels
+    const int w = (lane & 7) + 1, splits = 1 << (lane >> 3 & 3);
+    const int items = blocks * ((units + w - 1) / w) * splits;
+    const float tile = w <= 4 ? 0.87f + 0.053f * (float)w : 1.f + 0.08f * (float)w;
+    const float us = (float)((items + 255) / 256) * (float)((nk + splits - 1) / splits) * tile + (float)splits;
+    const bool there = lane < 8 || (may_split && lane < 24 && splits <= kManySplits && nk >= 4 * splits);   // no part is empty
+    // the least, of equal ones the first lane's; positive floats compare as whole numbers
+    uint32_t best = there ? (__float_as_uint(us) & ~31u) | (uint32_t)(lane & 31) : 0x7f800000u;
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) best = min(best, (uint32_t)__shfl_xor((int)best, off));
+    const int at = __builtin_amdgcn_readfirstlane((int)(best & 31));
+    return {(at & 7) + 1, 1 << (at >> 3 & 3)};
+}
 
-// The loop over K of a workgroup: wavefront w has RB blocks of 16 rows, `rows` of them there are (by the ring), and the
-// workgroup TB x 16 tokens, of which the first USED x 16 are multiplied.  `where(r)`: the first byte of token row r in `tokens`, or kOutside.
-// USED is a constant, and a block of few tokens has a loop of its own: with a branch around the second 16 tokens' MFMAs the compiler moves
-// accumulators behind the branch and leaves out the wait states for it (ROCm 7.2; tests/test_experts_host.py looks for that).
-template <typename WT, int TB, int USED, int RB, int D, typename Ring, typename Where>
-__device__ __forceinline__ void many_loop(f32x4 (&acc)[TB][RB], unsigned char* smem, Ring& ring, int nk, bool there, __amdgpu_buffer_rsrc_t tokens,
-                                          uint32_t ld, int wave, int lane, Where where) {
-    constexpr int kSlot = many_slot_bytes<WT, TB, RB>(), kRowsPer = TokenPiece<WT>::kRows, PIECES = TB * 16 / kRowsPer;
-    constexpr int NP = PIECES < 4 ? 1 : PIECES / 4, NL = RB * (2 + WT::kScales) + NP;
-    static_assert(D >= 3 && (D - 2) * NL < 64, "vmcnt");
-    const int l15 = lane & 15, kq = lane >> 4;
-    auto first_row = [&](int i) { return ((i * 4 + wave) % PIECES) * kRowsPer; };   // fewer than four pieces: some twice
-    TokenPiece<WT> piece[NP];
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        piece[i].set(first_row(i), lane);
-        piece[i].point(where(piece[i].row));
-    }
-    auto request = [&](int kt) {
-        unsigned char* const slot = smem + kt % D * kSlot;
-        ring.at_tile(kt, there ? nk : 0);
-        ring.request(slot + wave * RB * WT::kBlockBytes);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) piece[i].request(tokens, slot + 4 * RB * WT::kBlockBytes, first_row(i), kt, nk, ld);
-    };
-#pragma unroll
-    for (int i = 0; i < D - 1; ++i) request(i);
-#pragma unroll
-    for (int t = 0; t < TB; ++t)
-#pragma unroll
-        for (int r = 0; r < RB; ++r) acc[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int kt = 0; kt < nk; ++kt) {
-        // this wavefront's part of the tile has landed, and so, behind the barrier, the others'; the slot before is read by all
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((D - 2) * NL) : "memory");
-        request(kt + D - 1);
-        const unsigned char* const slot = smem + kt % D * kSlot;
-        WeightFrags<WT, RB> w;
-        w.read(slot + wave * RB * WT::kBlockBytes, kt, lane);
-        const unsigned char* const rows = slot + 4 * RB * WT::kBlockBytes;
-#pragma unroll
-        for (int i = 0; i < WT::kSteps; ++i) {
-            bf16x8 wf[RB];
-#pragma unroll
-            for (int r = 0; r < RB; ++r) wf[r] = w.at(i, r);
-#pragma unroll
-            for (int t = 0; t < USED; ++t) {
-                const bf16x8 xf = token_frag<WT>(rows, t * 16 + l15, kq, i);
-#pragma unroll
-                for (int r = 0; r < RB; ++r) acc[t][r] = mfma_bf16(wf[r], xf, acc[t][r]);
-            }
+// The plan of a call, in the workspace for the launches behind the first
+struct Plan {
+    int blocks, splits;   // splits: of the second product
+    int up_waves, down_waves;
+    uint32_t block[kMaxAdapters + kExpertsMaxTokens * kMaxTopK / 16];   // expert | tokens << 8 | first row of h and y << 16
+    int16_t row[kExpertsMaxTokens * kMaxTopK];                           // of pair (t, j), -1: none
+};
+size_t experts_plan_bytes() { return sizeof(Plan); }
+
+// All threads of a workgroup.  token: of a row of h.  to: where the plan goes, or nullptr.
+template <typename WT, int R>
+__device__ __forceinline__ void make_plan(const ExpertsArgs& a, Plan& plan, ExpertMasks& masks, int (&first)[kMaxAdapters],
+                                          uint8_t (&token)[kExpertsMaxTokens * kMaxTopK], Plan* to) {
+    const int lane = threadIdx.x & 63, pairs = a.T * a.k, p = threadIdx.x;   // 512 threads: a pair each
+    const int e = p < pairs ? a.idx[p] : -1, t = p / a.k;
+    const bool there = (unsigned)e < (unsigned)a.N;
+    for (int i = threadIdx.x; i < 2 * kMaxAdapters; i += blockDim.x) masks.word[i >> 1][i & 1] = 0;
+    __syncthreads();
+    if (there) atomicOr(&masks.word[e][t >> 5], 1u << (t & 31));
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const int n = lane < a.N ? __popcll(mask_of(masks, lane)) : 0, mine = (n + R - 1) / R;
+        const int at = wave_sums(n) - n, end = wave_sums(mine);
+        first[lane] = at;
+        for (int i = 0; i < mine; ++i) plan.block[end - mine + i] = (uint32_t)lane | (uint32_t)min(R, n - i * R) << 8 | (uint32_t)(at + i * R) << 16;
+        const int blocks = __builtin_amdgcn_readlane(end, 63);
+        const Tiling up = choose_tiling<WT>(blocks, ceil_div(a.f, 16), ceil_div(WT::row_bytes(a.d), 128), false, lane);
+        const Tiling down = choose_tiling<WT>(blocks, ceil_div(a.d, 32), ceil_div(WT::row_bytes(a.f), 128), true, lane);
+        if (lane == 0) {
+            plan.blocks = blocks;
+            plan.up_waves = up.waves;
+            plan.down_waves = down.waves;
+            plan.splits = down.splits;
         }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const int row = there ? first[e] + rank_in(mask_of(masks, e), t) : -1;
+    if (there) token[row] = (uint8_t)t;
+    if (p < pairs) plan.row[p] = (int16_t)row;
+    __syncthreads();
+    if (to != nullptr)
+        for (int i = threadIdx.x; i < (int)(sizeof(Plan) / 4); i += blockDim.x) reinterpret_cast<uint32_t*>(to)[i] = reinterpret_cast<const uint32_t*>(&plan)[i];
 }
+struct Block { int e, count, first; };
+__device__ __forceinline__ Block unpack_block(uint32_t v) {
+    const uint32_t u = (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+    return {(int)(u & 255), (int)(u >> 8 & 255), (int)(u >> 16)};
+}
+
+template <typename WT, int TB>
+constexpr int many_slot_bytes() { return kManyWaves * 2 * WT::kBlockBytes + TB * 16 * kTokenBytes<WT>; }
 
 // The rings of gate and up rows as one operand of two blocks
 template <typename WT>
 struct PairRing {
     WeightRing<WT, 1> g, u;
+    __device__ __forceinline__ PairRing(int bytes, int lane) : g(bytes, lane), u(bytes, lane) {}
     __device__ __forceinline__ void at_tile(int kt, int nk) { g.at_tile(kt, nk); u.at_tile(kt, nk); }
     __device__ __forceinline__ void request(unsigned char* slot) const {   // as two blocks of one ring lie: rows, rows, scales, scales
 #pragma unroll
@@ -469,106 +590,179 @@ struct PairRing {
     }
 };
 
-template <typename WT, int TB, int D>
-__global__ __launch_bounds__(256) void experts_up_kernel(const ExpertsArgs a) {
+// The second 16 tokens are multiplied whether there are any or not: with a branch around their MFMAs the compiler moves accumulators right behind
+// the branch and leaves out the wait states for it (ROCm 7.2; tests/test_experts_host.py looks for that).  For the same reason wavefronts
+// without channels, which only load tokens, have a loop of their own.
+// UP: channels of h from the rows of x, the first launch; otherwise channels of y from those of h
+template <typename WT, bool UP, int TB, int D>
+__global__ __launch_bounds__(kManyWaves * 64) void experts_many_kernel(const ExpertsArgs a) {
+    constexpr int WV = kManyWaves, R = TB * 16, RB = 2, kSlot = many_slot_bytes<WT, TB>(), kRowsPer = TokenPiece<WT>::kRows;
+    constexpr int PIECES = R / kRowsPer, NP = PIECES < WV ? 1 : PIECES / WV, NL = RB * (2 + WT::kScales) + NP;
+    constexpr int CW = UP ? 16 : 32;   // channels of a wavefront
+    static_assert(D >= 3 && (D - 2) * NL < 64, "vmcnt");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    __shared__ ExpertMasks masks;
-    __shared__ int list[TB * 16];
+    __shared__ Plan plan;
+    __shared__ uint8_t token[kExpertsMaxTokens * kMaxTopK];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l15 = lane & 15, kq = lane >> 4;
-    find_masks(a, masks);
-    const Blocks<TB * 16> blocks(a, masks, lane);
-    const int tiles = ceil_div(a.f, 64), total = blocks.total * tiles;
-    if ((int)blockIdx.x >= total) return;
-    const int id = xcd_order(blockIdx.x, total), column = id / blocks.total;
-    const Block b = blocks.at(id - column * blocks.total);
-    if (wave == 0) {
-        const uint64_t m = mask_of(masks, b.e);
-        const int r = rank_in(m, lane) - b.begin;
-        if ((m >> lane & 1) && r >= 0 && r < b.count) list[r] = lane;
+    if constexpr (UP) {
+        // masks and the experts' first rows are in the rings' place
+        make_plan<WT, R>(a, plan, *reinterpret_cast<ExpertMasks*>(smem), *reinterpret_cast<int(*)[kMaxAdapters]>(smem + sizeof(ExpertMasks)), token,
+                         blockIdx.x == 0 ? reinterpret_cast<Plan*>(a.plan) : nullptr);
+        __syncthreads();
+    } else {
+        for (int i = tid; i < (int)(offsetof(Plan, row) / 4); i += WV * 64)
+            reinterpret_cast<uint32_t*>(&plan)[i] = reinterpret_cast<const uint32_t*>(a.plan)[i];
+        __syncthreads();
     }
-    __syncthreads();
-    const int c0 = column * 64 + wave * 16, n = min(16, a.f - c0);
-    const int bytes = WT::row_bytes(a.d), nk = ceil_div(bytes, 128);
-    const uint8_t* W = a.W1 + ((size_t)b.e * 2 * a.f + c0) * bytes;
-    const uint8_t* S = WT::kScales ? a.s1 + (size_t)b.e * mx4_scale_bytes(2 * a.f, a.d) : nullptr;
-    PairRing<WT> ring{WeightRing<WT, 1>(W, S, 2 * a.f, c0, max(n, 0), bytes, lane),
-                      WeightRing<WT, 1>(W + (size_t)a.f * bytes, S, 2 * a.f, a.f + c0, max(n, 0), bytes, lane)};
-    const auto tile = [&](auto used) __attribute__((always_inline)) {
-        constexpr int USED = decltype(used)::value;
-        f32x4 acc[TB][2];
-        many_loop<WT, TB, USED, 2, D>(acc, smem, ring, nk, n > 0, token_rsrc(a.x, a.T, a.d), (uint32_t)a.d * 2u, wave, lane,
-                                      [&](int r) { return r < b.count ? (uint32_t)list[r] * (uint32_t)a.d * 2u : kOutside; });
-#pragma unroll
-        for (int t = 0; t < USED; ++t)
-            if (t * 16 + l15 < b.count && kq * 4 < n)
-                store_h(a.h + (size_t)(b.first + t * 16 + l15) * a.f + c0 + kq * 4, acc[t][0], acc[t][1]);
+    const int K = UP ? a.d : a.f, C = UP ? a.f : a.d;   // inputs, channels
+    const int waves = __builtin_amdgcn_readfirstlane(UP ? plan.up_waves : plan.down_waves);
+    const int splits = UP ? 1 : __builtin_amdgcn_readfirstlane(plan.splits);
+    const int bytes = WT::row_bytes(K), nk = ceil_div(bytes, 128), per = ceil_div(nk, splits);
+    const int nb = __builtin_amdgcn_readfirstlane(plan.blocks) * splits, total = nb * ceil_div(C, waves * CW);   // 0: no token has an expert
+    // workgroups: as many on every XCD, each with the same number of items but for some that have one less
+    const int G = ceil_div(total, max(ceil_div(total, (int)gridDim.x), 1));
+    if (total == 0 || (int)blockIdx.x >= G) return;
+    const int start = xcd_order(blockIdx.x, G);
+
+    struct Item { int col, part; Block b; };
+    auto item_at = [&](int i) {   // tiles of one column for all blocks, of a block for all parts
+        const int col = i / nb, rest = i - col * nb, b = rest / splits;
+        return Item{col, rest - b * splits, unpack_block(plan.block[b])};
     };
-    if (TB == 1 || b.count <= 16) tile(std::integral_constant<int, 1>{});
-    else tile(std::integral_constant<int, TB>{});
+    std::conditional_t<UP, PairRing<WT>, WeightRing<WT, RB>> ring(bytes, lane);
+    const auto rows = UP ? token_rsrc(a.x, a.T, a.d) : token_rsrc(a.h, a.T * a.k, a.f);
+    auto first_row = [&](int i) { return ((i * WV + wave) % PIECES) * kRowsPer; };   // fewer pieces than wavefronts: some twice
+    TokenPiece<WT> piece[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) piece[i].set(first_row(i), lane);
+
+    int req_item = start, req_kt, req_end, req_at = 0;   // next request: K tile of an item; behind the last one req_kt = req_end = 0
+    auto point = [&] {
+        const Item m = item_at(req_item);
+        const int c0 = (m.col * waves + wave) * CW, n = max(min(CW, C - c0), 0);
+        req_kt = m.part * per;
+        req_end = min(nk, req_kt + per);
+        if constexpr (UP) {
+            const uint8_t* W = a.W1 + ((size_t)m.b.e * 2 * a.f + c0) * bytes;
+            const uint8_t* S = WT::kScales ? a.s1 + (size_t)m.b.e * mx4_scale_bytes(2 * a.f, a.d) : nullptr;
+            ring.g.point(W, S, 2 * a.f, c0, n, bytes);
+            ring.u.point(W + (size_t)a.f * bytes, S, 2 * a.f, a.f + c0, n, bytes);
+        } else {
+            ring.point(a.W2 + ((size_t)m.b.e * a.d + c0) * bytes, WT::kScales ? a.s2 + (size_t)m.b.e * mx4_scale_bytes(a.d, a.f) : nullptr, a.d, c0, n,
+                       bytes);
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int r = piece[i].row;
+            const uint32_t row = UP ? (r < m.b.count ? token[m.b.first + r] : 0) : (uint32_t)(m.b.first + r);
+            piece[i].point(r < m.b.count ? row * (uint32_t)K * 2u : kOutside);
+        }
+    };
+    point();
+    auto request = [&](auto with_weights) {
+        unsigned char* const slot = smem + req_at * kSlot;
+        req_at = req_at + 1 == D ? 0 : req_at + 1;
+        if constexpr (decltype(with_weights)::value) {
+            ring.at_tile(req_kt, req_end);
+            ring.request(slot + wave * RB * WT::kBlockBytes);
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+            piece[i].request(rows, slot + WV * RB * WT::kBlockBytes, first_row(i), req_kt, req_end, (uint32_t)K * 2u);
+        if (++req_kt >= req_end && req_end > 0) {
+            req_item += G;
+            if (req_item < total) point();
+            else req_kt = req_end = 0;
+        }
+    };
+    if (wave >= waves) {
+#pragma unroll
+        for (int i = 0; i < D - 1; ++i) request(std::false_type{});
+        for (int item = start; item < total; item += G) {
+            const int part = item % splits;   // nb is a multiple of splits
+            for (int kt = part * per; kt < min(nk, part * per + per); ++kt) {
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((D - 2) * NP) : "memory");
+                request(std::false_type{});
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land after the end
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < D - 1; ++i) request(std::true_type{});
+    f32x4 acc[TB][RB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int r = 0; r < RB; ++r) acc[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int at = 0;
+    for (int item = start; item < total; item += G) {
+        const Item m = item_at(item);
+        const int end = min(nk, m.part * per + per);
+        for (int kt = m.part * per; kt < end; ++kt) {
+            // this wavefront's part of the tile has landed, and so, behind the barrier, the others'; the slot before is read by all
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((D - 2) * NL) : "memory");
+            request(std::true_type{});
+            const unsigned char* const slot = smem + at * kSlot;
+            at = at + 1 == D ? 0 : at + 1;
+            WeightFrags<WT, RB> w;
+            w.read(slot + wave * RB * WT::kBlockBytes, kt, lane);
+            const unsigned char* const tokens = slot + WV * RB * WT::kBlockBytes;
+#pragma unroll
+            for (int i = 0; i < WT::kSteps; ++i) {
+                bf16x8 wf[RB];
+#pragma unroll
+                for (int r = 0; r < RB; ++r) wf[r] = w.at(i, r);
+#pragma unroll
+                for (int t = 0; t < TB; ++t) {
+                    const bf16x8 xf = token_frag<WT>(tokens, t * 16 + l15, kq, i);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) acc[t][r] = mfma_bf16(wf[r], xf, acc[t][r]);
+                }
+            }
+        }
+        const int c0 = (m.col * waves + wave) * CW, n = min(CW, C - c0);
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+            const int r = t * 16 + l15;
+            if constexpr (UP) {
+                if (r < m.b.count && kq * 4 < n) store_h(a.h + (size_t)(m.b.first + r) * a.f + c0 + kq * 4, acc[t][0], acc[t][1]);
+            } else {
+                float* const y = a.y + (size_t)m.part * ((size_t)a.T * a.k * a.d) + (size_t)(m.b.first + r) * a.d + c0 + kq * 4;
+#pragma unroll
+                for (int q = 0; q < RB; ++q)
+                    if (r < m.b.count && q * 16 + kq * 4 < n) *reinterpret_cast<f32x4*>(y + q * 16) = acc[t][q];
+            }
+#pragma unroll
+            for (int q = 0; q < RB; ++q) acc[t][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land after the end
 }
 
-template <typename WT, int TB, int RB, int D>
-__global__ __launch_bounds__(256) void experts_down_kernel(const ExpertsArgs a) {
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    __shared__ ExpertMasks masks;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int l15 = lane & 15, kq = lane >> 4;
-    find_masks(a, masks);
-    const Blocks<TB * 16> blocks(a, masks, lane);
-    const int tiles = ceil_div(a.d, 64 * RB), total = blocks.total * tiles;
-    if ((int)blockIdx.x >= total) return;
-    const int id = xcd_order(blockIdx.x, total), column = id / blocks.total;
-    const Block b = blocks.at(id - column * blocks.total);
-    const int c0 = (column * 4 + wave) * 16 * RB, n = min(16 * RB, a.d - c0);
-    const int bytes = WT::row_bytes(a.f), nk = ceil_div(bytes, 128);
-    WeightRing<WT, RB> ring(a.W2 + ((size_t)b.e * a.d + c0) * bytes, WT::kScales ? a.s2 + (size_t)b.e * mx4_scale_bytes(a.d, a.f) : nullptr, a.d,
-                            c0, max(n, 0), bytes, lane);
-    const auto tile = [&](auto used) __attribute__((always_inline)) {
-        constexpr int USED = decltype(used)::value;
-        f32x4 acc[TB][RB];
-        many_loop<WT, TB, USED, RB, D>(acc, smem, ring, nk, n > 0, token_rsrc(a.h, a.T * a.k, a.f), (uint32_t)a.f * 2u, wave, lane,
-                                       [&](int r) { return r < b.count ? (uint32_t)(b.first + r) * (uint32_t)a.f * 2u : kOutside; });
-#pragma unroll
-        for (int t = 0; t < USED; ++t)
-#pragma unroll
-            for (int r = 0; r < RB; ++r)
-                if (t * 16 + l15 < b.count && r * 16 + kq * 4 < n)
-                    *reinterpret_cast<f32x4*>(a.y + (size_t)(b.first + t * 16 + l15) * a.d + c0 + r * 16 + kq * 4) = acc[t][r];
-    };
-    if (TB == 1 || b.count <= 16) tile(std::integral_constant<int, 1>{});
-    else tile(std::integral_constant<int, TB>{});
-}
-
-// out[t] = base[t] + scale * sum_j w[t,j] * y[row of (t, its expert j)], a token and 2048 channels to a workgroup
+// out[t] = base[t] + scale * sum_j w[t,j] * y[row of (t, j)], the parts of y added first; a token and 1024 channels to a workgroup
 __global__ __launch_bounds__(256) void experts_sum_kernel(const ExpertsArgs a) {
-    __shared__ ExpertMasks masks;
-    const int tid = threadIdx.x, lane = tid & 63, t = blockIdx.y;
-    find_masks(a, masks);
-    const uint64_t mine = lane < a.N ? mask_of(masks, lane) : 0;
-    const int row = wave_sums(__popcll(mine), lane) - __popcll(mine) + rank_in(mine, t);   // of this token for expert `lane`
-    const int c = (blockIdx.x * 256 + tid) * 8;
-    float sum[8] = {};
-    for (int j = 0; j < a.k; ++j) {
-        const int e = a.idx[t * a.k + j];
-        if ((unsigned)e >= (unsigned)a.N) continue;
-        const float w = a.w[t * a.k + j];
-        const float* y = a.y + (size_t)__shfl(row, e) * a.d + c;
-        if (c >= a.d) continue;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += w * y[i];
-    }
+    const Plan* const plan = reinterpret_cast<const Plan*>(a.plan);
+    const int t = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
     if (c >= a.d) return;
-    const size_t o = (size_t)t * a.d + c;
-    uint32_t packed[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float v[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) v[h] = a.scale * sum[2 * i + h] + (a.base != nullptr ? (float)a.base[o + 2 * i + h] : 0.f);
-        packed[i] = pack_bf16x2(v[0], v[1]);
+    const int splits = plan->splits;
+    const size_t part = (size_t)a.T * a.k * a.d;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < a.k; ++j) {
+        const int row = plan->row[t * a.k + j];
+        if (row < 0) continue;
+        const float w = a.w[t * a.k + j];
+        const float* const y = a.y + (size_t)row * a.d + c;
+        f32x4 v = *reinterpret_cast<const f32x4*>(y);
+        for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(y + (size_t)s * part);
+        sum += w * v;
     }
-    *reinterpret_cast<u32x4*>(a.out + o) = u32x4{packed[0], packed[1], packed[2], packed[3]};
+    const size_t o = (size_t)t * a.d + c;
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a.scale * sum[i] + (a.base != nullptr ? (float)a.base[o + i] : 0.f);
+    *reinterpret_cast<uint2*>(a.out + o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
 }
 
 template <typename K>
@@ -582,10 +776,10 @@ template <typename WT, int KS, int D>
 constexpr int few_up_lds() { return 4 * D * few_slot_bytes<WT, 2>(); }
 template <typename WT, int KS, int D>
 constexpr int few_down_lds() { return KS * D * few_slot_bytes<WT, 1>(); }
-template <typename WT, int TB, int RB, int D>
-constexpr int many_lds() { return D * many_slot_bytes<WT, TB, RB>(); }
 template <typename WT> constexpr int kFewUpDepth = WT::kScales ? 3 : 4;
-template <typename WT> constexpr int kFewDownDepth = 5;
+constexpr int kFewDownWaves = 8;
+template <typename WT> constexpr int kFewDownDepth = WT::kScales ? 4 : 5;
+template <typename WT> constexpr int kManyDepth = WT::kScales ? 3 : 4;
 
 template <typename WT>
 static hipError_t launch_few(const ExpertsArgs& a, hipStream_t stream) {
@@ -595,98 +789,60 @@ static hipError_t launch_few(const ExpertsArgs& a, hipStream_t stream) {
     const hipError_t e = split ? start(&experts_few_up_kernel<WT, 4, DU>, most * ceil_div(a.f, 16), 256, few_up_lds<WT, 4, DU>(), a, stream)
                                : start(&experts_few_up_kernel<WT, 1, DU>, most * ceil_div(a.f, 64), 256, few_up_lds<WT, 1, DU>(), a, stream);
     if (e != hipSuccess) return e;
-    return start(&experts_few_down_kernel<WT, 4, DD>, ceil_div(a.d, 16), 256, few_down_lds<WT, 4, DD>(), a, stream);
+    return start(&experts_few_down_kernel<WT, kFewDownWaves, DD>, ceil_div(a.d, 16), kFewDownWaves * 64, few_down_lds<WT, kFewDownWaves, DD>(), a, stream);
 }
 template <typename WT, int TB>
 static hipError_t launch_many(const ExpertsArgs& a, hipStream_t stream) {
-    constexpr int D = WT::kScales && TB == 2 ? 4 : 3;
-    const int most = a.T * a.k < a.N ? a.T * a.k : a.N;
-    const int blocks = most + a.T * a.k / (16 * TB);   // sum of ceil(n_e / R) over the experts in use, sum of n_e <= T * k
-    hipError_t e = start(&experts_up_kernel<WT, TB, D>, blocks * ceil_div(a.f, 64), 256, many_lds<WT, TB, 2, D>(), a, stream);
+    constexpr int D = kManyDepth<WT>, LDS = D * many_slot_bytes<WT, TB>();
+    static_assert(LDS + (int)sizeof(Plan) + kExpertsMaxTokens * kMaxTopK <= 160 * 1024, "LDS");
+    hipError_t e = start(&experts_many_kernel<WT, true, TB, D>, 256, kManyWaves * 64, LDS, a, stream);
     if (e != hipSuccess) return e;
-    e = start(&experts_down_kernel<WT, TB, 2, D>, blocks * ceil_div(a.d, 128), 256, many_lds<WT, TB, 2, D>(), a, stream);
+    e = start(&experts_many_kernel<WT, false, TB, D>, 256, kManyWaves * 64, LDS, a, stream);
     if (e != hipSuccess) return e;
-    experts_sum_kernel<<<dim3(ceil_div(a.d, 2048), a.T), 256, 0, stream>>>(a);
+    experts_sum_kernel<<<dim3(ceil_div(a.d, 1024), a.T), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 template <typename WT>
 static hipError_t launch(const ExpertsArgs& a, hipStream_t stream) {
     if (a.T <= kFewTokens) return launch_few<WT>(a, stream);
-    return a.T <= 16 ? launch_many<WT, 1>(a, stream) : launch_many<WT, 2>(a, stream);
+    return a.T * a.k <= 10 * a.N || a.T <= 16 ? launch_many<WT, 1>(a, stream) : launch_many<WT, 2>(a, stream);
 }
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t stream) {
     return a.s1 != nullptr ? launch<Mx4Weights>(a, stream) : launch<Bf16Weights>(a, stream);
 }
 
 size_t experts_h_bytes(int T, int k, int f) { return (size_t)T * k * f * sizeof(bf16_t); }
-size_t experts_y_bytes(int T, int k, int d) { return T <= kFewTokens ? 0 : (size_t)T * k * d * sizeof(float); }
+size_t experts_y_bytes(int T, int k, int d) { return T <= kFewTokens ? 0 : (size_t)kManySplits * T * k * d * sizeof(float); }
 
-// ---- the gate of a few tokens: a token to a workgroup, logits[j] = sum_i x[i] W_gate[i,j] + bias[j], top-k and softmax ------------
-// Lanes hold columns of W_gate, 64 / NP rows a load instruction; fp32 sums in a fixed order.
-template <int NP>
-__global__ __launch_bounds__(1024) void gate_few_kernel(const bf16_t* __restrict__ x, const float* __restrict__ W_gate,
-                                                        const float* __restrict__ bias, int d, int N, int k, float inv_temperature,
-                                                        int32_t* __restrict__ topk_idx, float* __restrict__ topk_w) {
-    constexpr int SUB = 64 / NP, STEP = 16 * SUB, U = 8;
-    __shared__ float part[16][64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane % NP, t = blockIdx.x;
-    const bf16_t* row = x + (size_t)t * d;
-    float sum[2] = {0.f, 0.f};
-    for (int i0 = wave * SUB + lane / NP; i0 < d; i0 += STEP * U) {
-        float w[U], v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * STEP;
-            const bool in = i < d && col < N;
-            w[u] = in ? W_gate[(size_t)i * N + col] : 0.f;
-            v[u] = in ? (float)row[i] : 0.f;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) sum[u & 1] = fmaf(v[u], w[u], sum[u & 1]);
+size_t experts_part_bytes(int T, int d, int N) { return (size_t)T * gate_slices(d, N) * gate_columns(N) * sizeof(float); }
+
+// the partial logits, and for more than 4 tokens the routing from them
+hipError_t launch_experts_gate(const ExpertsArgs& a, const float* W_gate, hipStream_t stream) {
+    const dim3 grid(gate_slices(a.d, a.N), ceil_div(a.T, kGateTokens));
+    const auto go = [&](auto kern) { kern<<<grid, 256, 0, stream>>>(a.x, W_gate, a.T, a.d, a.N, const_cast<float*>(a.part)); };
+    switch (gate_columns(a.N)) {
+        case 8: go(&gate_part_kernel<8>); break;
+        case 16: go(&gate_part_kernel<16>); break;
+        case 32: go(&gate_part_kernel<32>); break;
+        default: go(&gate_part_kernel<64>);
     }
-    float s = sum[0] + sum[1];
-#pragma unroll
-    for (int off = NP; off < 64; off <<= 1) s += __shfl_xor(s, off);
-    part[wave][lane] = s;
-    __syncthreads();
-    if (wave != 0) return;
-    float g[1] = {0.f};
-    if (lane < N) {
-        const int at = lane % NP;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) g[0] += part[v][at];
-        g[0] += bias != nullptr ? bias[lane] : 0.f;
-        if (g[0] == 0.f) g[0] = 0.f;   // -0 -> +0 so equal logits have equal keys
-    }
-    int sel[1];
-    float w[1];
-    wave_topk_softmax<64, 1>(g, lane, N, k, inv_temperature, sel, w);
-    if (lane < k) {
-        topk_idx[(size_t)t * k + lane] = sel[0];
-        topk_w[(size_t)t * k + lane] = w[0];
-    }
-}
-hipError_t launch_gate_few(const void* x, const float* W_gate, const float* bias, int T, int d, int N, int k, float inv_temperature,
-                           int32_t* topk_idx, float* topk_w, hipStream_t stream) {
-    const auto go = [&](auto kern) {
-        kern<<<T, 1024, 0, stream>>>((const bf16_t*)x, W_gate, bias, d, N, k, inv_temperature, topk_idx, topk_w);
-        return hipGetLastError();
-    };
-    return N <= 8 ? go(&gate_few_kernel<8>) : N <= 16 ? go(&gate_few_kernel<16>) : N <= 32 ? go(&gate_few_kernel<32>) : go(&gate_few_kernel<64>);
+    if (a.T > kFewTokens) experts_route_kernel<<<ceil_div(a.T, 4), 256, 0, stream>>>(a);
+    return hipGetLastError();
 }
 
 template <typename WT>
 static hipError_t init_experts() {   // every kernel that launch_experts may start
-    constexpr int DU = kFewUpDepth<WT>, DD = kFewDownDepth<WT>, D2 = WT::kScales ? 4 : 3;
+    constexpr int DU = kFewUpDepth<WT>, DD = kFewDownDepth<WT>;
     hipError_t e = hipSuccess;
     const auto set = [&](const void* k, int lds) { if (e == hipSuccess) e = ensure_lds_limit(k, lds); };
     set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 4, DU>), few_up_lds<WT, 4, DU>());
     set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 1, DU>), few_up_lds<WT, 1, DU>());
-    set(reinterpret_cast<const void*>(&experts_few_down_kernel<WT, 4, DD>), few_down_lds<WT, 4, DD>());
-    set(reinterpret_cast<const void*>(&experts_up_kernel<WT, 1, 3>), many_lds<WT, 1, 2, 3>());
-    set(reinterpret_cast<const void*>(&experts_up_kernel<WT, 2, D2>), many_lds<WT, 2, 2, D2>());
-    set(reinterpret_cast<const void*>(&experts_down_kernel<WT, 1, 2, 3>), many_lds<WT, 1, 2, 3>());
-    set(reinterpret_cast<const void*>(&experts_down_kernel<WT, 2, 2, D2>), many_lds<WT, 2, 2, D2>());
+    set(reinterpret_cast<const void*>(&experts_few_down_kernel<WT, kFewDownWaves, DD>), few_down_lds<WT, kFewDownWaves, DD>());
+    constexpr int D = kManyDepth<WT>;
+    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, true, 1, D>), D * many_slot_bytes<WT, 1>());
+    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, true, 2, D>), D * many_slot_bytes<WT, 2>());
+    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, false, 1, D>), D * many_slot_bytes<WT, 1>());
+    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, false, 2, D>), D * many_slot_bytes<WT, 2>());
     return e;
 }
 hipError_t experts_init_kernels() {

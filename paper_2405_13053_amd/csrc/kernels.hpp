@@ -259,21 +259,26 @@ I8Plan gemm_mx4_plan(int T, int d_in, int d_out, int N, bool grouped);
 constexpr int kExpertsMaxTokens = 64;
 struct ExpertsArgs {
     const bf16_t* x;                     // [T, d]
-    const int32_t* idx;                  // [T, k]; ids outside [0, N): nothing
-    const float* w;                      // [T, k]
+    int32_t* idx;                        // [T, k]; ids outside [0, N): nothing.  Written with `part`, else read only
+    float* w;                            // [T, k]
     const uint8_t *W1, *s1, *W2, *s2;    // [N, 2f, d], [N, d, f]: bf16 (scales nullptr), or 4 bits (quant_mx4.hpp)
     const bf16_t* base;                  // [T, d] or nullptr; may be out
     bf16_t* out;                         // [T, d]
-    bf16_t* h;                           // scratch: experts_h_bytes, experts_y_bytes
+    bf16_t* h;                           // scratch: experts_h_bytes, experts_y_bytes, experts_plan_bytes
     float* y;
+    void* plan;                          // experts_plan_bytes
     float scale;
     int T, k, N, d, f;
+    const float* part;                   // partial logits of the gate (experts_part_bytes), or nullptr: the routing is given
+    const float* bias;                   // [N] or nullptr
+    float inv_temperature;
 };
+size_t experts_part_bytes(int T, int d, int N);
 size_t experts_h_bytes(int T, int k, int f);
 size_t experts_y_bytes(int T, int k, int d);
+size_t experts_plan_bytes();
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t stream);
-hipError_t launch_gate_few(const void* x, const float* W_gate, const float* bias, int T, int d, int N, int k, float inv_temperature,
-                           int32_t* topk_idx, float* topk_w, hipStream_t stream);
+hipError_t launch_experts_gate(const ExpertsArgs& a, const float* W_gate, hipStream_t stream);   // in front of launch_experts, with `part`
 hipError_t experts_init_kernels();
 
 // ---- rows sorted by adapter: pos[T,k], offsets[N+1], xs[pos[t,j]] = x[t] (with xs_scale: as 8-bit whole numbers), and back

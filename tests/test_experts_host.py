@@ -14,7 +14,7 @@ from tests import test_mfma_waits_host as waits
 
 
 @pytest.mark.skipif(shutil.which("hipcc") is None, reason="needs hipcc")
-@pytest.mark.parametrize("source,kernels", [("experts", r"experts_(?:few_)?(?:up|down)_kernel"), ("gemm_mx4", r"gemm_mx4_(?:wave|one|row)_kernel")])
+@pytest.mark.parametrize("source,kernels", [("experts", r"experts_(?:few_up|few_down|many)_kernel"), ("gemm_mx4", r"gemm_mx4_(?:wave|one|row)_kernel")])
 def test_results_of_builtins_are_waited_for_on_every_path(source, kernels, tmp_path, monkeypatch):
     asm = tmp_path / "code.s"
     flags = [f for f in build.HIPCC_FLAGS if f not in ("-fPIC", "-shared")]
