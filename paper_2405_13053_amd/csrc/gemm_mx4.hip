@@ -283,9 +283,20 @@ __global__ __launch_bounds__(kRowThreads) void gemm_mx4_row_kernel(const GemmMx4
 
 // Many rows: the schedule of gemm_i8_ring_kernel.  The instruction is in assembly with its accumulator tied, with the same care
 // (tests/test_mfma_waits_mx4_host.py reads the compiled code).  Scales: with rings of two slots, which take all of LDS with 256 x 256 tiles, words in
-// registers, MB + NB a lane for two K tiles, loaded a tile and a half ahead; the second tile's are shifted down.  Loads complete in order, so in
+// registers, MB + NB a lane for two K tiles, loaded a tile and a half ahead: 64 rows' 16 bytes to an instruction, a row to a lane, and turned to
+// the words of four blocks of rows in registers (turn_scales); the second tile's are shifted down.  A load for every block of 16 rows
+// instead, 16 a wavefront rather than 4, held up the K tiles' own: 4096 x 4096 -> 4096 34.8 us, 8192 x 4096 -> 14336 240.  Loads complete in order, so in
 // deeper rings those words would wait for every K tile requested before them; there the scales are part of the slots, 16 bytes a row
 // (those of two K tiles, in either's slot), 64 rows a load instruction.
+// In: lane g * 16 + l has the 16 bytes of row g * 16 + l, a word for each quarter.  Out: word i of lane kq * 16 + l is word kq of row i * 16 + l.
+__device__ __forceinline__ void turn_scales(const u32x4& v, uint32_t (&out)[4]) {
+    const auto a = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false), b = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    out[0] = c[0];
+    out[1] = c[1];
+    out[2] = d[0];
+    out[3] = d[1];
+}
 template <int BLOCKS, int D>
 constexpr int mx4_slot_bytes() { return BLOCKS * 32 * kI8Tile + (D > 2 ? ceil_div(BLOCKS, 2) * 1024 : 0); }
 template <int MB, int NB, int D>
@@ -366,16 +377,23 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
     // Scales: the low half of a word is the tile's that is multiplied; next: of the chunk of two tiles behind it, or of the tile
     const ScaleRows xsc(a.q_scale, a.T, row0, rows, a.d_in);
     const ScaleRows wsc(a.w_scale + (size_t)e * mx4_scale_bytes(a.d_out, a.d_in * 2), a.d_out, n0, cols, a.d_in);
-    const uint32_t sx_at = (uint32_t)(wm + l15) * 16 + kq * 4, sw_at = (uint32_t)(wn + l15) * 16 + kq * 4;
-    uint32_t sx[MB], sw[NB], sx_next[MB], sw_next[NB];
-    auto request_scales = [&](uint32_t (&tx)[MB], uint32_t (&tw)[NB], int chunk) {
-        const __amdgpu_buffer_rsrc_t rx = xsc.chunk(chunk), rw = wsc.chunk(chunk);
-#pragma unroll
-        for (int i = 0; i < MB; ++i) tx[i] = __builtin_amdgcn_raw_buffer_load_b32(rx, sx_at + i * 256, 0, 0);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) tw[i] = __builtin_amdgcn_raw_buffer_load_b32(rw, sw_at + i * 256, 0, 0);
+    constexpr int SX = ceil_div(MB, 4), SW = ceil_div(NB, 4);
+    uint32_t sx[SX * 4], sw[SW * 4], sx_next[SX * 4], sw_next[SW * 4];
+    u32x4 ahead[SX + SW];
+    auto request_ahead = [&](int chunk, int i) {   // i < SX + SW
+        const int r = i < SX ? wm + i * 64 : wn + (i - SX) * 64;
+        ahead[i] = __builtin_amdgcn_raw_buffer_load_b128((i < SX ? xsc : wsc).chunk(chunk), (uint32_t)(r + lane) * 16, 0, 0);
     };
-    if constexpr (!SLOTS) request_scales(sx, sw, 0);
+    auto take_ahead = [&] {
+#pragma unroll
+        for (int i = 0; i < SX; ++i) turn_scales(ahead[i], *reinterpret_cast<uint32_t(*)[4]>(sx + i * 4));
+#pragma unroll
+        for (int i = 0; i < SW; ++i) turn_scales(ahead[SX + i], *reinterpret_cast<uint32_t(*)[4]>(sw + i * 4));
+    };
+    if constexpr (!SLOTS) {
+#pragma unroll
+        for (int i = 0; i < SX + SW; ++i) request_ahead(0, i);
+    }
     auto xslot = [&](int it) { return ring + (it % D) * kXElems; };
     auto wslot = [&](int it) { return ring + D * kXElems + (it % (D + 1)) * kWElems; };
     auto request_x = [&](bf16_t* slot, int kt, int i, auto is_part) {
@@ -396,7 +414,7 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
                 (uint32_t)(r * 64 + lane) * 16, 0, 0, 0);
         }
     };
-    auto read_scales = [&](uint32_t (&tx)[MB], uint32_t (&tw)[NB], const bf16_t* xsl, const bf16_t* wsl, int kt) {
+    auto read_scales = [&](uint32_t (&tx)[SX * 4], uint32_t (&tw)[SW * 4], const bf16_t* xsl, const bf16_t* wsl, int kt) {
         const int half = kt & 1;
 #pragma unroll
         for (int i = 0; i < MB; ++i)
@@ -438,7 +456,13 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
     wait_tiles(min(nk, D) - 1);   // d_in >= 16: one K tile at least
 #pragma unroll
     for (int i = 0; i < NR; ++i) load_frag16<MB, NB>(f0, xslot(0), wslot(0), wm, wn, l15, kq, 0, i);
-    if constexpr (SLOTS) read_scales(sx, sw, xslot(0), wslot(0), 0);
+    if constexpr (SLOTS) {
+        read_scales(sx, sw, xslot(0), wslot(0), 0);
+    } else {
+        take_ahead();
+        asm volatile("s_nop 1" ::: "memory");
+    }
+    __builtin_amdgcn_sched_barrier(0);
 
     using K0 = std::integral_constant<int, 0>;
     using K1 = std::integral_constant<int, 1>;
@@ -469,7 +493,7 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
         bf16_t* const xreq = xsl(D);
         bf16_t* const wreq = wsl(D);
         // k-step 0: its MFMAs, the fragment reads of k-step 1 and the W pieces of tile it + D
-        int issued = 0;
+        int issued = 0, scale_piece = 0;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             mfmas(f0, i * RA, (i + 1) * RA, K0{});
@@ -489,7 +513,10 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
             wait_tiles(nk - 2 - it);
         const bool odd = PH >= 0 ? PH % 2 != 0 : (it & 1) != 0;
         if constexpr (SLOTS) read_scales(sx_next, sw_next, xsl(1), wsl(1), it + 1);   // behind the last tile: of no use
-        else if (!odd) request_scales(sx_next, sw_next, (it >> 1) + 1);
+        else if (PH < 0 && !odd) {
+#pragma unroll
+            for (int i = 0; i < SX + SW; ++i) request_ahead((it >> 1) + 1, i);
+        }
         __builtin_amdgcn_sched_barrier(0);
         // k-step 1: its MFMAs, the first fragments of tile it + 1 and the row pieces of tile it + D into the slot just drained
         const bf16_t* xn = xsl(1);
@@ -502,6 +529,10 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
                 load_frag16<MB, NB>(f0, xn, wnx, wm, wn, l15, kq, 0, i);
 #pragma unroll
                 for (int c = 0; c < pieces_after_read(i, PX, NR); ++c) request_x(xreq, it + D, issued++, IsPart{});
+                if constexpr (!SLOTS && PH >= 0 && PH % 2 == 0) {
+#pragma unroll
+                    for (int c = 0; c < pieces_after_read(i, SX + SW, NR); ++c) request_ahead((it >> 1) + 1, scale_piece++);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             request_s(xreq, wreq, it + D);
@@ -515,11 +546,13 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
             __builtin_amdgcn_sched_barrier(0);
             mfmas(f1, 0, NM, K1{});
         }
-        if (SLOTS || odd) {
+        if constexpr (SLOTS) {
 #pragma unroll
             for (int i = 0; i < MB; ++i) sx[i] = sx_next[i];
 #pragma unroll
             for (int i = 0; i < NB; ++i) sw[i] = sw_next[i];
+        } else if (odd) {
+            take_ahead();
         } else {
 #pragma unroll
             for (int i = 0; i < MB; ++i) sx[i] >>= 16;
