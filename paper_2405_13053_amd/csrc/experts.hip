@@ -30,11 +30,12 @@
 namespace meteora {
 
 constexpr int kFewTokens = 4;
+constexpr int kRouteTokens = 16;   // up to here every workgroup of the first product routes, beyond it is a launch of its own
 
 // ---- the gate: logits[j] = sum_i x[i] W_gate[i,j] + bias[j], top-k and softmax.  gate_part_kernel: a slice of the rows of W_gate, 16 values to a
-// thread, for 8 tokens; part[t][slice][NP], NP = N rounded up to a power of two.  The slices are added where they are needed, by whoever
+// thread, for 4 tokens; part[t][slice][NP], NP = N rounded up to a power of two.  The slices are added where they are needed, by whoever
 // needs the routing: a wavefront to a token.
-constexpr int kGateSlices = 32, kGateTokens = 8, kGateHeld = 16;
+constexpr int kGateSlices = 32, kGateTokens = 4, kGateHeld = 16;
 __host__ __device__ constexpr int gate_columns(int N) { return N <= 8 ? 8 : N <= 16 ? 16 : N <= 32 ? 32 : 64; }
 __host__ __device__ constexpr int gate_slice_rows(int NP) { return 256 * kGateHeld / NP; }
 __host__ __device__ constexpr int gate_slices(int d, int N) {
@@ -60,20 +61,20 @@ __global__ __launch_bounds__(256) void gate_part_kernel(const bf16_t* __restrict
             w[i] = r < d && col < N ? W_gate[(size_t)r * N + col] : 0.f;
         }
         __syncthreads();
-        for (int p = tid; p < tokens * (R / 8); p += 256) {   // d % 8 == 0
+        for (int p = tid; p < kGateTokens * (R / 8); p += 256) {   // d % 8 == 0
             const int t = p / (R / 8), c = p % (R / 8) * 8;
             Piece8<bf16_t> v{};
-            if (r0 + c < d) v.load(x + (size_t)(t0 + t) * d + r0 + c);
+            if (t < tokens && r0 + c < d) v.load(x + (size_t)(t0 + t) * d + r0 + c);
 #pragma unroll
             for (int i = 0; i < 8; ++i) xs[t][c + i] = v.at(i);
         }
         __syncthreads();
-        for (int t = 0; t < tokens; ++t) {
+#pragma unroll
+        for (int t = 0; t < kGateTokens; ++t) {
             float s = 0.f;
 #pragma unroll
             for (int i = 0; i < kGateHeld; ++i) s = fmaf(xs[t][i * STEP + sub], w[i], s);
-#pragma unroll
-            for (int u = 0; u < kGateTokens; ++u) sum[u] += u == t ? s : 0.f;
+            sum[t] += s;
         }
     }
 #pragma unroll
@@ -162,26 +163,43 @@ struct Mx4Weights {
     static constexpr int row_bytes(int d) { return d / 2; }
 };
 
-// RB blocks of 16 rows of W in a wavefront's slots: the rows' bytes (see WaveOperand), then their words of scales
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<const uint8_t*>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+                                            (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v));
+}
+
+// RB blocks of 16 rows of W in a wavefront's slots: the rows' bytes (see WaveOperand), then their words of scales.  Addresses are kept as they are and made
+// resources for every K tile: where a ring goes from matrix to matrix the compiler keeps resources in vector registers otherwise and
+// walks every load through a loop over the lanes (0.9 us to a K tile, whatever its size).
 template <typename WT, int RB>
 struct WeightRing {
     static constexpr int kLoads = RB * (2 + WT::kScales), kBytes = RB * WT::kBlockBytes;
     WaveOperand<RB> rows;
-    ScaleRows scales;
     __amdgpu_buffer_rsrc_t scale_rsrc;
+    const uint8_t *W, *scale;
+    int n, all, bytes;
     uint32_t at_scale;
     // W: the first of `n` rows of `bytes` each; scale: that matrix's, with `all` rows, of which it is row0
     __device__ __forceinline__ WeightRing(const uint8_t* W, const uint8_t* scale, int all, int row0, int n, int bytes, int lane)
-        : rows(reinterpret_cast<const int8_t*>(W), n, (uint32_t)bytes, lane), scales(scale, all, row0, n, bytes),
-          at_scale((uint32_t)(lane & 15) * 16 + (lane >> 4) * 4) {}
-    __device__ __forceinline__ WeightRing(int bytes, int lane) : WeightRing(nullptr, nullptr, 0, 0, 0, bytes, lane) {}
-    __device__ __forceinline__ void point(const uint8_t* W, const uint8_t* scale, int all, int row0, int n, int bytes) {
-        rows.mat = i8_operand(reinterpret_cast<const int8_t*>(W), n, (uint32_t)bytes);
-        scales = ScaleRows(scale, all, row0, n, bytes);
+        : WeightRing(bytes, lane) {
+        point(W, scale, all, row0, n);
+    }
+    __device__ __forceinline__ WeightRing(int bytes, int lane)
+        : rows(nullptr, 0, (uint32_t)bytes, lane), bytes(bytes), at_scale((uint32_t)(lane & 15) * 16 + (lane >> 4) * 4) {}
+    __device__ __forceinline__ void point(const uint8_t* w, const uint8_t* s, int of, int row0, int count) {
+        W = w;
+        n = count;
+        all = of;
+        if constexpr (WT::kScales) scale = s + (size_t)row0 * 16;
     }
     __device__ __forceinline__ void at_tile(int kt, int nk) {
+        const int there = __builtin_amdgcn_readfirstlane(n);
+        rows.mat = i8_operand(reinterpret_cast<const int8_t*>(uniform(W)), there, (uint32_t)bytes);
         rows.at_tile(kt, nk);
-        if constexpr (WT::kScales) scale_rsrc = scales.chunk(kt < nk ? kt >> 1 : scales.chunks);
+        if constexpr (WT::kScales)
+            scale_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(uniform(scale + (size_t)(kt >> 1) * ((size_t)all * 16))), 0,
+                                                           kt < nk ? (uint32_t)there * 16u : 0u, 0x00020000);
     }
     __device__ __forceinline__ void request(unsigned char* slot) const {
 #pragma unroll
@@ -424,7 +442,7 @@ __global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const Experts
     auto point = [&](int i) {
         const int e = __builtin_amdgcn_readfirstlane(list[i][0]), row = __builtin_amdgcn_readfirstlane(list[i][1]);
         const uint32_t tokens = masks.word[e][0];
-        w.point(a.W2 + ((size_t)e * a.d + c0) * bytes, WT::kScales ? a.s2 + (size_t)e * mx4_scale_bytes(a.d, a.f) : nullptr, a.d, c0, n, bytes);
+        w.point(a.W2 + ((size_t)e * a.d + c0) * bytes, WT::kScales ? a.s2 + (size_t)e * mx4_scale_bytes(a.d, a.f) : nullptr, a.d, c0, n);
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const int t = piece[p].row;
@@ -495,22 +513,22 @@ __global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const Experts
 // ---- more tokens -----------------------------------------------------------------------------------------------------------------
 // Blocks of R = 16 TB tokens of an expert; w wavefronts of a workgroup's 8 take 16 rows of gate and up (32 rows of W2) each, and all share the
 // tokens' rows.  A workgroup has every grid-th (tile, block), and its loads run on from one into the next.
-constexpr int kManyWaves = 8, kManySplits = 4;
+constexpr int kManyWaves = 8, kManyThreads = kManyWaves * 64, kManyGroups = 256, kManySplits = 4;
+static_assert(kManyThreads >= kExpertsMaxTokens * kMaxTopK, "a pair to a thread");
 
 // What a launch of 256 workgroups does: w, and (down) the parts that K is cut into.  The choice is the one that takes the least by
 //   rounds * K tiles of a part * time of one + parts
-// us.  A K tile of w wavefronts took, 4 bits and blocks of 16 tokens (20 tokens of 16 experts, 4096 and 2048 wide), 0.76, 0.81, 0.86, 0.90, 1.09, 1.15,
-// 1.18, 1.4 us for w = 1 to 8, and with blocks of 32 (64 tokens of 8 experts, 4096 and 14336) 0.92, 0.97, 1.02, 1.08, 1.37, 1.45, 1.53, 1.73: up to 4, one
-// wavefront to a SIMD, mostly the way from the barrier through LDS and the MFMAs to the next one.
-// Calls of 33 tokens of 28 experts, 2080 and 1376 wide, with w = 4, 5 and 8 for the first product 53.9, 53.8, 62.3; of 64 of 8, 4096 and 14336, w = 4, 7, 8
-// 181, 158, 171, and the second product with w = 8 whole and in two and four parts 195, 158, 162.
+// us.  A K tile of w wavefronts took, 4 bits and blocks of 16 tokens (20 tokens of 16 experts, 4096 and 2048 wide), 0.54, 0.57, 0.62, 0.69, 0.85, 0.91,
+// 0.94, 1.24 us for w = 1 to 8, and with blocks of 32 (64 tokens of 8 experts, 4096 and 14336) 0.70, 0.74, 0.83, 0.97, 1.25, 1.32, 1.45, 1.6.
+// Calls of 33 tokens of 28 experts, 2080 and 1376 wide, with w = 4, 5 and 8 for the first product 51.6, 49.4, 55.5; of 64 of 8, 4096 and 14336, w = 4, 7, 8
+// 166, 150, 159, and the second product with w = 8 whole and in two and four parts 180, 152, 154.
 struct Tiling { int waves, splits; };
 template <typename WT>
 __device__ __forceinline__ Tiling choose_tiling(int blocks, int units, int nk, bool may_split, int lane) {   // a wavefront; units: of channels
     const int w = (lane & 7) + 1, splits = 1 << (lane >> 3 & 3);
     const int items = blocks * ((units + w - 1) / w) * splits;
-    const float tile = w <= 4 ? 0.87f + 0.053f * (float)w : 1.f + 0.08f * (float)w;
-    const float us = (float)((items + 255) / 256) * (float)((nk + splits - 1) / splits) * tile + (float)splits;
+    const float tile = w <= 4 ? 0.49f + 0.05f * (float)w : 0.5f + 0.07f * (float)w;
+    const float us = (float)((items + kManyGroups - 1) / kManyGroups) * (float)((nk + splits - 1) / splits) * tile + (float)splits;
     const bool there = lane < 8 || (may_split && lane < 24 && splits <= kManySplits && nk >= 4 * splits);   // no part is empty
     // the least, of equal ones the first lane's; positive floats compare as whole numbers
     uint32_t best = there ? (__float_as_uint(us) & ~31u) | (uint32_t)(lane & 31) : 0x7f800000u;
@@ -529,14 +547,36 @@ struct Plan {
 };
 size_t experts_plan_bytes() { return sizeof(Plan); }
 
-// All threads of a workgroup.  token: of a row of h.  to: where the plan goes, or nullptr.
+static_assert(kRouteTokens * kMaxTopK <= 2 * kMaxAdapters, "room");
+
+// All threads of a workgroup.  token: of a row of h.  first: room for the first row of every expert.  to: where the plan goes, or nullptr.
 template <typename WT, int R>
-__device__ __forceinline__ void make_plan(const ExpertsArgs& a, Plan& plan, ExpertMasks& masks, int (&first)[kMaxAdapters],
+__device__ __forceinline__ void make_plan(const ExpertsArgs& a, Plan& plan, ExpertMasks& masks, int (&first)[2 * kMaxAdapters],
                                           uint8_t (&token)[kExpertsMaxTokens * kMaxTopK], Plan* to) {
-    const int lane = threadIdx.x & 63, pairs = a.T * a.k, p = threadIdx.x;   // 512 threads: a pair each
-    const int e = p < pairs ? a.idx[p] : -1, t = p / a.k;
+    const int lane = threadIdx.x & 63, pairs = a.T * a.k, p = threadIdx.x;   // a pair each
+    const int t = p / a.k;
+    int e = -1;
+    if (a.part != nullptr && a.T <= kRouteTokens) {   // two tokens to a wavefront; the first workgroup says how
+        int* const ids = first;   // of kRouteTokens * kMaxTopK pairs, and room for as many
+        for (int i = threadIdx.x >> 6; i < a.T; i += kManyWaves) {
+            int choice;
+            float w;
+            route_token(a, i, lane, choice, w);
+            if (lane < a.k) {
+                ids[i * a.k + lane] = choice;
+                if (to != nullptr) {
+                    a.idx[i * a.k + lane] = choice;
+                    a.w[i * a.k + lane] = w;
+                }
+            }
+        }
+        __syncthreads();
+        if (p < pairs) e = ids[p];
+    } else if (p < pairs) {
+        e = a.idx[p];
+    }
     const bool there = (unsigned)e < (unsigned)a.N;
-    for (int i = threadIdx.x; i < 2 * kMaxAdapters; i += blockDim.x) masks.word[i >> 1][i & 1] = 0;
+    for (int i = threadIdx.x; i < 2 * kMaxAdapters; i += kManyThreads) masks.word[i >> 1][i & 1] = 0;
     __syncthreads();
     if (there) atomicOr(&masks.word[e][t >> 5], 1u << (t & 31));
     __syncthreads();
@@ -561,7 +601,7 @@ __device__ __forceinline__ void make_plan(const ExpertsArgs& a, Plan& plan, Expe
     if (p < pairs) plan.row[p] = (int16_t)row;
     __syncthreads();
     if (to != nullptr)
-        for (int i = threadIdx.x; i < (int)(sizeof(Plan) / 4); i += blockDim.x) reinterpret_cast<uint32_t*>(to)[i] = reinterpret_cast<const uint32_t*>(&plan)[i];
+        for (int i = threadIdx.x; i < (int)(sizeof(Plan) / 4); i += kManyThreads) reinterpret_cast<uint32_t*>(to)[i] = reinterpret_cast<const uint32_t*>(&plan)[i];
 }
 struct Block { int e, count, first; };
 __device__ __forceinline__ Block unpack_block(uint32_t v) {
@@ -569,8 +609,17 @@ __device__ __forceinline__ Block unpack_block(uint32_t v) {
     return {(int)(u & 255), (int)(u >> 8 & 255), (int)(u >> 16)};
 }
 
+// A slot with room for the rows of MOST wavefronts, and as many of them as LDS has room for
+template <typename WT, int TB, int MOST>
+constexpr int many_slot_bytes() { return MOST * 2 * WT::kBlockBytes + TB * 16 * kTokenBytes<WT>; }
+constexpr int kManyRings = 160 * 1024 - 2048;   // what the plan leaves
+template <typename WT, int TB, int MOST>
+constexpr int many_depth() { return kManyRings / many_slot_bytes<WT, TB, MOST>() < 8 ? kManyRings / many_slot_bytes<WT, TB, MOST>() : 8; }
 template <typename WT, int TB>
-constexpr int many_slot_bytes() { return kManyWaves * 2 * WT::kBlockBytes + TB * 16 * kTokenBytes<WT>; }
+constexpr int many_lds() {
+    constexpr int a = many_depth<WT, TB, 4>() * many_slot_bytes<WT, TB, 4>(), b = many_depth<WT, TB, 8>() * many_slot_bytes<WT, TB, 8>();
+    return a > b ? a : b;
+}
 
 // The rings of gate and up rows as one operand of two blocks
 template <typename WT>
@@ -593,35 +642,24 @@ struct PairRing {
 // The second 16 tokens are multiplied whether there are any or not: with a branch around their MFMAs the compiler moves accumulators right behind
 // the branch and leaves out the wait states for it (ROCm 7.2; tests/test_experts_host.py looks for that).  For the same reason wavefronts
 // without channels, which only load tokens, have a loop of their own.
-// UP: channels of h from the rows of x, the first launch; otherwise channels of y from those of h
-template <typename WT, bool UP, int TB, int D>
-__global__ __launch_bounds__(kManyWaves * 64) void experts_many_kernel(const ExpertsArgs a) {
-    constexpr int WV = kManyWaves, R = TB * 16, RB = 2, kSlot = many_slot_bytes<WT, TB>(), kRowsPer = TokenPiece<WT>::kRows;
+// UP: channels of h from the rows of x, the first launch; otherwise channels of y from those of h.  MOST: of the wavefronts that have channels,
+// 4 or 8: up to 4, which have the shorter K tiles, run on deeper rings.
+template <typename WT, bool UP, int TB, int MOST>
+__device__ __forceinline__ void many_tiles(const ExpertsArgs& a, const Plan& plan, const uint8_t (&token)[kExpertsMaxTokens * kMaxTopK],
+                                           unsigned char* smem, int waves) {
+    constexpr int WV = kManyWaves, R = TB * 16, RB = 2, kSlot = many_slot_bytes<WT, TB, MOST>(), D = many_depth<WT, TB, MOST>();
+    constexpr int kTokens = MOST * RB * WT::kBlockBytes, kRowsPer = TokenPiece<WT>::kRows;   // where the tokens' rows lie in a slot
     constexpr int PIECES = R / kRowsPer, NP = PIECES < WV ? 1 : PIECES / WV, NL = RB * (2 + WT::kScales) + NP;
     constexpr int CW = UP ? 16 : 32;   // channels of a wavefront
     static_assert(D >= 3 && (D - 2) * NL < 64, "vmcnt");
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    __shared__ Plan plan;
-    __shared__ uint8_t token[kExpertsMaxTokens * kMaxTopK];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l15 = lane & 15, kq = lane >> 4;
-    if constexpr (UP) {
-        // masks and the experts' first rows are in the rings' place
-        make_plan<WT, R>(a, plan, *reinterpret_cast<ExpertMasks*>(smem), *reinterpret_cast<int(*)[kMaxAdapters]>(smem + sizeof(ExpertMasks)), token,
-                         blockIdx.x == 0 ? reinterpret_cast<Plan*>(a.plan) : nullptr);
-        __syncthreads();
-    } else {
-        for (int i = tid; i < (int)(offsetof(Plan, row) / 4); i += WV * 64)
-            reinterpret_cast<uint32_t*>(&plan)[i] = reinterpret_cast<const uint32_t*>(a.plan)[i];
-        __syncthreads();
-    }
     const int K = UP ? a.d : a.f, C = UP ? a.f : a.d;   // inputs, channels
-    const int waves = __builtin_amdgcn_readfirstlane(UP ? plan.up_waves : plan.down_waves);
     const int splits = UP ? 1 : __builtin_amdgcn_readfirstlane(plan.splits);
     const int bytes = WT::row_bytes(K), nk = ceil_div(bytes, 128), per = ceil_div(nk, splits);
     const int nb = __builtin_amdgcn_readfirstlane(plan.blocks) * splits, total = nb * ceil_div(C, waves * CW);   // 0: no token has an expert
     // workgroups: as many on every XCD, each with the same number of items but for some that have one less
-    const int G = ceil_div(total, max(ceil_div(total, (int)gridDim.x), 1));
+    const int G = ceil_div(total, max(ceil_div(total, kManyGroups), 1));
     if (total == 0 || (int)blockIdx.x >= G) return;
     const int start = xcd_order(blockIdx.x, G);
 
@@ -646,16 +684,15 @@ __global__ __launch_bounds__(kManyWaves * 64) void experts_many_kernel(const Exp
         if constexpr (UP) {
             const uint8_t* W = a.W1 + ((size_t)m.b.e * 2 * a.f + c0) * bytes;
             const uint8_t* S = WT::kScales ? a.s1 + (size_t)m.b.e * mx4_scale_bytes(2 * a.f, a.d) : nullptr;
-            ring.g.point(W, S, 2 * a.f, c0, n, bytes);
-            ring.u.point(W + (size_t)a.f * bytes, S, 2 * a.f, a.f + c0, n, bytes);
+            ring.g.point(W, S, 2 * a.f, c0, n);
+            ring.u.point(W + (size_t)a.f * bytes, S, 2 * a.f, a.f + c0, n);
         } else {
-            ring.point(a.W2 + ((size_t)m.b.e * a.d + c0) * bytes, WT::kScales ? a.s2 + (size_t)m.b.e * mx4_scale_bytes(a.d, a.f) : nullptr, a.d, c0, n,
-                       bytes);
+            ring.point(a.W2 + ((size_t)m.b.e * a.d + c0) * bytes, WT::kScales ? a.s2 + (size_t)m.b.e * mx4_scale_bytes(a.d, a.f) : nullptr, a.d, c0, n);
         }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int r = piece[i].row;
-            const uint32_t row = UP ? (r < m.b.count ? token[m.b.first + r] : 0) : (uint32_t)(m.b.first + r);
+            const uint32_t row = UP ? token[m.b.first + min(r, m.b.count - 1)] : (uint32_t)(m.b.first + r);
             piece[i].point(r < m.b.count ? row * (uint32_t)K * 2u : kOutside);
         }
     };
@@ -669,7 +706,7 @@ __global__ __launch_bounds__(kManyWaves * 64) void experts_many_kernel(const Exp
         }
 #pragma unroll
         for (int i = 0; i < NP; ++i)
-            piece[i].request(rows, slot + WV * RB * WT::kBlockBytes, first_row(i), req_kt, req_end, (uint32_t)K * 2u);
+            piece[i].request(rows, slot + kTokens, first_row(i), req_kt, req_end, (uint32_t)K * 2u);
         if (++req_kt >= req_end && req_end > 0) {
             req_item += G;
             if (req_item < total) point();
@@ -703,23 +740,28 @@ __global__ __launch_bounds__(kManyWaves * 64) void experts_many_kernel(const Exp
         for (int kt = m.part * per; kt < end; ++kt) {
             // this wavefront's part of the tile has landed, and so, behind the barrier, the others'; the slot before is read by all
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((D - 2) * NL) : "memory");
-            request(std::true_type{});
             const unsigned char* const slot = smem + at * kSlot;
             at = at + 1 == D ? 0 : at + 1;
             WeightFrags<WT, RB> w;
             w.read(slot + wave * RB * WT::kBlockBytes, kt, lane);
-            const unsigned char* const tokens = slot + WV * RB * WT::kBlockBytes;
+            const unsigned char* const tokens = slot + kTokens;
+            bf16x8 xf[TB][WT::kSteps];
+#pragma unroll
+            for (int i = 0; i < WT::kSteps; ++i)
+#pragma unroll
+                for (int t = 0; t < TB; ++t) xf[t][i] = token_frag<WT>(tokens, t * 16 + l15, kq, i);
+            __builtin_amdgcn_sched_barrier(0);
+            request(std::true_type{});   // while the fragments are on their way
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < WT::kSteps; ++i) {
                 bf16x8 wf[RB];
 #pragma unroll
                 for (int r = 0; r < RB; ++r) wf[r] = w.at(i, r);
 #pragma unroll
-                for (int t = 0; t < TB; ++t) {
-                    const bf16x8 xf = token_frag<WT>(tokens, t * 16 + l15, kq, i);
+                for (int t = 0; t < TB; ++t)
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) acc[t][r] = mfma_bf16(wf[r], xf, acc[t][r]);
-                }
+                    for (int r = 0; r < RB; ++r) acc[t][r] = mfma_bf16(wf[r], xf[t][i], acc[t][r]);
             }
         }
         const int c0 = (m.col * waves + wave) * CW, n = min(CW, C - c0);
@@ -739,6 +781,27 @@ __global__ __launch_bounds__(kManyWaves * 64) void experts_many_kernel(const Exp
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land after the end
+}
+
+template <typename WT, bool UP, int TB>
+__global__ __launch_bounds__(kManyThreads) void experts_many_kernel(const ExpertsArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    __shared__ Plan plan;
+    __shared__ uint8_t token[kExpertsMaxTokens * kMaxTopK];
+    const int tid = threadIdx.x;
+    if constexpr (UP) {
+        // masks and the experts' first rows are in the rings' place
+        make_plan<WT, TB * 16>(a, plan, *reinterpret_cast<ExpertMasks*>(smem), *reinterpret_cast<int(*)[2 * kMaxAdapters]>(smem + sizeof(ExpertMasks)), token,
+                               blockIdx.x == 0 ? reinterpret_cast<Plan*>(a.plan) : nullptr);
+        __syncthreads();
+    } else {
+        for (int i = tid; i < (int)(offsetof(Plan, row) / 4); i += kManyThreads)
+            reinterpret_cast<uint32_t*>(&plan)[i] = reinterpret_cast<const uint32_t*>(a.plan)[i];
+        __syncthreads();
+    }
+    const int waves = __builtin_amdgcn_readfirstlane(UP ? plan.up_waves : plan.down_waves);
+    if (waves <= 4) many_tiles<WT, UP, TB, 4>(a, plan, token, smem, waves);
+    else many_tiles<WT, UP, TB, 8>(a, plan, token, smem, waves);
 }
 
 // out[t] = base[t] + scale * sum_j w[t,j] * y[row of (t, j)], the parts of y added first; a token and 1024 channels to a workgroup
@@ -779,7 +842,6 @@ constexpr int few_down_lds() { return KS * D * few_slot_bytes<WT, 1>(); }
 template <typename WT> constexpr int kFewUpDepth = WT::kScales ? 3 : 4;
 constexpr int kFewDownWaves = 8;
 template <typename WT> constexpr int kFewDownDepth = WT::kScales ? 4 : 5;
-template <typename WT> constexpr int kManyDepth = WT::kScales ? 3 : 4;
 
 template <typename WT>
 static hipError_t launch_few(const ExpertsArgs& a, hipStream_t stream) {
@@ -793,11 +855,11 @@ static hipError_t launch_few(const ExpertsArgs& a, hipStream_t stream) {
 }
 template <typename WT, int TB>
 static hipError_t launch_many(const ExpertsArgs& a, hipStream_t stream) {
-    constexpr int D = kManyDepth<WT>, LDS = D * many_slot_bytes<WT, TB>();
+    constexpr int LDS = many_lds<WT, TB>();
     static_assert(LDS + (int)sizeof(Plan) + kExpertsMaxTokens * kMaxTopK <= 160 * 1024, "LDS");
-    hipError_t e = start(&experts_many_kernel<WT, true, TB, D>, 256, kManyWaves * 64, LDS, a, stream);
+    hipError_t e = start(&experts_many_kernel<WT, true, TB>, kManyGroups, kManyThreads, LDS, a, stream);
     if (e != hipSuccess) return e;
-    e = start(&experts_many_kernel<WT, false, TB, D>, 256, kManyWaves * 64, LDS, a, stream);
+    e = start(&experts_many_kernel<WT, false, TB>, kManyGroups, kManyThreads, LDS, a, stream);
     if (e != hipSuccess) return e;
     experts_sum_kernel<<<dim3(ceil_div(a.d, 1024), a.T), 256, 0, stream>>>(a);
     return hipGetLastError();
@@ -816,7 +878,7 @@ size_t experts_y_bytes(int T, int k, int d) { return T <= kFewTokens ? 0 : (size
 
 size_t experts_part_bytes(int T, int d, int N) { return (size_t)T * gate_slices(d, N) * gate_columns(N) * sizeof(float); }
 
-// the partial logits, and for more than 4 tokens the routing from them
+// the partial logits, and for more than kRouteTokens tokens the routing from them
 hipError_t launch_experts_gate(const ExpertsArgs& a, const float* W_gate, hipStream_t stream) {
     const dim3 grid(gate_slices(a.d, a.N), ceil_div(a.T, kGateTokens));
     const auto go = [&](auto kern) { kern<<<grid, 256, 0, stream>>>(a.x, W_gate, a.T, a.d, a.N, const_cast<float*>(a.part)); };
@@ -826,7 +888,7 @@ hipError_t launch_experts_gate(const ExpertsArgs& a, const float* W_gate, hipStr
         case 32: go(&gate_part_kernel<32>); break;
         default: go(&gate_part_kernel<64>);
     }
-    if (a.T > kFewTokens) experts_route_kernel<<<ceil_div(a.T, 4), 256, 0, stream>>>(a);
+    if (a.T > kRouteTokens) experts_route_kernel<<<ceil_div(a.T, 4), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -838,11 +900,10 @@ static hipError_t init_experts() {   // every kernel that launch_experts may sta
     set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 4, DU>), few_up_lds<WT, 4, DU>());
     set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 1, DU>), few_up_lds<WT, 1, DU>());
     set(reinterpret_cast<const void*>(&experts_few_down_kernel<WT, kFewDownWaves, DD>), few_down_lds<WT, kFewDownWaves, DD>());
-    constexpr int D = kManyDepth<WT>;
-    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, true, 1, D>), D * many_slot_bytes<WT, 1>());
-    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, true, 2, D>), D * many_slot_bytes<WT, 2>());
-    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, false, 1, D>), D * many_slot_bytes<WT, 1>());
-    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, false, 2, D>), D * many_slot_bytes<WT, 2>());
+    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, true, 1>), many_lds<WT, 1>());
+    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, true, 2>), many_lds<WT, 2>());
+    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, false, 1>), many_lds<WT, 1>());
+    set(reinterpret_cast<const void*>(&experts_many_kernel<WT, false, 2>), many_lds<WT, 2>());
     return e;
 }
 hipError_t experts_init_kernels() {
