@@ -201,9 +201,19 @@ struct WeightRing {
             scale_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(uniform(scale + (size_t)(kt >> 1) * ((size_t)all * 16))), 0,
                                                            kt < nk ? (uint32_t)there * 16u : 0u, 0x00020000);
     }
-    __device__ __forceinline__ void request(unsigned char* slot) const {
+    // requested as read once where rows are whole lines; where a K tile's row ends within a line, the next tile reads that line again (second product of 33
+    // tokens of 28 experts, rows of 688 bytes: read once 17.2 us, kept 14.5)
+    __device__ __forceinline__ void request_rows(unsigned char* slot) const {
+        if (bytes % 128 == 0) {
 #pragma unroll
-        for (int j = 0; j < 2 * RB; ++j) rows.template request<kReadOnceI8>(slot, j);
+            for (int j = 0; j < 2 * RB; ++j) rows.template request<kReadOnceI8>(slot, j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 2 * RB; ++j) rows.template request<0>(slot, j);
+        }
+    }
+    __device__ __forceinline__ void request(unsigned char* slot) const {
+        request_rows(slot);
         if constexpr (WT::kScales)
 #pragma unroll
             for (int r = 0; r < RB; ++r) mx4_scale_lds(scale_rsrc, slot + RB * 2048 + r * 256, at_scale + r * 256);
@@ -628,10 +638,8 @@ struct PairRing {
     __device__ __forceinline__ PairRing(int bytes, int lane) : g(bytes, lane), u(bytes, lane) {}
     __device__ __forceinline__ void at_tile(int kt, int nk) { g.at_tile(kt, nk); u.at_tile(kt, nk); }
     __device__ __forceinline__ void request(unsigned char* slot) const {   // as two blocks of one ring lie: rows, rows, scales, scales
-#pragma unroll
-        for (int j = 0; j < 2; ++j) g.rows.template request<kReadOnceI8>(slot, j);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) u.rows.template request<kReadOnceI8>(slot + 2048, j);
+        g.request_rows(slot);
+        u.request_rows(slot + 2048);
         if constexpr (WT::kScales) {
             mx4_scale_lds(g.scale_rsrc, slot + 4096, g.at_scale);
             mx4_scale_lds(u.scale_rsrc, slot + 4352, u.at_scale);
