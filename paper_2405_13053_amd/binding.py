@@ -619,12 +619,13 @@ def quantize_mx4(x, out=None):
     """meteora_quantize_mx4: (q[rows,d/2] uint8, scale[ceil(d/512),rows,16] uint8), the rows of x as 4-bit values with a power of two
     for every 32 inputs.  `out` = the two result tensors if the caller has them already."""
     rows, d = x.shape
-    _chk(x, "x")
+    shape = mx4_scale_shape(rows, d)
     if out is None:
-        out = (torch.empty((rows, d // 2), dtype=torch.uint8, device=x.device),
-               torch.empty(mx4_scale_shape(rows, d), dtype=torch.uint8, device=x.device))
-    q, scale = out
-    _chk(q, "q", torch.uint8, (rows, d // 2)); _chk(scale, "scale", torch.uint8, mx4_scale_shape(rows, d))
+        _chk(x, "x")
+        q, scale = x.new_empty((rows, d // 2), dtype=torch.uint8), x.new_empty(shape, dtype=torch.uint8)
+    else:
+        q, scale = out
+        _chk(x, "x"); _chk(q, "q", torch.uint8, (rows, d // 2)); _chk(scale, "scale", torch.uint8, shape)
     _chk_device(x, q, scale)
     st = load_library().meteora_quantize_mx4(_pe(x), rows, d, _dt(x), _pe(q), _pe(scale), _stream())
     if st != 0:
@@ -638,8 +639,11 @@ def dequantize_mx4(q, scale, transpose: bool = False, out: Optional[torch.Tensor
     rows, d = q.shape[0], q.shape[1] * 2
     shape = (d, rows) if transpose else (rows, d)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=q.device)
-    _chk(q, "q", torch.uint8); _chk(scale, "scale", torch.uint8, mx4_scale_shape(rows, d)); _chk(out, "out", None, shape)
+        out = q.new_empty(shape, dtype=dtype)
+    # written out, as in linear_forward
+    if not (q.is_cuda and q.is_contiguous() and q.dtype == torch.uint8 and scale.dtype == torch.uint8 and scale.is_contiguous() and
+            scale.shape == ((d + 511) // 512, rows, 16) and out.is_contiguous() and out.shape == shape):
+        _chk(q, "q", torch.uint8); _chk(scale, "scale", torch.uint8, mx4_scale_shape(rows, d)); _chk(out, "out", None, shape)
     _chk_device(q, scale, out)
     st = load_library().meteora_dequantize_mx4(_pe(q), _pe(scale), rows, d, _dt(out), int(transpose), _pe(out), _stream())
     if st != 0:

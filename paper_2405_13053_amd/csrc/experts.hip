@@ -186,7 +186,7 @@ struct WeightRing {
         point(W, scale, all, row0, n);
     }
     __device__ __forceinline__ WeightRing(int bytes, int lane)
-        : rows(nullptr, 0, (uint32_t)bytes, lane), bytes(bytes), at_scale((uint32_t)(lane & 15) * 16 + (lane >> 4) * 4) {}
+        : rows(nullptr, 0, (uint32_t)bytes, lane), W(nullptr), scale(nullptr), n(0), all(0), bytes(bytes), at_scale((uint32_t)(lane & 15) * 16 + (lane >> 4) * 4) {}
     __device__ __forceinline__ void point(const uint8_t* w, const uint8_t* s, int of, int row0, int count) {
         W = w;
         n = count;
@@ -300,15 +300,56 @@ struct FewTile {   // a wavefront's slot: W, then the four rows
     static constexpr int kPieces = kFewTokens * kTokenBytes<WT> > 1024 ? 2 : 1, kLoads = WeightRing<WT, RB>::kLoads + kPieces;
 };
 
-template <typename WT, int KS, int D>
-__global__ __launch_bounds__(256) void experts_few_up_kernel(const ExpertsArgs a) {
-    constexpr int RB = 2, NL = FewTile<WT, RB>::kLoads, NP = FewTile<WT, RB>::kPieces, kSlot = few_slot_bytes<WT, RB>();
-    constexpr int CH = 16 * (4 / KS);   // channels of a workgroup
+// The rings of gate and up rows as one operand of two blocks
+template <typename WT>
+struct PairRing {
+    WeightRing<WT, 1> g, u;
+    __device__ __forceinline__ PairRing(int bytes, int lane) : g(bytes, lane), u(bytes, lane) {}
+    __device__ __forceinline__ void at_tile(int kt, int nk) { g.at_tile(kt, nk); u.at_tile(kt, nk); }
+    __device__ __forceinline__ void request(unsigned char* slot) const {   // as two blocks of one ring lie: rows, rows, scales, scales
+        g.request_rows(slot);
+        u.request_rows(slot + 2048);
+        if constexpr (WT::kScales) {
+            mx4_scale_lds(g.scale_rsrc, slot + 4096, g.at_scale);
+            mx4_scale_lds(u.scale_rsrc, slot + 4352, u.at_scale);
+        }
+    }
+};
+
+// First product.  The tokens' rows, all of x, are in LDS for the whole workgroup; a unit is 16 channels of one expert, KS wavefronts to it, which split K,
+// and the groups of a workgroup's 8 wavefronts go through the units with the loads of the next one already on their way.
+constexpr int kFewWaves = 8, kFewGroups = 256, kFewDepth = 3, kFewRowsMost = 34816;   // bytes of the rows in LDS
+template <typename WT>
+__host__ __device__ constexpr int few_row_bytes(int d) {   // whole pieces of 1024 bytes, and K tiles; rows start 4 banks apart
+    return (ceil_div(WT::row_bytes(d), 128) * kTokenBytes<WT> + 1023) / 1024 * 1024 + 16;
+}
+template <typename WT>
+constexpr int few_up_lds(int rows_bytes, bool sums) { return kFewWaves * (kFewDepth * 2 * WT::kBlockBytes + (sums ? 2048 : 0)) + rows_bytes; }
+static_assert(few_up_lds<Mx4Weights>(kFewRowsMost, true) + 1024 <= 160 * 1024, "LDS");
+
+template <typename WT, int KS>
+__global__ __launch_bounds__(kFewWaves * 64) void experts_few_up_kernel(const ExpertsArgs a) {
+    constexpr int D = kFewDepth, NL = 2 * (2 + WT::kScales), kSlot = 2 * WT::kBlockBytes, GROUPS = kFewWaves / KS;
     static_assert((D - 1) * NL < 64, "vmcnt");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     __shared__ ExpertMasks masks;
+    __shared__ uint32_t list[kMaxAdapters];   // the experts in use: id | tokens << 8 | first row of h << 16
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l15 = lane & 15, kq = lane >> 4;
+    unsigned char* const ring = smem + wave * D * kSlot;
+    f32x4* const sums = reinterpret_cast<f32x4*>(smem + kFewWaves * D * kSlot);
+    unsigned char* const rows = smem + kFewWaves * (D * kSlot + (KS > 1 ? 2048 : 0));
+    const int row_bytes = few_row_bytes<WT>(a.d);
+    {   // x, before anything is known of the routing
+        const auto x = token_rsrc(a.x, a.T, a.d);
+        const int per = row_bytes / 1024;
+        for (int p = wave; p < a.T * per; p += kFewWaves) {
+            const int t = p / per, c = (p - t * per) * 1024 + lane * 16;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                x, (__attribute__((address_space(3))) void*)(rows + t * row_bytes + (p - t * per) * 1024), 16,
+                c < a.d * 2 ? (uint32_t)t * (uint32_t)a.d * 2u + (uint32_t)c : kOutside, 0, 0, 0);   // zeros behind a row
+        }
+    }
     if (a.part != nullptr) {   // every workgroup routes; the first one says how
         int e = -1;
         float w = 0.f;
@@ -328,84 +369,100 @@ __global__ __launch_bounds__(256) void experts_few_up_kernel(const ExpertsArgs a
     }
     const uint64_t mine = lane < a.N ? mask_of(masks, lane) : 0;
     const uint64_t active = __ballot(mine != 0);
-    const int tiles = ceil_div(a.f, CH), total = __popcll(active) * tiles;
-    if ((int)blockIdx.x >= total) return;
-    const int id = xcd_order(blockIdx.x, total);
-    const int which = id / tiles;
-    const int e = __builtin_amdgcn_readfirstlane(__ffsll(__ballot(mine != 0 && rank_in(active, lane) == which)) - 1);
-    const int sums = wave_sums(__popcll(mine));
-    const int first = __builtin_amdgcn_readfirstlane(__shfl(sums, e) - __popcll(mask_of(masks, e)));   // row of h
-    const uint32_t tokens = masks.word[e][0];
-    const int c0 = (id - which * tiles) * CH + (KS == 1 ? wave * 16 : 0), n = min(16, a.f - c0);   // this wavefront's channels; n <= 0: none
-    unsigned char* const ring = smem + wave * D * kSlot;
+    if (wave == 0) {
+        const int n = __popcll(mine), at = wave_sums(n) - n;
+        if (n != 0) list[rank_in(active, lane)] = (uint32_t)lane | (uint32_t)mine << 8 | (uint32_t)at << 16;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wavefront's part of x
+    __syncthreads();
 
-    const int bytes = WT::row_bytes(a.d), nk = ceil_div(bytes, 128), kp = KS == 1 ? 0 : wave;
-    const int steps = n > 0 && kp < nk ? (nk - 1 - kp) / KS + 1 : 0;
-    const uint8_t* W = a.W1 + ((size_t)e * 2 * a.f + c0) * bytes;
-    const uint8_t* S = WT::kScales ? a.s1 + (size_t)e * mx4_scale_bytes(2 * a.f, a.d) : nullptr;
-    WeightRing<WT, 1> g(W, S, 2 * a.f, c0, max(n, 0), bytes, lane), u(W + (size_t)a.f * bytes, S, 2 * a.f, a.f + c0, max(n, 0), bytes, lane);
-    const auto x = token_rsrc(a.x, a.T, a.d);
-    TokenPiece<WT> piece[NP];
-#pragma unroll
-    for (int i = 0; i < NP; ++i) piece[i].set(i * TokenPiece<WT>::kRows, lane);
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-        piece[i].point(piece[i].row < kFewTokens && (tokens >> piece[i].row & 1) ? (uint32_t)piece[i].row * (uint32_t)a.d * 2u : kOutside);
-    auto request = [&](unsigned char* slot, int kt) {
-        const int end = n > 0 ? nk : 0;
-        g.at_tile(kt, end);
-        u.at_tile(kt, end);
-        g.request(slot);
-        u.request(slot + WT::kBlockBytes);
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-            piece[i].request(x, slot + 2 * WT::kBlockBytes, i * TokenPiece<WT>::kRows, kt, end, (uint32_t)a.d * 2u);
+    const int group = wave / KS, kp = wave % KS, each = ceil_div(a.f, 16), total = __popcll(active) * each;
+    const int slot0 = xcd_order(blockIdx.x, kFewGroups), stride = kFewGroups * GROUPS;   // a unit to every workgroup, then a second one
+    const int mine_at = group * kFewGroups;
+    const int bytes = WT::row_bytes(a.d), nk = ceil_div(bytes, 128);
+    struct Unit { int e, first, c0, n; uint32_t tokens; };
+    auto unit_at = [&](int u) {
+        const int i = u / each, c0 = (u - i * each) * 16;
+        const uint32_t v = (uint32_t)__builtin_amdgcn_readfirstlane((int)list[i]);
+        return Unit{(int)(v & 255), (int)(v >> 16), c0, min(16, a.f - c0), v >> 8 & 255};
+    };
+    PairRing<WT> w(bytes, lane);
+    int req_u = slot0 + mine_at, req_kt = kp, req_end = 0, req_at = 0;   // req_end: 0 where there are no more
+    auto point = [&] {
+        const Unit m = unit_at(req_u);
+        const uint8_t* W = a.W1 + ((size_t)m.e * 2 * a.f + m.c0) * bytes;
+        const uint8_t* S = WT::kScales ? a.s1 + (size_t)m.e * mx4_scale_bytes(2 * a.f, a.d) : nullptr;
+        w.g.point(W, S, 2 * a.f, m.c0, m.n);
+        w.u.point(W + (size_t)a.f * bytes, S, 2 * a.f, a.f + m.c0, m.n);
+        req_end = nk;
+    };
+    if (req_u < total && kp < nk) point();
+    auto request = [&] {
+        w.at_tile(req_kt, req_end);
+        w.request(ring + req_at * kSlot);
+        req_at = req_at + 1 == D ? 0 : req_at + 1;
+        req_kt += KS;
+        if (req_kt >= req_end && req_end > 0) {
+            req_kt = kp;
+            req_u += stride;
+            if (req_u < total) point();
+            else req_end = 0;
+        }
     };
 #pragma unroll
-    for (int i = 0; i < D; ++i) request(ring + i * kSlot, kp + i * KS);
-    f32x4 ag = {0.f, 0.f, 0.f, 0.f}, au = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < D; ++i) request();
+    const unsigned char* const mine_row = rows + (l15 % a.T) * row_bytes;   // columns past the last token: another's, not kept
     int at = 0;
-    for (int s = 0; s < steps; ++s) {
-        const int kt = kp + s * KS;
-        unsigned char* const slot = ring + at * kSlot;
-        at = at + 1 == D ? 0 : at + 1;
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * NL) : "memory");
-        WeightFrags<WT, 1> wg, wu;
-        wg.read(slot, kt, lane);
-        wu.read(slot + WT::kBlockBytes, kt, lane);
-        bf16x8 xf[WT::kSteps];
+    for (int u0 = slot0; u0 < total; u0 += stride) {   // the same rounds for all groups
+        const int u = u0 + mine_at;
+        f32x4 ag = {0.f, 0.f, 0.f, 0.f}, au = {0.f, 0.f, 0.f, 0.f};
+        const int end = u < total ? nk : 0;
+        for (int kt = kp; kt < end; kt += KS) {
+            unsigned char* const slot = ring + at * kSlot;
+            at = at + 1 == D ? 0 : at + 1;
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * NL) : "memory");
+            WeightFrags<WT, 2> wf;
+            wf.read(slot, kt, lane);
+            bf16x8 xf[WT::kSteps];
 #pragma unroll
-        for (int i = 0; i < WT::kSteps; ++i) xf[i] = token_frag<WT>(slot + 2 * WT::kBlockBytes, l15 & (kFewTokens - 1), kq, i);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot is read
-        request(slot, kt + D * KS);
+            for (int i = 0; i < WT::kSteps; ++i) {
+                const int c = WT::kScales ? ((i >> 2) * 4 + kq) * 4 + (i & 3) : i * 4 + kq;
+                xf[i] = *reinterpret_cast<const bf16x8*>(mine_row + kt * kTokenBytes<WT> + c * 16);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot is read
+            request();
 #pragma unroll
-        for (int i = 0; i < WT::kSteps; ++i) {
-            ag = mfma_bf16(wg.at(i, 0), xf[i], ag);
-            au = mfma_bf16(wu.at(i, 0), xf[i], au);
+            for (int i = 0; i < WT::kSteps; ++i) {
+                ag = mfma_bf16(wf.at(i, 0), xf[i], ag);
+                au = mfma_bf16(wf.at(i, 1), xf[i], au);
+            }
         }
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land in what follows, or after the end
-    if constexpr (KS > 1) {
-        __syncthreads();
-        f32x4* part = reinterpret_cast<f32x4*>(smem);
-        part[wave * 128 + lane] = ag;
-        part[wave * 128 + 64 + lane] = au;
-        __syncthreads();
-        if (wave != 0) return;
+        if constexpr (KS > 1) {
+            sums[wave * 128 + lane] = ag;
+            sums[wave * 128 + 64 + lane] = au;
+            __syncthreads();
+            if (kp == 0) {
 #pragma unroll
-        for (int v = 1; v < KS; ++v) {
-            ag += part[v * 128 + lane];
-            au += part[v * 128 + 64 + lane];
+                for (int v = 1; v < KS; ++v) {
+                    ag += sums[(wave + v) * 128 + lane];
+                    au += sums[(wave + v) * 128 + 64 + lane];
+                }
+            }
         }
+        if (kp == 0 && u < total) {
+            const Unit m = unit_at(u);
+            if (l15 < a.T && (m.tokens >> l15 & 1) && kq * 4 < m.n)   // f % 8 == 0
+                store_h(a.h + (size_t)(m.first + rank_in(m.tokens, l15)) * a.f + m.c0 + kq * 4, ag, au);
+        }
+        if constexpr (KS > 1) __syncthreads();   // the sums are read
     }
-    const int t = l15;
-    if (t < kFewTokens && (tokens >> t & 1) && kq * 4 < n)   // f % 8 == 0
-        store_h(a.h + (size_t)(first + rank_in(tokens, t)) * a.f + c0 + kq * 4, ag, au);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land after the end
 }
 
-// The wavefronts split K (KS of them); sequence numbers run over the experts in use and their K tiles.
+// Second product.  The wavefronts split K (KS of them), and where there are few channels so do `splits` workgroups, whose sums then leave as y[part][T][d];
+// sequence numbers run over the experts in use and their K tiles.
 template <typename WT, int KS, int D>
-__global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const ExpertsArgs a) {
+__global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const ExpertsArgs a, int splits) {
     constexpr int NL = FewTile<WT, 1>::kLoads, NP = FewTile<WT, 1>::kPieces, kSlot = few_slot_bytes<WT, 1>();
     static_assert((D - 1) * NL < 64, "vmcnt");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -439,16 +496,17 @@ __global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const Experts
         }
     }
     __syncthreads();
-    const int c0 = xcd_order(blockIdx.x, gridDim.x) * 16, n = min(16, a.d - c0);
+    const int id = xcd_order(blockIdx.x, gridDim.x), part = id % splits, c0 = id / splits * 16, n = min(16, a.d - c0);
     unsigned char* const ring = smem + wave * D * kSlot;
-    const int bytes = WT::row_bytes(a.f), nk = ceil_div(bytes, 128);
-    const int per = wave < nk ? (nk - 1 - wave) / KS + 1 : 0, steps = per * count;
+    const int bytes = WT::row_bytes(a.f), nk = ceil_div(bytes, 128), share = ceil_div(nk, splits);
+    const int kt0 = part * share + wave, kt1 = min(nk, part * share + share);   // this wavefront's: every KS-th of an expert's
+    const int per = kt0 < kt1 ? (kt1 - 1 - kt0) / KS + 1 : 0, steps = per * count;
     const auto h = token_rsrc(a.h, a.T * a.k, a.f);
     WeightRing<WT, 1> w(a.W2, a.s2, a.d, c0, n, bytes, lane);
     TokenPiece<WT> piece[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) piece[i].set(i * TokenPiece<WT>::kRows, lane);
-    int req_i = 0, req_kt = wave;   // next request: expert of the list, K tile
+    int req_i = 0, req_kt = kt0;   // next request: expert of the list, K tile
     auto point = [&](int i) {
         const int e = __builtin_amdgcn_readfirstlane(list[i][0]), row = __builtin_amdgcn_readfirstlane(list[i][1]);
         const uint32_t tokens = masks.word[e][0];
@@ -461,22 +519,22 @@ __global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const Experts
     };
     if (count > 0) point(0);
     auto request = [&](unsigned char* slot) {
-        const int end = req_i < count && per > 0 ? nk : 0;
+        const int end = req_i < count && per > 0 ? kt1 : 0;
         w.at_tile(req_kt, end);
         w.request(slot);
 #pragma unroll
         for (int p = 0; p < NP; ++p)
             piece[p].request(h, slot + WT::kBlockBytes, p * TokenPiece<WT>::kRows, req_kt, end, (uint32_t)a.f * 2u);
         req_kt += KS;
-        if (req_kt >= nk && req_i < count) {
-            req_kt = wave;
+        if (req_kt >= kt1 && req_i < count) {
+            req_kt = kt0;
             if (++req_i < count) point(req_i);
         }
     };
 #pragma unroll
     for (int i = 0; i < D; ++i) request(ring + i * kSlot);
     f32x4 acc = {0.f, 0.f, 0.f, 0.f}, total = {0.f, 0.f, 0.f, 0.f};
-    int at = 0, i = 0, kt = wave;
+    int at = 0, i = 0, kt = kt0;
     for (int s = 0; s < steps; ++s) {
         unsigned char* const slot = ring + at * kSlot;
         at = at + 1 == D ? 0 : at + 1;
@@ -491,7 +549,7 @@ __global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const Experts
 #pragma unroll
         for (int j = 0; j < WT::kSteps; ++j) acc = mfma_bf16(wf.at(j, 0), xf[j], acc);
         kt += KS;
-        if (kt >= nk) {   // the expert's last: its sum with the token's weight
+        if (kt >= kt1) {   // the expert's last: its sum with the token's weight
             const int t = l15 & (kFewTokens - 1);
             const float wt = weight[i][t];
             const bool routed = masks.word[list[i][0]][0] >> t & 1;   // a column of zeros may meet a NaN in the weights
@@ -500,23 +558,38 @@ __global__ __launch_bounds__(KS * 64) void experts_few_down_kernel(const Experts
                 total[c] += routed ? wt * acc[c] : 0.f;
                 acc[c] = 0.f;
             }
-            kt = wave;
+            kt = kt0;
             ++i;
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land in what follows
     __syncthreads();
-    f32x4* part = reinterpret_cast<f32x4*>(smem);
-    part[wave * 64 + lane] = total;
+    f32x4* const sums = reinterpret_cast<f32x4*>(smem);
+    sums[wave * 64 + lane] = total;
     __syncthreads();
     if (wave != 0) return;
 #pragma unroll
-    for (int v = 1; v < KS; ++v) total += part[v * 64 + lane];
+    for (int v = 1; v < KS; ++v) total += sums[v * 64 + lane];
     if (l15 >= a.T || l15 >= kFewTokens || kq * 4 >= n) return;
     const size_t o = (size_t)l15 * a.d + c0 + kq * 4;
+    if (splits > 1) {
+        *reinterpret_cast<f32x4*>(a.y + (size_t)part * a.T * a.d + o) = total;
+        return;
+    }
     float v[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) v[c] = a.scale * total[c] + (a.base != nullptr ? (float)a.base[o + c] : 0.f);
+    *reinterpret_cast<uint2*>(a.out + o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+}
+
+__global__ __launch_bounds__(256) void experts_few_sum_kernel(const ExpertsArgs a, int splits) {   // 4 channels of a token to a thread
+    const size_t o = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, all = (size_t)a.T * a.d;
+    if (o >= all) return;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(a.y + o);
+    for (int p = 1; p < splits; ++p) sum += *reinterpret_cast<const f32x4*>(a.y + (size_t)p * all + o);
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a.scale * sum[i] + (a.base != nullptr ? (float)a.base[o + i] : 0.f);
     *reinterpret_cast<uint2*>(a.out + o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
 }
 
@@ -630,22 +703,6 @@ constexpr int many_lds() {
     constexpr int a = many_depth<WT, TB, 4>() * many_slot_bytes<WT, TB, 4>(), b = many_depth<WT, TB, 8>() * many_slot_bytes<WT, TB, 8>();
     return a > b ? a : b;
 }
-
-// The rings of gate and up rows as one operand of two blocks
-template <typename WT>
-struct PairRing {
-    WeightRing<WT, 1> g, u;
-    __device__ __forceinline__ PairRing(int bytes, int lane) : g(bytes, lane), u(bytes, lane) {}
-    __device__ __forceinline__ void at_tile(int kt, int nk) { g.at_tile(kt, nk); u.at_tile(kt, nk); }
-    __device__ __forceinline__ void request(unsigned char* slot) const {   // as two blocks of one ring lie: rows, rows, scales, scales
-        g.request_rows(slot);
-        u.request_rows(slot + 2048);
-        if constexpr (WT::kScales) {
-            mx4_scale_lds(g.scale_rsrc, slot + 4096, g.at_scale);
-            mx4_scale_lds(u.scale_rsrc, slot + 4352, u.at_scale);
-        }
-    }
-};
 
 // The second 16 tokens are multiplied whether there are any or not: with a branch around their MFMAs the compiler moves accumulators right behind
 // the branch and leaves out the wait states for it (ROCm 7.2; tests/test_experts_host.py looks for that).  For the same reason wavefronts
@@ -844,22 +901,55 @@ static hipError_t start(K kern, int grid, int threads, int lds, const ExpertsArg
     return hipGetLastError();
 }
 template <typename WT, int KS, int D>
-constexpr int few_up_lds() { return 4 * D * few_slot_bytes<WT, 2>(); }
-template <typename WT, int KS, int D>
 constexpr int few_down_lds() { return KS * D * few_slot_bytes<WT, 1>(); }
-template <typename WT> constexpr int kFewUpDepth = WT::kScales ? 3 : 4;
 constexpr int kFewDownWaves = 8;
 template <typename WT> constexpr int kFewDownDepth = WT::kScales ? 4 : 5;
 
+// Wavefronts to a unit of the first product: rounds * K tiles of each, and a round's sum in LDS as half a K tile.
+static int few_up_split(int units, int nk) {
+    int best = 1;
+    float least = 0.f;
+    for (int KS = 1; KS <= kFewWaves; KS *= 2) {
+        const float us = (float)ceil_div(units, kFewGroups * kFewWaves / KS) * ((float)ceil_div(nk, KS) + (KS > 1 ? 0.5f : 0.f));
+        if (KS == 1 || us < least) { least = us; best = KS; }
+    }
+    return best;
+}
+// Workgroups to a tile of the second product: rounds * K tiles of a wavefront, 0.4 us each, and a launch of 3.5 us that adds the parts
+static int few_down_split(int tiles, int experts, int nk) {
+    int best = 1;
+    float least = 0.f;
+    for (int S = 1; S <= kManySplits; S *= 2) {
+        const float us = (float)ceil_div(tiles * S, 256) * (float)(experts * ceil_div(ceil_div(nk, S), kFewDownWaves)) * 0.4f + (S > 1 ? 3.5f : 0.f);
+        if (S > 1 && nk < kFewDownWaves * S) break;
+        if (S == 1 || us < least) { least = us; best = S; }
+    }
+    return best;
+}
+template <typename WT>
+static bool few_fits(const ExpertsArgs& a) { return a.T <= kFewTokens && a.T * few_row_bytes<WT>(a.d) <= kFewRowsMost; }
+
 template <typename WT>
 static hipError_t launch_few(const ExpertsArgs& a, hipStream_t stream) {
-    constexpr int DU = kFewUpDepth<WT>, DD = kFewDownDepth<WT>;
+    constexpr int DD = kFewDownDepth<WT>;
     const int most = a.T * a.k < a.N ? a.T * a.k : a.N;   // experts in use
-    const bool split = (int64_t)most * ceil_div(a.f, 64) < 256;
-    const hipError_t e = split ? start(&experts_few_up_kernel<WT, 4, DU>, most * ceil_div(a.f, 16), 256, few_up_lds<WT, 4, DU>(), a, stream)
-                               : start(&experts_few_up_kernel<WT, 1, DU>, most * ceil_div(a.f, 64), 256, few_up_lds<WT, 1, DU>(), a, stream);
+    const int rows = a.T * few_row_bytes<WT>(a.d), KS = few_up_split(most * ceil_div(a.f, 16), ceil_div(WT::row_bytes(a.d), 128));
+    const auto up = [&](auto kern) {
+        const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(kern), few_up_lds<WT>(kFewRowsMost, KS > 1));
+        if (e != hipSuccess) return e;
+        kern<<<kFewGroups, kFewWaves * 64, few_up_lds<WT>(rows, KS > 1), stream>>>(a);
+        return hipGetLastError();
+    };
+    const hipError_t e = KS == 1 ? up(&experts_few_up_kernel<WT, 1>) : KS == 2 ? up(&experts_few_up_kernel<WT, 2>)
+                       : KS == 4 ? up(&experts_few_up_kernel<WT, 4>) : up(&experts_few_up_kernel<WT, 8>);
     if (e != hipSuccess) return e;
-    return start(&experts_few_down_kernel<WT, kFewDownWaves, DD>, ceil_div(a.d, 16), kFewDownWaves * 64, few_down_lds<WT, kFewDownWaves, DD>(), a, stream);
+    const int tiles = ceil_div(a.d, 16), splits = few_down_split(tiles, most, ceil_div(WT::row_bytes(a.f), 128));
+    const auto down = &experts_few_down_kernel<WT, kFewDownWaves, DD>;
+    const hipError_t f = ensure_lds_limit(reinterpret_cast<const void*>(down), few_down_lds<WT, kFewDownWaves, DD>());
+    if (f != hipSuccess) return f;
+    down<<<tiles * splits, kFewDownWaves * 64, few_down_lds<WT, kFewDownWaves, DD>(), stream>>>(a, splits);
+    if (splits > 1) experts_few_sum_kernel<<<ceil_div(a.T * a.d, 1024), 256, 0, stream>>>(a, splits);
+    return hipGetLastError();
 }
 template <typename WT, int TB>
 static hipError_t launch_many(const ExpertsArgs& a, hipStream_t stream) {
@@ -874,7 +964,7 @@ static hipError_t launch_many(const ExpertsArgs& a, hipStream_t stream) {
 }
 template <typename WT>
 static hipError_t launch(const ExpertsArgs& a, hipStream_t stream) {
-    if (a.T <= kFewTokens) return launch_few<WT>(a, stream);
+    if (few_fits<WT>(a)) return launch_few<WT>(a, stream);
     return a.T * a.k <= 10 * a.N || a.T <= 16 ? launch_many<WT, 1>(a, stream) : launch_many<WT, 2>(a, stream);
 }
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t stream) {
@@ -882,7 +972,7 @@ hipError_t launch_experts(const ExpertsArgs& a, hipStream_t stream) {
 }
 
 size_t experts_h_bytes(int T, int k, int f) { return (size_t)T * k * f * sizeof(bf16_t); }
-size_t experts_y_bytes(int T, int k, int d) { return T <= kFewTokens ? 0 : (size_t)kManySplits * T * k * d * sizeof(float); }
+size_t experts_y_bytes(int T, int k, int d) { return (size_t)kManySplits * T * k * d * sizeof(float); }
 
 size_t experts_part_bytes(int T, int d, int N) { return (size_t)T * gate_slices(d, N) * gate_columns(N) * sizeof(float); }
 
@@ -902,11 +992,13 @@ hipError_t launch_experts_gate(const ExpertsArgs& a, const float* W_gate, hipStr
 
 template <typename WT>
 static hipError_t init_experts() {   // every kernel that launch_experts may start
-    constexpr int DU = kFewUpDepth<WT>, DD = kFewDownDepth<WT>;
+    constexpr int DD = kFewDownDepth<WT>;
     hipError_t e = hipSuccess;
     const auto set = [&](const void* k, int lds) { if (e == hipSuccess) e = ensure_lds_limit(k, lds); };
-    set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 4, DU>), few_up_lds<WT, 4, DU>());
-    set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 1, DU>), few_up_lds<WT, 1, DU>());
+    set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 1>), few_up_lds<WT>(kFewRowsMost, false));
+    set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 2>), few_up_lds<WT>(kFewRowsMost, true));
+    set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 4>), few_up_lds<WT>(kFewRowsMost, true));
+    set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 8>), few_up_lds<WT>(kFewRowsMost, true));
     set(reinterpret_cast<const void*>(&experts_few_down_kernel<WT, kFewDownWaves, DD>), few_down_lds<WT, kFewDownWaves, DD>());
     set(reinterpret_cast<const void*>(&experts_many_kernel<WT, true, 1>), many_lds<WT, 1>());
     set(reinterpret_cast<const void*>(&experts_many_kernel<WT, true, 2>), many_lds<WT, 2>());

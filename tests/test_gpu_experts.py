@@ -87,7 +87,8 @@ def routing(T, N, k, g, padded=False, zipf=False):
 # T, N, k, d, f: one token to the most; channels past the last tile, K tiles that end in parts, more tokens to an expert than a block takes
 CASES = [(1, 8, 2, 512, 256), (1, 1, 1, 32, 32), (1, 64, 8, 1024, 96), (2, 4, 2, 544, 1056), (3, 3, 3, 96, 4128), (4, 7, 2, 1056, 288),
          (4, 2, 8, 256, 64), (5, 8, 2, 512, 256), (9, 28, 4, 2080, 160), (16, 4, 1, 288, 544), (16, 8, 8, 64, 1024), (17, 8, 2, 512, 96),
-         (33, 28, 4, 1056, 352), (64, 2, 2, 320, 288), (64, 64, 8, 128, 64), (63, 3, 2, 4096, 512), (40, 1, 1, 96, 2048), (1, 2, 2, 2048, 16384)]
+         (33, 28, 4, 1056, 352), (64, 2, 2, 320, 288), (64, 64, 8, 128, 64), (63, 3, 2, 4096, 512), (40, 1, 1, 96, 2048), (1, 2, 2, 2048, 16384),
+         (4, 5, 3, 64, 8192), (1, 7, 4, 992, 4000), (2, 64, 8, 544, 2048), (4, 16, 2, 4096, 320), (2, 3, 2, 12288, 64), (4, 3, 2, 8192, 96)]
 
 
 @pytest.mark.parametrize("mx4", [True, False])

@@ -174,7 +174,9 @@ def test_gemm_mx4_scales_far_apart():
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T,d_in,d_out", [(1, 32, 8), (1, 4096, 512), (2, 1056, 264), (3, 544, 4104), (4, 4096, 4096), (5, 4096, 264), (17, 608, 72),
-                                          (64, 2048, 1000), (300, 1056, 520), (1, 16384, 64), (4, 8192, 40)])
+                                          (64, 2048, 1000), (300, 1056, 520), (1, 16384, 64), (4, 8192, 40),
+                                          (2, 672, 12336), (64, 1024, 14336), (100, 512, 14336), (300, 1024, 8192), (700, 1024, 5120),
+                                          (1, 64, 4096), (65, 4096, 4096)])
 def test_base_gemm_mx4_and_its_gradient(T, d_in, d_out, dtype):
     g = gen(T + d_in)
     x = torch.randn((T, d_in), generator=g, device="cuda").to(dtype)
