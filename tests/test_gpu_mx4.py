@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import paper_2405_13053_amd as m
+from tests import i8_kernels
 from tests import mx4_cases as mx
 
 pytestmark = pytest.mark.gpu
@@ -200,3 +201,228 @@ def test_gradient_against_differences():
     V = mx.values(W, ws).abs()
     size = ((b.abs() + a.abs()).double() @ V.t() * dy.abs().double()).sum(1)
     assert ((left - right).abs() <= 64 * U * size).all()
+
+
+# ---- every kernel --------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("T,half,d_out,N", i8_kernels.PRODUCTS + [(*c, None) for cases in i8_kernels.TAILS.values() for c in cases])
+def test_every_kernel_of_the_product(T, half, d_out, N):
+    """The sizes that lead to each tile shape and copy of its loop (half: bytes of a row), in both types of the output."""
+    d_in = half * 2
+    g = gen(T + d_in + d_out)
+    if N is None:
+        q, s, v = operand(T, d_in, g)
+        W, ws, wv = operand(d_out, d_in, g)
+        ref, size = mx.product(v, wv), mx.product(v.abs(), wv.abs())
+        for dtype in TYPES:
+            out = torch.full((T + 1, d_out), 7.0, device="cuda", dtype=dtype)
+            m.gemm_mx4(q, s, W, ws, out=out[:T])
+            close(out[:T], ref, size, d_in / 32)
+            assert (out[T] == 7).all()
+        return
+    counts = i8_kernels.deal(T, N)
+    bounds = [0]
+    for c in counts:
+        bounds.append(bounds[-1] + c)
+    q, s, v = operand(T, d_in, g)
+    parts = [operand(d_out, d_in, g) for _ in range(N)]
+    W, ws = torch.stack([p[0] for p in parts]), torch.stack([p[1] for p in parts])
+    offsets = torch.tensor(bounds, dtype=torch.int32, device="cuda")
+    for dtype in TYPES:
+        out = torch.full((T, d_out), 7.0, device="cuda", dtype=dtype)
+        m.gemm_mx4(q, s, W, ws, offsets=offsets, out=out)
+        for e, (a, b) in enumerate(zip(bounds, bounds[1:])):
+            if b > a:
+                close(out[a:b], mx.product(v[a:b], parts[e][2]), mx.product(v[a:b].abs(), parts[e][2].abs()), d_in / 32)
+        assert (out[bounds[-1]:] == 7).all()
+
+
+# ---- calls that programs make -----------------------------------------------------------------------------------------------------
+def test_without_tokens():
+    g = gen(40)
+    W, ws = m.quantize_mx4(torch.randn((64, 96), generator=g, device="cuda"))
+    x = torch.empty((0, 96), device="cuda")
+    q, s = m.quantize_mx4(x)
+    assert q.shape == (0, 48) and s.shape == (1, 0, 16)
+    assert m.dequantize_mx4(q, s).shape == (0, 96) and m.dequantize_mx4(q, s, transpose=True).shape == (96, 0)
+    assert m.gemm_mx4(q, s, W, ws).shape == (0, 64) and m.base_gemm_mx4(x, W, ws).shape == (0, 64)
+    assert m.gemm_mx4(q, s, W[None], ws[None], offsets=torch.zeros(2, dtype=torch.int32, device="cuda")).shape == (0, 64)
+    assert m.base_gemm_mx4_backward(torch.empty((0, 64), device="cuda"), W, ws).shape == (0, 96)
+
+
+def test_refusals_of_the_binding():
+    x = torch.randn((16, 128), device="cuda")
+    W, ws = m.quantize_mx4(torch.randn((64, 128), device="cuda"))
+    q, s = m.quantize_mx4(x)
+    wrong = [lambda: m.quantize_mx4(x[:, :64]), lambda: m.quantize_mx4(x, out=(q[:8], s)), lambda: m.quantize_mx4(x, out=(q, s[:, :8])),
+             lambda: m.dequantize_mx4(q, s[:, :8]), lambda: m.dequantize_mx4(q.t(), s), lambda: m.dequantize_mx4(q, s, out=x[:8]),
+             lambda: m.gemm_mx4(q, s, W[:, :32], ws), lambda: m.gemm_mx4(q, s, W, ws[:, :8]), lambda: m.gemm_mx4(q[::2], s, W, ws),
+             lambda: m.gemm_mx4(q, s, W[None], ws[None]), lambda: m.gemm_mx4(q, s, W, ws, offsets=torch.zeros(2, dtype=torch.int32, device="cuda")),
+             lambda: m.base_gemm_mx4(x, W[:32], ws), lambda: m.base_gemm_mx4(x.t(), W, ws), lambda: m.base_gemm_mx4(x, W, ws, out=x),
+             lambda: m.base_gemm_mx4_backward(x, W, ws), lambda: m.base_gemm_mx4_backward(torch.zeros((4, 64), device="cuda"), W, ws[:, :8])]
+    for call in wrong:
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: m.quantize_mx4(x.half()), lambda: m.quantize_mx4(x, out=(q.view(torch.int8), s)), lambda: m.gemm_mx4(q.view(torch.int8), s, W, ws),
+                 lambda: m.base_gemm_mx4(x, W, ws.view(torch.int8)), lambda: m.dequantize_mx4(q, s, dtype=torch.float16)):
+        with pytest.raises(TypeError):
+            call()
+    for call, status in ((lambda: m.quantize_mx4(torch.zeros((4, 48), device="cuda")), 2),
+                         (lambda: m.dequantize_mx4(q[:12].contiguous(), s[:, :12].contiguous(), transpose=True), 2),
+                         (lambda: m.base_gemm_mx4(x, W, ws, ws=torch.empty(64, dtype=torch.uint8, device="cuda")), 3),
+                         (lambda: m.base_gemm_mx4_backward(torch.zeros((4, 64), device="cuda"), W, ws,
+                                                           ws=torch.empty(256, dtype=torch.uint8, device="cuda")), 3)):
+        with pytest.raises(m.MeteoraError) as e:
+            call()
+        assert e.value.status == status
+
+
+@pytest.mark.parametrize("T,d_in,d_out", [(2, 1056, 264), (40, 1056, 520), (300, 288, 8192), (2000, 800, 1032)])
+def test_what_a_workspace_holds_does_not_matter(T, d_in, d_out):
+    g = gen(T)
+    x, dy = torch.randn((T, d_in), generator=g, device="cuda").bfloat16(), torch.randn((T, d_out), generator=g, device="cuda").bfloat16()
+    W, ws = m.quantize_mx4(torch.randn((d_out, d_in), generator=g, device="cuda"))
+    results = []
+    for fill in (0, 255):
+        a = torch.full((m.base_gemm_mx4_workspace_bytes(T + 100, d_in),), fill, dtype=torch.uint8, device="cuda")
+        b = torch.full((m.base_gemm_mx4_backward_workspace_bytes(d_in, d_out, torch.bfloat16),), fill, dtype=torch.uint8, device="cuda")
+        results.append((m.base_gemm_mx4(x, W, ws, ws=a), m.base_gemm_mx4_backward(dy, W, ws, ws=b)))
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+
+
+def test_another_stream_and_graphs_that_share_a_workspace():
+    g = gen(41)
+    W, ws = m.quantize_mx4(torch.randn((520, 1056), generator=g, device="cuda"))
+    m.init()
+
+    def step(x, dy, y, dx, a, b):
+        return m.base_gemm_mx4(x, W, ws, out=y, ws=a), m.base_gemm_mx4_backward(dy, W, ws, out=dx, ws=b)
+
+    a = torch.empty(m.base_gemm_mx4_workspace_bytes(700, 1056), dtype=torch.uint8, device="cuda")
+    b = torch.empty(m.base_gemm_mx4_backward_workspace_bytes(1056, 520, torch.bfloat16), dtype=torch.uint8, device="cuda")
+    cases = []
+    for T in (700, 3, 40):
+        x, dy = (torch.randn((T, n), generator=g, device="cuda").bfloat16() for n in (1056, 520))
+        y, dx = torch.empty_like(dy), torch.empty_like(x)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(x, dy, y, dx, a, b)
+            q, s = m.quantize_mx4(y.repeat(1, 4))   # 2080 wide
+            back = m.dequantize_mx4(q, s)
+        cases.append((x, dy, y, dx, back, graph))
+    for i in range(3):
+        for x, dy, y, dx, back, graph in cases:
+            x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+            dy.copy_(torch.randn(dy.shape, generator=g, device="cuda"))
+            graph.replay()
+            torch.cuda.synchronize()
+            want = step(x, dy, None, None, None, None)
+            assert torch.equal(y, want[0]) and torch.equal(dx, want[1]), f"replay {i}"
+            assert torch.equal(back, m.dequantize_mx4(*m.quantize_mx4(want[0].repeat(1, 4))))
+    x, dy, y, dx, _, _ = cases[0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step(x, dy, None, None, None, None)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got[0], y) and torch.equal(got[1], dx)
+
+
+def test_two_streams_at_once():
+    g = gen(43)
+    W, ws = m.quantize_mx4(torch.randn((1032, 2080), generator=g, device="cuda"))
+    xs = [torch.randn((T, 2080), generator=g, device="cuda").bfloat16() for T in (900, 64)]
+    want = [m.base_gemm_mx4(x, W, ws) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(20):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(m.base_gemm_mx4(xs[i], W, ws))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i]) for i in (0, 1) for y in got[i])
+
+
+def test_more_than_four_gigabytes_of_outputs():
+    g = gen(44)
+    T, d_out = 70000, 40960
+    q, s, v = operand(T, 64, g)
+    W, ws, wv = operand(d_out, 64, g)
+    out = m.gemm_mx4(q, s, W, ws)
+    at = torch.tensor([0, 1, 255, 256, 26213, 26214, 26215, 52428, 52429, 69887, 69999], device="cuda")   # around 2^31 and 2^32 bytes
+    close(out[at], mx.product(v[at], wv), mx.product(v[at].abs(), wv.abs()), 2)
+
+
+def test_rows_of_more_than_four_gigabytes():
+    rows, d = 70000, 32768
+    x = torch.zeros((rows, d), dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 7, 32767, 32768, 65535, 65536, 69992, 69999], device="cuda")
+    x[at] = torch.randn((len(at), d), generator=gen(45), device="cuda").bfloat16()
+    q, s = m.quantize_mx4(x)
+    rq, rs = mx.quantize(x[at])
+    assert torch.equal(q[at], rq) and torch.equal(s[:, at], rs)
+    assert torch.equal(m.dequantize_mx4(q, s, out=x)[at].double(), mx.values(rq, rs))
+    turned = m.dequantize_mx4(q, s, transpose=True)
+    assert torch.equal(turned[:, at].double(), mx.values(rq, rs).t()) and not turned[:, 1:7].any()
+
+
+def test_matrices_past_four_gigabytes():
+    """The last of 64 matrices of 70 MB; its scales lie behind 280 MB of others."""
+    g = gen(46)
+    W = torch.empty((64, 17408, 4096), dtype=torch.uint8, device="cuda")
+    ws = torch.zeros((64, 16, 17408, 16), dtype=torch.uint8, device="cuda")
+    W[63], ws[63], wv = operand(17408, 8192, g)
+    q, s, v = operand(20, 8192, g)
+    offsets = torch.tensor([0] * 64 + [20], dtype=torch.int32, device="cuda")
+    out = m.gemm_mx4(q, s, W, ws, offsets=offsets)
+    close(out, mx.product(v, wv), mx.product(v.abs(), wv.abs()), 256)
+
+
+# ---- run together -----------------------------------------------------------------------------------------------------------------
+def test_a_layers_own_adapters_on_a_4_bit_base_projection():
+    """The layer with its frozen projection in 4 bits: base_gemm_mx4, then lora_forward onto it; and the input's gradient through the projection."""
+    g = gen(50)
+    T, d_in, d_out, N, r, k, scale = 130, 512, 264, 6, 8, 2, 2.0
+    x, dy = (torch.randn((T, n), generator=g, device="cuda").bfloat16() for n in (d_in, d_out))
+    A, B = (torch.randn(shape, generator=g, device="cuda").mul_(shape[1] ** -0.5).bfloat16() for shape in ((N, d_in, r), (N, r, d_out)))
+    Wg = torch.randn((d_in, N), generator=g, device="cuda")
+    W, ws = m.quantize_mx4(torch.randn((d_out, d_in), generator=g, device="cuda").mul_(d_in ** -0.5))
+    idx, w, _ = m.gate_topk(x, Wg, None, k)
+    y = m.base_gemm_mx4(x, W, ws)
+    base = y.double()
+    out = m.lora_forward(x, A, B, idx, w, scale, out=y, accumulate=True)
+    V = mx.values(W, ws)
+    assert (base - mx.product(mx.values(*mx.quantize(x)), V)).abs().max() <= 5e-3 * base.abs().max()
+    lora = torch.zeros_like(base)
+    for j in range(k):
+        a = idx[:, j].long()
+        h = torch.bmm(x.double()[:, None], A.double()[a])
+        lora += scale * w[:, j, None].double() * torch.bmm(h, B.double()[a])[:, 0]
+    assert (out.double() - (base + lora)).abs().max() <= 5e-3 * (base + lora).abs().max()
+    dx = m.base_gemm_mx4_backward(dy, W, ws)
+    close(dx, mx.product(dy.double(), V.t()), mx.product(dy.double().abs(), V.t().abs()), d_out)
+
+
+def test_sorted_rows_through_4_bit_matrices_of_adapters_and_back():
+    """sort_tokens, quantize_mx4, gemm_mx4 over the adapters, unsort_tokens, with padding tokens and rows that nothing was written to."""
+    g = gen(51)
+    T, N, k, d_in, d_out = 203, 7, 3, 544, 264
+    x = torch.randn((T, d_in), generator=g, device="cuda").bfloat16()
+    idx = torch.randint(-1, N, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    w = torch.rand((T, k), generator=g, device="cuda")
+    parts = [operand(d_out, d_in, g, spread=2) for _ in range(N)]
+    W, ws = torch.stack([p[0] for p in parts]), torch.stack([p[1] for p in parts])
+    xs = torch.full((T * k, d_in), float("nan"), dtype=torch.bfloat16, device="cuda")
+    xs, pos, offsets = m.sort_tokens(x, idx, N, out=xs)
+    q, s = m.quantize_mx4(xs)
+    ys = m.gemm_mx4(q, s, W, ws, offsets=offsets, out=torch.full((T * k, d_out), 7.0, dtype=torch.bfloat16, device="cuda"))
+    out = m.unsort_tokens(ys, pos, w)
+    xv = mx.values(*mx.quantize(x))
+    ref, tol = (torch.zeros((T, d_out), dtype=torch.float64, device="cuda") for _ in range(2))
+    for e in range(N):
+        y, size = mx.product(xv, parts[e][2]), mx.product(xv.abs(), parts[e][2].abs())
+        share = (w.double() * (idx == e)).sum(1)[:, None]
+        ref += share * y
+        tol += share * (d_in / 32 * U * size + half_step(torch.bfloat16) * (y.abs() + d_in / 32 * U * size))
+    tol += 4 * U * ref.abs() + half_step(torch.bfloat16) * (ref.abs() + tol)
+    assert ((out.double() - ref).abs() <= tol * 1.001 + 4 * U * tol).all()
