@@ -192,3 +192,145 @@ def test_equal_logits_go_to_the_lowest_index():
     Wg = randn((64, 1), g, 0.1, torch.float32).expand(64, 6).contiguous()
     _, idx, w = m.moe_forward(x, Wg, None, *layer.weights, 3, return_routing=True)
     assert (idx == torch.arange(3, device="cuda")).all() and ((w - 1 / 3).abs() <= 1e-6).all()
+
+
+# ---- calls that programs make -----------------------------------------------------------------------------------------------------
+def moe(layer, x, Wg, k, **more):
+    return m.moe_forward(x, Wg, None, *layer.weights, k, **layer.scales, **more)
+
+
+def test_without_tokens():
+    layer = Layer(4, 64, 32, True, gen(1))
+    x, idx, w = torch.empty((0, 64), dtype=BF, device="cuda"), torch.empty((0, 2), dtype=torch.int32, device="cuda"), torch.empty((0, 2), device="cuda")
+    assert m.experts_forward(x, idx, w, *layer.weights, **layer.scales).shape == (0, 64)
+    out, i, v = moe(layer, x, torch.zeros((64, 4), device="cuda"), 2, return_routing=True)
+    assert out.shape == (0, 64) and i.shape == v.shape == (0, 2)
+
+
+def test_refusals_of_the_binding():
+    g = gen(2)
+    a, b = Layer(4, 64, 96, True, g), Layer(4, 64, 96, False, g)
+    x, (idx, w) = randn((8, 64), g), routing(8, 4, 2, g)
+    call = lambda layer=a, x=x, idx=idx, w=w, W1=None, W2=None, **more: m.experts_forward(
+        x, idx, w, W1 if W1 is not None else layer.weights[0], W2 if W2 is not None else layer.weights[1], **{**layer.scales, **more})
+    Wg = torch.zeros((64, 4), device="cuda")
+    wrong = [lambda: call(x=x[:4]), lambda: call(idx=idx[:4]), lambda: call(w=w[:, :1]), lambda: call(W1=a.weights[0][:2]), lambda: call(W2=a.weights[1][:, :32]),
+             lambda: call(w1_scale=None), lambda: call(w2_scale=a.scales["w2_scale"][:, :, :8]), lambda: call(layer=b, W1=b.weights[0][:, :96]),
+             lambda: call(base=x[:4]), lambda: call(out=x[:, :32]), lambda: call(x=x.t()), lambda: call(idx=idx.t()),
+             lambda: moe(a, x, Wg.t().contiguous(), 2), lambda: m.moe_forward(x, Wg, torch.zeros(3, device="cuda"), *a.weights, 2, **a.scales)]
+    for f in wrong:
+        with pytest.raises(ValueError):
+            f()
+    for f in (lambda: call(idx=idx.long()), lambda: call(w=w.double()), lambda: call(layer=b, x=x.float()), lambda: call(W1=a.weights[0].view(torch.int8)),
+              lambda: call(base=x.float())):
+        with pytest.raises(TypeError):
+            f()
+    small = torch.empty(256, dtype=torch.uint8, device="cuda")
+    f32 = [t.float() for t in b.weights]
+    for f, status in ((lambda: call(ws=small), 3), (lambda: call(layer=b, x=x.float(), W1=f32[0], W2=f32[1]), 2), (lambda: call(scale=float("nan")), 1),
+                      (lambda: moe(a, x, Wg, 5), 1), (lambda: moe(a, x, Wg, 2, ws=small), 3),
+                      (lambda: m.experts_forward(randn((65, 64), g), *routing(65, 4, 2, g), *a.weights, **a.scales), 2)):
+        with pytest.raises(m.MeteoraError) as e:
+            f()
+        assert e.value.status == status
+
+
+@pytest.mark.parametrize("mx4", [True, False])
+@pytest.mark.parametrize("T,N,k,d,f", [(1, 8, 2, 512, 256), (3, 16, 4, 64, 8192), (4, 3, 2, 8192, 96), (13, 8, 2, 1056, 352), (64, 6, 3, 96, 2080)])
+def test_what_a_workspace_holds_does_not_matter(T, N, k, d, f, mx4):
+    g = gen(T + d)
+    layer, x, Wg = Layer(N, d, f, mx4, g), randn((T, d), g), randn((d, N), g, d ** -0.5, torch.float32)
+    idx, w = routing(T, N, k, g)
+    for call in (lambda ws: m.experts_forward(x, idx, w, *layer.weights, **layer.scales, ws=ws), lambda ws: moe(layer, x, Wg, k, ws=ws)):
+        got = [call(torch.full((m.experts_workspace_bytes(64, d, f, N, k),), fill, dtype=torch.uint8, device="cuda")) for fill in (0, 255, 255)]
+        assert torch.equal(got[0], got[1]) and torch.equal(got[1], got[2])
+
+
+@pytest.mark.parametrize("mx4", [True, False])
+def test_graphs_that_share_a_workspace_and_another_stream(mx4):
+    g = gen(61)
+    N, k, d, f = 6, 2, 288, 352
+    layer, Wg = Layer(N, d, f, mx4, g), randn((d, N), g, d ** -0.5, torch.float32)
+    m.init()
+    ws = torch.empty(m.experts_workspace_bytes(64, d, f, N, k), dtype=torch.uint8, device="cuda")
+
+    def step(x, idx, w, ws):   # a gated layer, and one with its routing given onto it
+        y, i, v = moe(layer, x, Wg, k, ws=ws, return_routing=True)
+        return m.experts_forward(y, idx, w, *layer.weights, **layer.scales, base=x, scale=0.5, ws=ws), i, v
+
+    cases = []
+    for T in (64, 1, 20, 4):
+        x, (idx, w) = randn((T, d), g), routing(T, N, k, g)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = step(x, idx, w, ws)
+        cases.append((x, idx, w, got, graph))
+    for i in range(3):
+        for x, idx, w, got, graph in cases:
+            x.copy_(randn(x.shape, g))
+            idx.copy_(routing(x.shape[0], N, k, g, padded=i == 2)[0])
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, step(x, idx, w, None))), f"replay {i}"
+    x, idx, w, got, _ = cases[0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = step(x, idx, w, None)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, other))
+
+
+def test_two_streams_at_once():
+    g = gen(63)
+    layer, Wg = Layer(8, 512, 768, True, g), randn((512, 8), g, 512 ** -0.5, torch.float32)
+    xs = [randn((T, 512), g) for T in (64, 2)]
+    want = [moe(layer, x, Wg, 2) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(20):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(moe(layer, xs[i], Wg, 2))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i]) for i in (0, 1) for y in got[i])
+
+
+@pytest.mark.parametrize("T", [2, 24])
+def test_weights_past_four_gigabytes(T):
+    """The last of 48 experts of 57 + 29 MB in 4 bits; the first product's weights are 4.8 GB, their scales 0.3."""
+    g = gen(70 + T)
+    N, d, f = 48, 4096, 24576
+    W1 = torch.zeros((N, 2 * f, d // 2), dtype=torch.uint8, device="cuda")
+    W2 = torch.zeros((N, d, f // 2), dtype=torch.uint8, device="cuda")
+    s1, s2 = (torch.zeros((N, *m.mx4_scale_shape(*shape)), dtype=torch.uint8, device="cuda") for shape in ((2 * f, d), (d, f)))
+    W1[-1], s1[-1] = m.quantize_mx4(randn((2 * f, d), g, d ** -0.5))
+    W2[-1], s2[-1] = m.quantize_mx4(randn((d, f), g, f ** -0.5))
+    x = randn((T, d), g)
+    idx = torch.full((T, 1), N - 1, dtype=torch.int32, device="cuda")
+    w = torch.ones((T, 1), device="cuda")
+    out = m.experts_forward(x, idx, w, W1, W2, w1_scale=s1, w2_scale=s2)
+    one = Layer.__new__(Layer)
+    one.N, one.d, one.f, one.V1, one.V2 = 1, d, f, [mx.values(W1[-1], s1[-1])], [mx.values(W2[-1], s2[-1])]
+    close(out, one.reference(x, idx * 0, w))
+
+
+# ---- run together -----------------------------------------------------------------------------------------------------------------
+def test_a_block_with_4_bit_experts_from_its_own_quantisation():
+    """A decode step of a block: a 4-bit projection, then the experts onto the residual stream, then the same through sorted rows."""
+    g = gen(80)
+    T, N, k, d, f = 24, 6, 2, 512, 352
+    x, Wo = randn((T, d), g), m.quantize_mx4(randn((d, d), g, d ** -0.5))
+    layer, Wg = Layer(N, d, f, True, g), randn((d, N), g, d ** -0.5, torch.float32)
+    y = m.base_gemm_mx4(x, *Wo)
+    out, idx, w = moe(layer, y, Wg, k, base=x, return_routing=True)
+    close(out, layer.reference(y, idx, w, 1.0, x))
+    # the experts' products over sorted rows, with x and h in 4 bits too: the same but for their rounding
+    ys, pos, offsets = m.sort_tokens(y, idx, N)
+    both = m.gemm_mx4(*m.quantize_mx4(ys), layer.weights[0], layer.scales["w1_scale"], offsets=offsets).float()
+    h = (torch.nn.functional.silu(both[:, :f]) * both[:, f:]).bfloat16()
+    sorted_out = m.unsort_tokens(m.gemm_mx4(*m.quantize_mx4(h.contiguous()), layer.weights[1], layer.scales["w2_scale"], offsets=offsets), pos, w, base=x)
+    moved = (out.double() - x.double()).norm()
+    # a normal row rounded to 4 bits is off by some 0.12 of its norm: y's rounding acts on gate and up (0.17), h's adds its own: 0.21 together
+    assert (sorted_out.double() - out.double()).norm() <= 0.35 * moved
