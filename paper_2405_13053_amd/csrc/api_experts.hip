@@ -50,7 +50,7 @@ ExpertsArgs arguments(const void* x, int32_t* idx, float* w, const void* W1, con
     char* const p = static_cast<char*>(ws);
     return {static_cast<const bf16_t*>(x), idx, w, static_cast<const uint8_t*>(W1), s1, static_cast<const uint8_t*>(W2), s2,
             static_cast<const bf16_t*>(base), static_cast<bf16_t*>(out), reinterpret_cast<bf16_t*>(p), reinterpret_cast<float*>(p + s.y), p + s.plan, scale,
-            T, k, N, d, f, nullptr, nullptr, 1.f};
+            T, k, N, d, f, nullptr, nullptr, nullptr, 1.f};
 }
 
 }  // namespace
@@ -83,16 +83,15 @@ meteora_status meteora_moe_forward(const void* x, const float* W_gate, const flo
     if (s != METEORA_OK) return s;
     if (!aligned(W_gate, 16) || !aligned(gate_bias, 4) || !aligned(topk_idx_out, 4) || !aligned(topk_w_out, 4)) return METEORA_ERR_UNSUPPORTED;
     if (T == 0) return METEORA_OK;
-    hipStream_t st = static_cast<hipStream_t>(stream);
     const Scratch c = carve(T, d, f, N, k);
     int32_t* idx = topk_idx_out ? topk_idx_out : reinterpret_cast<int32_t*>(static_cast<char*>(ws) + c.idx);
     float* w = topk_w_out ? topk_w_out : reinterpret_cast<float*>(static_cast<char*>(ws) + c.w);
     ExpertsArgs a = arguments(x, idx, w, W1, w1_scale, W2, w2_scale, T, d, f, N, k, scale, base, out, ws);
     a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + c.part);
+    a.W_gate = W_gate;
     a.bias = gate_bias;
     a.inv_temperature = inv_temperature;
-    const hipError_t e = launch_experts_gate(a, W_gate, st);
-    return e != hipSuccess ? METEORA_ERR_HIP : status(launch_experts(a, st));
+    return status(launch_experts(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

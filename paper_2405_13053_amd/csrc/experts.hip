@@ -91,7 +91,16 @@ __global__ __launch_bounds__(256) void gate_part_kernel(const bf16_t* __restrict
     }
 }
 
-// Token t by a wavefront: lane j < k has its j-th choice and weight.
+// A token by a wavefront, lane e with the logit of expert e: lane j < k has the j-th choice and its weight.
+__device__ __forceinline__ void choose_experts(const ExpertsArgs& a, float logit, int lane, int& expert, float& weight) {
+    float g[1] = {logit == 0.f ? 0.f : logit};   // -0 -> +0 so equal logits have equal keys
+    int sel[1];
+    float w[1];
+    wave_topk_softmax<64, 1>(g, lane, a.N, a.k, a.inv_temperature, sel, w);
+    expert = sel[0];
+    weight = w[0];
+}
+// Token t from the partial logits
 __device__ __forceinline__ void route_token(const ExpertsArgs& a, int t, int lane, int& expert, float& weight) {
     const int NP = gate_columns(a.N), slices = gate_slices(a.d, a.N), each = 64 / NP, col = lane % NP;
     const float* p = a.part + (size_t)t * slices * NP + col;
@@ -104,13 +113,7 @@ __device__ __forceinline__ void route_token(const ExpertsArgs& a, int t, int lan
     }
     const float b = a.bias != nullptr && lane < a.N ? a.bias[lane] : 0.f;
     for (int off = NP; off < 64; off <<= 1) g[0] += __shfl_xor(g[0], off);
-    g[0] += b;
-    if (g[0] == 0.f) g[0] = 0.f;   // -0 -> +0 so equal logits have equal keys
-    int sel[1];
-    float w[1];
-    wave_topk_softmax<64, 1>(g, lane, a.N, a.k, a.inv_temperature, sel, w);
-    expert = sel[0];
-    weight = w[0];
+    choose_experts(a, g[0] + b, lane, expert, weight);
 }
 __global__ __launch_bounds__(256) void experts_route_kernel(const ExpertsArgs a) {
     const int lane = threadIdx.x & 63, t = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -327,6 +330,36 @@ template <typename WT>
 constexpr int few_up_lds(int rows_bytes, bool sums) { return kFewWaves * (kFewDepth * 2 * WT::kBlockBytes + (sums ? 2048 : 0)) + rows_bytes; }
 static_assert(few_up_lds<Mx4Weights>(kFewRowsMost, true) + 1024 <= 160 * 1024, "LDS");
 
+// The gate of one token by every workgroup for itself, from x in LDS (zeros at `pad`): two rows of W_gate to a thread and step, all steps on their way at
+// once.  sums: [wavefront][NP], which whoever routes adds up.  A layer of 28 experts of 1024 inputs takes 15.3 us so, with gate_part_kernel in front 16.6,
+// of 8 experts of 1024 14.0 and 17.5; of more tokens every workgroup has too much to add up (4 tokens of 8 experts of 4096: 24.8 and 20.6).
+constexpr int kGateHere = 32768, kGatePairs = kGateHere / (2 * kFewWaves * 64);
+__device__ __forceinline__ void load_gate(const ExpertsArgs& a, int lane, int wave, float (&w)[2 * kGatePairs]) {
+    const int NP = gate_columns(a.N), col = lane & (NP - 1), each = 64 / NP;
+    const auto W = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.W_gate), 0, (uint32_t)(a.d * a.N) * 4u, 0x00020000);   // zeros behind the last row
+    const uint32_t row = (uint32_t)a.N * 4, step = 2 * kFewWaves * each * row;
+    uint32_t at = col < a.N ? 2 * (wave * each + lane / NP) * row + col * 4 : kOutside;
+#pragma unroll
+    for (int i = 0; i < kGatePairs; ++i, at += step) {
+        w[2 * i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(W, at, 0, 0));
+        w[2 * i + 1] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(W, at + row, 0, 0));
+    }
+}
+__device__ __forceinline__ void gate_here(const ExpertsArgs& a, const float (&w)[2 * kGatePairs], const unsigned char* x, int pad, int lane, int wave, float* sums) {
+    const int NP = gate_columns(a.N), each = 64 / NP;
+    int at = (wave * each + lane / NP) * 4;
+    float s[4] = {};
+#pragma unroll
+    for (int i = 0; i < kGatePairs; ++i, at += kFewWaves * each * 4) {
+        const uint32_t v = *reinterpret_cast<const uint32_t*>(x + min(at, pad));
+        s[i & 3] = fmaf(__uint_as_float(v << 16), w[2 * i], s[i & 3]);
+        s[i & 3] = fmaf(__uint_as_float(v & 0xffff0000u), w[2 * i + 1], s[i & 3]);
+    }
+    float sum = (s[0] + s[1]) + (s[2] + s[3]);
+    for (int off = NP; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
+    if (lane < NP) sums[wave * NP + lane] = sum;
+}
+
 template <typename WT, int KS>
 __global__ __launch_bounds__(kFewWaves * 64) void experts_few_up_kernel(const ExpertsArgs a) {
     constexpr int D = kFewDepth, NL = 2 * (2 + WT::kScales), kSlot = 2 * WT::kBlockBytes, GROUPS = kFewWaves / KS;
@@ -353,7 +386,27 @@ __global__ __launch_bounds__(kFewWaves * 64) void experts_few_up_kernel(const Ex
     if (a.part != nullptr) {   // every workgroup routes; the first one says how
         int e = -1;
         float w = 0.f;
-        if (wave < a.T) route_token(a, wave, lane, e, w);
+        if (a.W_gate != nullptr) {
+            float* const logits = reinterpret_cast<float*>(smem);   // in the rings' place
+            const int NP = gate_columns(a.N);
+            float held[2 * kGatePairs];
+            load_gate(a, lane, wave, held);
+            const float b = a.bias != nullptr && lane < a.N ? a.bias[lane] : 0.f;
+            if (tid < 4) reinterpret_cast<uint32_t*>(rows + row_bytes - 16)[tid] = 0;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // x
+            __syncthreads();
+            gate_here(a, held, rows, row_bytes - 16, lane, wave, logits);
+            __syncthreads();
+            if (wave == 0) {
+                float g = 0.f;
+                if (lane < NP)
+#pragma unroll
+                    for (int v = 0; v < kFewWaves; ++v) g += logits[v * NP + lane];
+                choose_experts(a, g + b, lane, e, w);
+            }
+        } else if (wave < a.T) {
+            route_token(a, wave, lane, e, w);
+        }
         if (tid < 2 * kMaxAdapters) masks.word[tid >> 1][tid & 1] = 0;
         __syncthreads();
         if (wave < a.T && lane < a.k) {
@@ -926,6 +979,20 @@ static int few_down_split(int tiles, int experts, int nk) {
     }
     return best;
 }
+// the partial logits, and for more than kRouteTokens tokens the routing from them
+static hipError_t launch_gate(const ExpertsArgs& a, hipStream_t stream) {
+    const dim3 grid(gate_slices(a.d, a.N), ceil_div(a.T, kGateTokens));
+    const auto go = [&](auto kern) { kern<<<grid, 256, 0, stream>>>(a.x, a.W_gate, a.T, a.d, a.N, const_cast<float*>(a.part)); };
+    switch (gate_columns(a.N)) {
+        case 8: go(&gate_part_kernel<8>); break;
+        case 16: go(&gate_part_kernel<16>); break;
+        case 32: go(&gate_part_kernel<32>); break;
+        default: go(&gate_part_kernel<64>);
+    }
+    if (a.T > kRouteTokens) experts_route_kernel<<<ceil_div(a.T, 4), 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
 template <typename WT>
 static bool few_fits(const ExpertsArgs& a) { return a.T <= kFewTokens && a.T * few_row_bytes<WT>(a.d) <= kFewRowsMost; }
 
@@ -963,8 +1030,14 @@ static hipError_t launch_many(const ExpertsArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 template <typename WT>
-static hipError_t launch(const ExpertsArgs& a, hipStream_t stream) {
-    if (few_fits<WT>(a)) return launch_few<WT>(a, stream);
+static hipError_t launch(ExpertsArgs a, hipStream_t stream) {
+    const bool few = few_fits<WT>(a);
+    if (a.W_gate != nullptr && !(few && a.T == 1 && a.d * gate_columns(a.N) <= kGateHere)) {
+        const hipError_t e = launch_gate(a, stream);
+        if (e != hipSuccess) return e;
+        a.W_gate = nullptr;   // done
+    }
+    if (few) return launch_few<WT>(a, stream);
     return a.T * a.k <= 10 * a.N || a.T <= 16 ? launch_many<WT, 1>(a, stream) : launch_many<WT, 2>(a, stream);
 }
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t stream) {
@@ -975,20 +1048,6 @@ size_t experts_h_bytes(int T, int k, int f) { return (size_t)T * k * f * sizeof(
 size_t experts_y_bytes(int T, int k, int d) { return (size_t)kManySplits * T * k * d * sizeof(float); }
 
 size_t experts_part_bytes(int T, int d, int N) { return (size_t)T * gate_slices(d, N) * gate_columns(N) * sizeof(float); }
-
-// the partial logits, and for more than kRouteTokens tokens the routing from them
-hipError_t launch_experts_gate(const ExpertsArgs& a, const float* W_gate, hipStream_t stream) {
-    const dim3 grid(gate_slices(a.d, a.N), ceil_div(a.T, kGateTokens));
-    const auto go = [&](auto kern) { kern<<<grid, 256, 0, stream>>>(a.x, W_gate, a.T, a.d, a.N, const_cast<float*>(a.part)); };
-    switch (gate_columns(a.N)) {
-        case 8: go(&gate_part_kernel<8>); break;
-        case 16: go(&gate_part_kernel<16>); break;
-        case 32: go(&gate_part_kernel<32>); break;
-        default: go(&gate_part_kernel<64>);
-    }
-    if (a.T > kRouteTokens) experts_route_kernel<<<ceil_div(a.T, 4), 256, 0, stream>>>(a);
-    return hipGetLastError();
-}
 
 template <typename WT>
 static hipError_t init_experts() {   // every kernel that launch_experts may start

@@ -270,6 +270,7 @@ struct ExpertsArgs {
     float scale;
     int T, k, N, d, f;
     const float* part;                   // partial logits of the gate (experts_part_bytes), or nullptr: the routing is given
+    const float* W_gate;                 // [d, N] with `part`
     const float* bias;                   // [N] or nullptr
     float inv_temperature;
 };
@@ -278,7 +279,6 @@ size_t experts_h_bytes(int T, int k, int f);
 size_t experts_y_bytes(int T, int k, int d);
 size_t experts_plan_bytes();
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t stream);
-hipError_t launch_experts_gate(const ExpertsArgs& a, const float* W_gate, hipStream_t stream);   // in front of launch_experts, with `part`
 hipError_t experts_init_kernels();
 
 // ---- rows sorted by adapter: pos[T,k], offsets[N+1], xs[pos[t,j]] = x[t] (with xs_scale: as 8-bit whole numbers), and back
