@@ -181,7 +181,8 @@ __global__ __launch_bounds__(WV * 64) void gemm_mx4_wave_kernel(const GemmMx4Arg
 
 // ------------------------------------------------------------------------------------------
 // A few tokens and their quantisation in one launch (meteora_base_gemm_mx4): every workgroup quantises all of x itself, into LDS, while its
-// first tiles of W are on their way, which costs less than a launch in front.  W goes through the wavefronts' rings as above; a lane
+// first tiles of W are on their way, which costs less than a launch in front: 1, 2 and 4 tokens of 4096 -> 4096 4.7, 5.3 and 5.6 us, with a launch
+// of quantize_mx4_kernel in front 6.9, 6.8 and 6.9; of 4096 -> 14336, where workgroups follow one another on a CU, 9.1, 9.6 and 12.3, and 11.1, 10.8 and 11.1.  W goes through the wavefronts' rings as above; a lane
 // without a row of its own multiplies another's, and its result is not kept.
 // ------------------------------------------------------------------------------------------
 constexpr int kRowThreads = 256, kRowMaxTokens = 4, kRowMaxInputs = 16384;   // of all tokens
@@ -642,7 +643,8 @@ __global__ __launch_bounds__(256) void gemm_mx4_tail_kernel(const GemmMx4Args a)
 }
 
 // Up to 256 inputs (the expand of adapters): one K tile, and the output is what there is to move.  The same tiles without a ring, so
-// that four or five workgroups share a CU and one's loads and arithmetic lie under another's stores.
+// that four or five workgroups share a CU and one's loads and arithmetic lie under another's stores.  4096 x 256 -> 4096 9.8 us, with rings of 64 x 64 and
+// 128 x 128 32.3 and 10.6; 8192 x 128 -> 4096 14.2, 65.3 and 17.8; 16384 x 64 -> 4096 25.4 (5.4 TB/s), 129 and 31.0.
 template <typename TO, int MB, int NB>
 constexpr int one_mx4_lds() {
     constexpr int tiles = (MB + NB) * 32 * kI8Tile, stage = 4 * (MB % 2 == 0 ? 32 : 16) * (NB * 16 * (int)sizeof(TO) + 16);
@@ -767,7 +769,11 @@ static hipError_t launch_one_mx4(GemmMx4Args a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// ---- which kernel and tile, as for the products of 8-bit integers (kI8Shapes): a row's bytes count
+// ---- which kernel and tile, as for the products of 8-bit integers (see kI8Shapes): a row's bytes count.  The constants of the tiles of 128 x 128
+// and more are fitted to the times of all shapes at 269 sizes (27 numbers of rows from 1 to 8192, 10 matrices of 512 to 14336 inputs and 1024 to
+// 14336 channels).  The shape that is taken is 0.3 % slower than the best one on average and at most 15 % (512 x 4096 -> 1024, 10.5 and 9.1 us).  300 x
+// 4096 -> 4096: 64 x 64 13.7 us, 96 x 64 8.8, 128 x 128 11.4; 2048 x 1024 -> 4096: 128 x 128 two to a CU 8.8, 256 x 256 12.2; 1024 x 4096 -> 14336:
+// 128 x 128 42.3, 256 x 128 39.3, 256 x 256 31.9; 8192 x 4096 -> 14336: 330, 271, 227 (4.2 PFLOP/s).
 constexpr I8Shape kMx4Shapes[kI8ShapeCount] = {
     {16, 16, 1, true, 2.92f, 1.00f, 0.039f, 0.017f},
     {16, 32, 1, true, 1.31f, 2.84f, 0.036f, 0.060f},
@@ -776,12 +782,12 @@ constexpr I8Shape kMx4Shapes[kI8ShapeCount] = {
     {64, 64, 1, false, 1.00f, 3.07f, 0.145f, 0.110f},
     {96, 64, 1, false, 1.07f, 3.08f, 0.185f, 0.108f},
     {128, 64, 1, false, 1.07f, 3.12f, 0.229f, 0.102f},
-    {128, 128, 1, false, 1.36f, 3.50f, 0.357f, 0.182f},
-    {128, 128, 2, false, 1.76f, 2.98f, 0.293f, 0.394f},
-    {192, 128, 1, false, 1.71f, 4.09f, 0.486f, 0.173f},
-    {224, 128, 1, false, 1.76f, 4.53f, 0.546f, 0.155f},
-    {256, 128, 1, false, 1.68f, 5.00f, 0.619f, 0.147f},
-    {256, 256, 1, false, 1.21f, 8.19f, 0.665f, 0.665f},
+    {128, 128, 1, false, 1.13f, 2.81f, 0.474f, 0.104f},
+    {128, 128, 2, false, 1.29f, 2.81f, 0.480f, 0.328f},
+    {192, 128, 1, false, 0.98f, 4.04f, 0.589f, 0.177f},
+    {224, 128, 1, false, 0.91f, 3.47f, 0.650f, 0.178f},
+    {256, 128, 1, false, 0.78f, 4.19f, 0.681f, 0.239f},
+    {256, 256, 1, false, 0.84f, 6.34f, 0.853f, 0.700f},
 };
 template <typename TO>
 static hipError_t launch_mx4(const GemmMx4Args& a, hipStream_t stream) {

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import paper_2405_13053_amd as m
-from tests import i8_kernels
+from tests import i8_kernels, mx4_kernels
 from tests import mx4_cases as mx
 
 pytestmark = pytest.mark.gpu
@@ -204,7 +204,7 @@ def test_gradient_against_differences():
 
 
 # ---- every kernel --------------------------------------------------------------------------------------------------------------
-@pytest.mark.parametrize("T,half,d_out,N", i8_kernels.PRODUCTS + [(*c, None) for cases in i8_kernels.TAILS.values() for c in cases])
+@pytest.mark.parametrize("T,half,d_out,N", mx4_kernels.PRODUCTS)
 def test_every_kernel_of_the_product(T, half, d_out, N):
     """The sizes that lead to each tile shape and copy of its loop (half: bytes of a row), in both types of the output."""
     d_in = half * 2

@@ -7,7 +7,8 @@ import pytest
 import torch
 
 import paper_2405_13053_amd as m
-from tests.i8_kernels import PRODUCTS, TAILS
+from tests.i8_kernels import deal
+from tests.mx4_kernels import PRODUCTS, code_of
 
 OK, INVALID, UNSUPPORTED, WORKSPACE, HIP = range(5)
 F32, BF16 = 0, 1
@@ -139,15 +140,28 @@ def test_experts_refuse(lib):
     assert moe(inv=float("nan")) == INVALID and moe(io=ODDER) == UNSUPPORTED and moe(wo=ODDER) == UNSUPPORTED
 
 
-def test_products_take_the_kernels_of_as_many_bytes_in_8_bits():
-    """So the sizes that reach every kernel of those reach every kernel of these (tests/test_i8_kernels_host.py)."""
-    for T, d_in, d_out, N in PRODUCTS + [(*c, None) for cases in TAILS.values() for c in cases]:
-        assert m.gemm_mx4_kernel(T, 2 * d_in, d_out, N) == m.gemm_i8_kernel(T, d_in, d_out, N)
-    rng = random.Random(7)
+def test_every_kernel_that_sizes_lead_to_is_covered():
+    """The products of tests.mx4_kernels reach every kernel, and every copy of its loop, that gemm_mx4 starts for any size."""
+    code = lambda T, half, d_out, N: code_of(T, half, d_out, None if N is None else deal(T, N))
+    covered = set().union(*(code(*case) for case in PRODUCTS))
+    rng, seen = random.Random(7), {}
     spread = lambda lo, hi: int(math.exp(rng.uniform(math.log(lo), math.log(hi))))
-    for _ in range(20000):
-        T, d_in, d_out, N = spread(1, 12000), 16 * spread(1, 900), 8 * spread(1, 2000), rng.choice([None, 2, 3, 5, 8, 64])
-        assert m.gemm_mx4_kernel(T, 2 * d_in, d_out, N) == m.gemm_i8_kernel(T, d_in, d_out, N)
+    for _ in range(400000):
+        T, half, d_out, N = spread(1, 12000), 16 * spread(9, 900), 8 * spread(1, 2000), rng.choice([None, 2, 3, 5, 8])
+        if rng.random() < 0.5:
+            half = max(half // 128, 2) * 128
+        if T * d_out <= 2e8 and (rng.random() < 0.5 or half * d_out * (N or 1) >= 1e8):
+            for c in code(T, half, d_out, N):
+                seen.setdefault(c, (T, half, d_out, N))
+    missing = {c: case for c, case in seen.items() if c not in covered}
+    assert not missing, missing
+    assert len(covered) >= 100 and len({c[:4] for c in covered}) == 13   # tile shapes
+
+
+def test_up_to_256_inputs_take_one_kernel():
+    for d_in in range(32, 257, 32):
+        for T in (1, 64, 5000):
+            assert m.gemm_mx4_kernel(T, d_in, 4096)[0] == m.gemm_mx4_kernel(T, d_in, 4096, 28)[0] == "one"
 
 
 def test_the_query_refuses_what_the_product_refuses():
