@@ -958,7 +958,8 @@ constexpr int few_down_lds() { return KS * D * few_slot_bytes<WT, 1>(); }
 constexpr int kFewDownWaves = 8;
 template <typename WT> constexpr int kFewDownDepth = WT::kScales ? 4 : 5;
 
-// Wavefronts to a unit of the first product: rounds * K tiles of each, and a round's sum in LDS as half a K tile.
+// Wavefronts to a unit of the first product: rounds * K tiles of each, and a round's sum in LDS as half a K tile.  1, 2, 4 and 8 took 19.3, 15.1, 13.3
+// and 13.4 us for a token of 2 experts of 4096 and 1024 in 4 bits (it takes 4), 42.1, 42.9, 43.0 and 45.5 for 14336 channels (1).
 static int few_up_split(int units, int nk) {
     int best = 1;
     float least = 0.f;
@@ -968,12 +969,16 @@ static int few_up_split(int units, int nk) {
     }
     return best;
 }
-// Workgroups to a tile of the second product: rounds * K tiles of a wavefront, 0.4 us each, and a launch of 3.5 us that adds the parts
+// Workgroups to a tile of the second product: rounds * K tiles of a wavefront, 0.4 us each (of 4 bits 0.75), and a launch of 3.5 us that adds the parts.
+// 1, 2 and 4 took 40.3, 31.9 and 28.4 us for 8 experts of 512 and 4096 in bf16 (it takes 4), 24.8, 21.8 and 20.7 in 4 bits (2: 4 would leave
+// wavefronts without a K tile), 39.2, 44.3 and 53.7 for 8 of 4096 and 1024 in bf16 (1).
+template <typename WT>
 static int few_down_split(int tiles, int experts, int nk) {
+    constexpr float kTile = WT::kScales ? 0.75f : 0.4f;
     int best = 1;
     float least = 0.f;
     for (int S = 1; S <= kManySplits; S *= 2) {
-        const float us = (float)ceil_div(tiles * S, 256) * (float)(experts * ceil_div(ceil_div(nk, S), kFewDownWaves)) * 0.4f + (S > 1 ? 3.5f : 0.f);
+        const float us = (float)ceil_div(tiles * S, 256) * (float)(experts * ceil_div(ceil_div(nk, S), kFewDownWaves)) * kTile + (S > 1 ? 3.5f : 0.f);
         if (S > 1 && nk < kFewDownWaves * S) break;
         if (S == 1 || us < least) { least = us; best = S; }
     }
@@ -993,14 +998,19 @@ static hipError_t launch_gate(const ExpertsArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
+static int few_experts(const ExpertsArgs& a) { return a.T * a.k < a.N ? a.T * a.k : a.N; }   // in use, at most
+// The kernels for up to 4 tokens, or those for more: in 4 bits up to 8 experts.  2 of 32 experts of 4096 and 1024 take 13.6 us with these and 23.4 with those, 8 take
+// 21.8 and 28.7, 16 take 32.1 and 32.4; of 1024 and 1504 11.8 and 17.2, 20.2 and 20.5, 29.2 and 23.8.  In bf16 there is more to
+// read in the same K tiles: 16 of 4096 and 1024 64.8 and 75.3, of 1024 and 1504 37.2 and 35.9.
 template <typename WT>
-static bool few_fits(const ExpertsArgs& a) { return a.T <= kFewTokens && a.T * few_row_bytes<WT>(a.d) <= kFewRowsMost; }
+static bool few_fits(const ExpertsArgs& a) {
+    return a.T <= kFewTokens && a.T * few_row_bytes<WT>(a.d) <= kFewRowsMost && (!WT::kScales || few_experts(a) <= 8);
+}
 
 template <typename WT>
 static hipError_t launch_few(const ExpertsArgs& a, hipStream_t stream) {
     constexpr int DD = kFewDownDepth<WT>;
-    const int most = a.T * a.k < a.N ? a.T * a.k : a.N;   // experts in use
-    const int rows = a.T * few_row_bytes<WT>(a.d), KS = few_up_split(most * ceil_div(a.f, 16), ceil_div(WT::row_bytes(a.d), 128));
+    const int most = few_experts(a), rows = a.T * few_row_bytes<WT>(a.d), KS = few_up_split(most * ceil_div(a.f, 16), ceil_div(WT::row_bytes(a.d), 128));
     const auto up = [&](auto kern) {
         const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(kern), few_up_lds<WT>(kFewRowsMost, KS > 1));
         if (e != hipSuccess) return e;
@@ -1010,7 +1020,7 @@ static hipError_t launch_few(const ExpertsArgs& a, hipStream_t stream) {
     const hipError_t e = KS == 1 ? up(&experts_few_up_kernel<WT, 1>) : KS == 2 ? up(&experts_few_up_kernel<WT, 2>)
                        : KS == 4 ? up(&experts_few_up_kernel<WT, 4>) : up(&experts_few_up_kernel<WT, 8>);
     if (e != hipSuccess) return e;
-    const int tiles = ceil_div(a.d, 16), splits = few_down_split(tiles, most, ceil_div(WT::row_bytes(a.f), 128));
+    const int tiles = ceil_div(a.d, 16), splits = few_down_split<WT>(tiles, most, ceil_div(WT::row_bytes(a.f), 128));
     const auto down = &experts_few_down_kernel<WT, kFewDownWaves, DD>;
     const hipError_t f = ensure_lds_limit(reinterpret_cast<const void*>(down), few_down_lds<WT, kFewDownWaves, DD>());
     if (f != hipSuccess) return f;
@@ -1038,6 +1048,7 @@ static hipError_t launch(ExpertsArgs a, hipStream_t stream) {
         a.W_gate = nullptr;   // done
     }
     if (few) return launch_few<WT>(a, stream);
+    // blocks of 16 or of 32 tokens: 64 tokens of 2 of 8 experts of 4096 and 3584 62.0 and 49.9 us, 32 tokens 43.6 and 48.6
     return a.T * a.k <= 10 * a.N || a.T <= 16 ? launch_many<WT, 1>(a, stream) : launch_many<WT, 2>(a, stream);
 }
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t stream) {
