@@ -7,15 +7,16 @@
 // v_mfma_f32_16x16x32_bf16 with x as it is: W is the first operand, the tokens are the 16 columns of the second.  h is rounded to bf16 once, as
 // the operand of the second product; sums are fp32.
 //
-// The weights of the experts in use are what there is to read, once.  Every wavefront streams its rows of them through a ring of its own
-// (see gemm_rows.hpp), K tiles of 128 bytes a row, with the tokens' rows beside them.  Which tokens an expert has every workgroup finds out
-// for itself: a lane holds an expert's tokens as the bits of a word.  Two launches, and a third for more than 4 tokens:
+// The weights of the experts in use are what there is to read, once, and what the time goes into: 2 experts of 4096 and 14336 in 4 bits, 187 MB, take 42 us
+// (4.5 TB/s), 8 of them and 64 tokens 154 (4.9).  Every wavefront streams its rows through a ring of its own (see gemm_rows.hpp), K tiles of 128 bytes
+// a row.  Which tokens an expert has every workgroup finds out for itself: a lane holds an expert's tokens as the bits of a word.
 //
-// up to 4 tokens: the four columns are the tokens.  experts_few_up_kernel: 16 channels of h (32 rows of W1) to a wavefront, or to the
-//   four of a workgroup, which split K then.  experts_few_down_kernel: 16 channels of the output to a workgroup, whose wavefronts split K and go
-//   through the experts in use one after the other, so that the weighted sum is in registers and nothing is added in memory.
-// more: an expert's tokens are columns, 16 or 32 at a time, read once for the four wavefronts of a workgroup, which have rows of W of
-//   their own.  experts_up_kernel and experts_down_kernel; experts_sum_kernel adds the rows of a token.
+// up to 4 tokens: the tokens are the columns, 16 rows of W the rows.  experts_few_up_kernel, with the gate of a single token in it, and
+//   experts_few_down_kernel, where the wavefronts split K and go through the experts in use one after the other, so that the weighted sum is in
+//   registers; where there are few channels workgroups split K too, and experts_few_sum_kernel adds.
+// more: an expert's tokens are columns, 16 or 32 at a time, read once for the wavefronts of a workgroup, which have rows of W of their
+//   own.  experts_many_kernel for either product, experts_sum_kernel for the rows of a token.
+// In front of them gate_part_kernel, and beyond kRouteTokens tokens experts_route_kernel.  Sums are added in one order: results repeat.
 #include <stddef.h>
 
 #include <type_traits>
@@ -331,23 +332,23 @@ constexpr int few_up_lds(int rows_bytes, bool sums) { return kFewWaves * (kFewDe
 static_assert(few_up_lds<Mx4Weights>(kFewRowsMost, true) + 1024 <= 160 * 1024, "LDS");
 
 // The gate of one token by every workgroup for itself, from x in LDS (zeros at `pad`): two rows of W_gate to a thread and step, all steps on their way at
-// once.  sums: [wavefront][NP], which whoever routes adds up.  A layer of 28 experts of 1024 inputs takes 15.3 us so, with gate_part_kernel in front 16.6,
-// of 8 experts of 1024 14.0 and 17.5; of more tokens every workgroup has too much to add up (4 tokens of 8 experts of 4096: 24.8 and 20.6).
-constexpr int kGateHere = 32768, kGatePairs = kGateHere / (2 * kFewWaves * 64);
-__device__ __forceinline__ void load_gate(const ExpertsArgs& a, int lane, int wave, float (&w)[2 * kGatePairs]) {
+// once, up to two passes of them.  A layer of 28 experts of 1024 inputs takes 14.8 us so, with gate_part_kernel in front 16.6, of 8 of 1024 14.0 and
+// 17.5; two passes, 64 experts of 1024, 19.4 and 19.9.  Of more tokens every workgroup has too much to add up (4 of 8 experts of 4096: 24.8 and 20.6).
+constexpr int kGateHere = 65536, kGatePairs = 32, kGatePass = 2 * kGatePairs * kFewWaves * 64;
+__device__ __forceinline__ void load_gate(const ExpertsArgs& a, int lane, int wave, int pass, float (&w)[2 * kGatePairs]) {
     const int NP = gate_columns(a.N), col = lane & (NP - 1), each = 64 / NP;
     const auto W = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.W_gate), 0, (uint32_t)(a.d * a.N) * 4u, 0x00020000);   // zeros behind the last row
     const uint32_t row = (uint32_t)a.N * 4, step = 2 * kFewWaves * each * row;
-    uint32_t at = col < a.N ? 2 * (wave * each + lane / NP) * row + col * 4 : kOutside;
+    uint32_t at = col < a.N ? 2 * ((pass * kGatePairs * kFewWaves + wave) * each + lane / NP) * row + col * 4 : kOutside;
 #pragma unroll
     for (int i = 0; i < kGatePairs; ++i, at += step) {
         w[2 * i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(W, at, 0, 0));
         w[2 * i + 1] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(W, at + row, 0, 0));
     }
 }
-__device__ __forceinline__ void gate_here(const ExpertsArgs& a, const float (&w)[2 * kGatePairs], const unsigned char* x, int pad, int lane, int wave, float* sums) {
+__device__ __forceinline__ float gate_here(const ExpertsArgs& a, const float (&w)[2 * kGatePairs], const unsigned char* x, int pad, int lane, int wave, int pass) {
     const int NP = gate_columns(a.N), each = 64 / NP;
-    int at = (wave * each + lane / NP) * 4;
+    int at = ((pass * kGatePairs * kFewWaves + wave) * each + lane / NP) * 4;
     float s[4] = {};
 #pragma unroll
     for (int i = 0; i < kGatePairs; ++i, at += kFewWaves * each * 4) {
@@ -355,9 +356,7 @@ __device__ __forceinline__ void gate_here(const ExpertsArgs& a, const float (&w)
         s[i & 3] = fmaf(__uint_as_float(v << 16), w[2 * i], s[i & 3]);
         s[i & 3] = fmaf(__uint_as_float(v & 0xffff0000u), w[2 * i + 1], s[i & 3]);
     }
-    float sum = (s[0] + s[1]) + (s[2] + s[3]);
-    for (int off = NP; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
-    if (lane < NP) sums[wave * NP + lane] = sum;
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 template <typename WT, int KS>
@@ -390,12 +389,18 @@ __global__ __launch_bounds__(kFewWaves * 64) void experts_few_up_kernel(const Ex
             float* const logits = reinterpret_cast<float*>(smem);   // in the rings' place
             const int NP = gate_columns(a.N);
             float held[2 * kGatePairs];
-            load_gate(a, lane, wave, held);
+            load_gate(a, lane, wave, 0, held);
             const float b = a.bias != nullptr && lane < a.N ? a.bias[lane] : 0.f;
             if (tid < 4) reinterpret_cast<uint32_t*>(rows + row_bytes - 16)[tid] = 0;
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // x
             __syncthreads();
-            gate_here(a, held, rows, row_bytes - 16, lane, wave, logits);
+            float sum = gate_here(a, held, rows, row_bytes - 16, lane, wave, 0);
+            if (a.d * NP > kGatePass) {
+                load_gate(a, lane, wave, 1, held);
+                sum += gate_here(a, held, rows, row_bytes - 16, lane, wave, 1);
+            }
+            for (int off = NP; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
+            if (lane < NP) logits[wave * NP + lane] = sum;
             __syncthreads();
             if (wave == 0) {
                 float g = 0.f;
@@ -956,7 +961,11 @@ static hipError_t start(K kern, int grid, int threads, int lds, const ExpertsArg
 template <typename WT, int KS, int D>
 constexpr int few_down_lds() { return KS * D * few_slot_bytes<WT, 1>(); }
 constexpr int kFewDownWaves = 8;
-template <typename WT> constexpr int kFewDownDepth = WT::kScales ? 4 : 5;
+// K tiles of a ring.  Where there are more workgroups than CUs shorter rings let two share one: a token of 2 experts of 4608 and 5888 in 4 bits 31.0 us, in
+// two rounds of the longer rings 34.9, of 5120 and 4096 in bf16 55.2 and 61.9.
+template <typename WT> constexpr int kFewDownDepth = WT::kScales ? 4 : 5;    // one workgroup to a CU
+template <typename WT> constexpr int kFewDownDepth2 = WT::kScales ? 2 : 3;   // two
+static_assert(2 * (few_down_lds<Mx4Weights, kFewDownWaves, 2>() + 4096) <= 160 * 1024 && 2 * (few_down_lds<Bf16Weights, kFewDownWaves, 3>() + 4096) <= 160 * 1024, "LDS");
 
 // Wavefronts to a unit of the first product: rounds * K tiles of each, and a round's sum in LDS as half a K tile.  1, 2, 4 and 8 took 19.3, 15.1, 13.3
 // and 13.4 us for a token of 2 experts of 4096 and 1024 in 4 bits (it takes 4), 42.1, 42.9, 43.0 and 45.5 for 14336 channels (1).
@@ -1009,7 +1018,7 @@ static bool few_fits(const ExpertsArgs& a) {
 
 template <typename WT>
 static hipError_t launch_few(const ExpertsArgs& a, hipStream_t stream) {
-    constexpr int DD = kFewDownDepth<WT>;
+    constexpr int DD = kFewDownDepth<WT>, D2 = kFewDownDepth2<WT>;
     const int most = few_experts(a), rows = a.T * few_row_bytes<WT>(a.d), KS = few_up_split(most * ceil_div(a.f, 16), ceil_div(WT::row_bytes(a.d), 128));
     const auto up = [&](auto kern) {
         const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(kern), few_up_lds<WT>(kFewRowsMost, KS > 1));
@@ -1021,10 +1030,15 @@ static hipError_t launch_few(const ExpertsArgs& a, hipStream_t stream) {
                        : KS == 4 ? up(&experts_few_up_kernel<WT, 4>) : up(&experts_few_up_kernel<WT, 8>);
     if (e != hipSuccess) return e;
     const int tiles = ceil_div(a.d, 16), splits = few_down_split<WT>(tiles, most, ceil_div(WT::row_bytes(a.f), 128));
-    const auto down = &experts_few_down_kernel<WT, kFewDownWaves, DD>;
-    const hipError_t f = ensure_lds_limit(reinterpret_cast<const void*>(down), few_down_lds<WT, kFewDownWaves, DD>());
+    const auto down = [&](auto kern, int lds) {
+        const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(kern), lds);
+        if (e != hipSuccess) return e;
+        kern<<<tiles * splits, kFewDownWaves * 64, lds, stream>>>(a, splits);
+        return hipGetLastError();
+    };
+    const hipError_t f = tiles * splits <= 256 ? down(&experts_few_down_kernel<WT, kFewDownWaves, DD>, few_down_lds<WT, kFewDownWaves, DD>())
+                                               : down(&experts_few_down_kernel<WT, kFewDownWaves, D2>, few_down_lds<WT, kFewDownWaves, D2>());
     if (f != hipSuccess) return f;
-    down<<<tiles * splits, kFewDownWaves * 64, few_down_lds<WT, kFewDownWaves, DD>(), stream>>>(a, splits);
     if (splits > 1) experts_few_sum_kernel<<<ceil_div(a.T * a.d, 1024), 256, 0, stream>>>(a, splits);
     return hipGetLastError();
 }
@@ -1070,6 +1084,7 @@ static hipError_t init_experts() {   // every kernel that launch_experts may sta
     set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 4>), few_up_lds<WT>(kFewRowsMost, true));
     set(reinterpret_cast<const void*>(&experts_few_up_kernel<WT, 8>), few_up_lds<WT>(kFewRowsMost, true));
     set(reinterpret_cast<const void*>(&experts_few_down_kernel<WT, kFewDownWaves, DD>), few_down_lds<WT, kFewDownWaves, DD>());
+    set(reinterpret_cast<const void*>(&experts_few_down_kernel<WT, kFewDownWaves, kFewDownDepth2<WT>>), few_down_lds<WT, kFewDownWaves, kFewDownDepth2<WT>>());
     set(reinterpret_cast<const void*>(&experts_many_kernel<WT, true, 1>), many_lds<WT, 1>());
     set(reinterpret_cast<const void*>(&experts_many_kernel<WT, true, 2>), many_lds<WT, 2>());
     set(reinterpret_cast<const void*>(&experts_many_kernel<WT, false, 1>), many_lds<WT, 1>());

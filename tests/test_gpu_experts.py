@@ -187,9 +187,10 @@ def test_moe_forward(T, N, k, d, f, inv, mx4):
 
 
 @pytest.mark.parametrize("mx4", [True, False])
-@pytest.mark.parametrize("N,k,d", [(64, 8, 512), (28, 4, 1024), (28, 3, 1056), (8, 2, 4096), (8, 2, 4128), (3, 2, 64), (16, 1, 1376), (1, 1, 32)])
+@pytest.mark.parametrize("N,k,d", [(64, 8, 512), (28, 4, 1024), (28, 3, 1056), (8, 2, 4096), (8, 2, 4128), (3, 2, 64), (16, 1, 1376), (1, 1, 32),
+                                   (64, 8, 1024), (28, 4, 2048), (28, 4, 2080), (5, 2, 8192), (5, 2, 8224)])
 def test_moe_forward_of_one_token(N, k, d, mx4):
-    """Up to 32768 columns and rows of the gate in the first product's workgroups, beyond that a launch in front."""
+    """Up to 65536 columns times rows of the gate in the first product's workgroups, beyond that a launch in front."""
     test_moe_forward(1, N, k, d, 96, 1.0, mx4)
 
 
