@@ -31,15 +31,11 @@ meteora_status check_weights(const uint8_t* W, const uint8_t* w_scale, int T, in
 size_t base_gemm_bytes(int T, int d_in) {   // the quantised rows, then their scales
     return align_up((size_t)T * (d_in / 2), 256) + align_up(mx4_scale_bytes(T, d_in), 256);
 }
-// The transposed values, then the K splits of few tokens (bf16), which number the contraction's outputs d_in
+// The gradient's: the transposed values, then (bf16) the parts of a split contraction, which numbers the outputs d_in.  Where it reads the codes
+// themselves the parts are in the values' place.
 size_t values_bytes(int d_in, int d_out, meteora_dtype dt) { return align_up((size_t)d_in * d_out * (dt == METEORA_BF16 ? 2 : 4), 256); }
-// Up to 64 tokens K is split where the contraction is long: dequantisation and product, split and not, 2 x 12336 -> 672 27.4 and 52.5 us, 64 x 14336 -> 4096
-// 50.5 and 65.8, 64 x 4096 -> 14336 48.8 and 44.5, 1 x 4096 -> 4096 31.8 and 21.5.
-bool splits_few_tokens(int T, int d_out) { return T <= 64 && d_out >= 8192; }
 size_t splits_bytes(int T, int d_in, int d_out, meteora_dtype dt) {
-    if (dt != METEORA_BF16) return 0;
-    const int S = gemm_few_tile_splits(T, d_out, d_in);
-    return S > 0 ? (size_t)S * T * d_in * sizeof(float) : splits_few_tokens(T, d_out) ? gemm_splitk_bytes(T, d_out, d_in, true) : 0;
+    return dt == METEORA_BF16 && !mx4_back_takes(T, d_in) ? (size_t)gemm_few_tile_splits(T, d_out, d_in) * T * d_in * sizeof(float) : 0;
 }
 
 }  // namespace
@@ -127,13 +123,15 @@ meteora_status meteora_base_gemm_mx4_backward(const void* dy, const uint8_t* W, 
     if (T == 0) return METEORA_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool bf16 = dt == METEORA_BF16;
+    if (bf16 && mx4_back_takes(T, d_in))
+        return status(launch_mx4_back(dy, W, w_scale, T, d_in, d_out, dx, ws, values_bytes(d_in, d_out, dt), st));
     hipError_t e = launch_dequantize_mx4(W, w_scale, d_out, d_in, true, bf16, ws, st);
     if (e != hipSuccess) return METEORA_ERR_HIP;
     float* const splits = reinterpret_cast<float*>(static_cast<char*>(ws) + values_bytes(d_in, d_out, dt));
     if (bf16 && gemm_few_tile_splits(T, d_out, d_in) > 0)
         e = launch_gemm_few_tiles(dy, ws, T, d_out, d_in, nullptr, 0, nullptr, 0, dx, splits, st);
     else
-        e = launch_gemm(dy, ws, T, d_out, d_in, bf16, nullptr, 0, nullptr, 0, dx, 0, bf16 && splits_few_tokens(T, d_out) ? splits : nullptr, st);
+        e = launch_gemm(dy, ws, T, d_out, d_in, bf16, nullptr, 0, nullptr, 0, dx, 0, nullptr, st);
     return status(e);
 }
 

@@ -54,6 +54,8 @@ hipError_t init_kernels() {
     if (e != hipSuccess) return e;
     e = gemm_mx4_init_kernels();
     if (e != hipSuccess) return e;
+    e = mx4_back_init_kernels();
+    if (e != hipSuccess) return e;
     e = experts_init_kernels();
     if (e != hipSuccess) return e;
     return bucket_init_scratch();
