@@ -1,4 +1,4 @@
-// Gradient of a projection with its weight in 4 bits (quant_mx4.hpp) with respect to a few tokens' rows, from the codes themselves:
+// Gradient of a projection with its weight in 4 bits (quant_mx4.hpp) with respect to its input, of a few tokens in bf16, from the codes themselves:
 //
 //     dx[t,i] = sum_o dy[t,o] * 2^(E[o, i / 32] - 127) * W[o,i]
 //
@@ -7,7 +7,7 @@
 // terms of one input's sum, a lane's part of the first operand of v_mfma_f32_16x16x32_bf16.  The 16 rows of that operand are inputs 8 apart,
 // one of each lane's, and its 8 instructions to 16 tokens together give every lane 8 consecutive inputs of a token.
 //
-// A workgroup has 128 inputs and up to 64 tokens; its 8 wavefronts, and `splits` workgroups, share out the rows of W, 32 to a step.  A wavefront's steps
+// A workgroup has 128 inputs and up to 64 tokens (fp32: 32); its 8 wavefronts, and `splits` workgroups, share out the rows of W, 32 to a step.  A wavefront's steps
 // come through a ring of its own in LDS: 64 bytes of each row, its 16 bytes of scales, and 32 columns of dy.  The wavefronts' sums are added
 // in LDS, the workgroups' by a second launch, in one order.
 #include "common.hpp"
@@ -18,15 +18,16 @@
 
 namespace meteora {
 
-constexpr int kBackWaves = 8, kBackInputs = 128, kBackStep = 32, kBackTokens = 64;
+constexpr int kBackWaves = 8, kBackInputs = 128, kBackStep = 32;
+template <typename TX> constexpr int kBackTokens = sizeof(TX) == 2 ? 64 : 32;   // of a workgroup
 constexpr int kBackSum = 8 * (1024 + 16);   // bytes of a wavefront's sums of 16 tokens: 8 registers of 4 values; 4 banks apart
 
 struct MxBackArgs {
-    const bf16_t* dy;        // [T, d_out]
+    const void* dy;          // [T, d_out]
     const uint8_t *W, *scale;
-    bf16_t* dx;              // [T, d_in], without splits
+    void* dx;                // [T, d_in], without splits
     float* part;             // [splits][T, d_in], or nullptr
-    int T, d_in, d_out, tiles, blocks, splits;   // of 128 inputs, of 64 tokens
+    int T, d_in, d_out, tiles, blocks, splits;   // of 128 inputs, of kBackTokens tokens
 };
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t back_rsrc(const void* p, uint32_t bytes) {
@@ -40,43 +41,79 @@ __device__ __forceinline__ f32x4 back_mfma(const bf16x8& w, const bf16x8& x, con
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, acc, 0, 0, 0);
 }
 
-template <int TB> constexpr int back_slot() { return 2048 + 1024 + TB * 1024; }
-template <int TB> constexpr int kBackDepth = TB == 1 ? 4 : TB == 2 ? 3 : 2;
-template <int TB>
+template <typename TX, int TB> constexpr int back_slot() { return 2048 + 1024 + TB * 512 * (int)sizeof(TX); }
+template <typename TX, int TB> constexpr int kBackDepth = back_slot<TX, TB>() <= 4096 ? 4 : back_slot<TX, TB>() <= 5120 ? 3 : 2;
+template <typename TX, int TB>
 constexpr int back_lds() {
-    constexpr int ring = kBackWaves * kBackDepth<TB> * back_slot<TB>(), sums = kBackWaves * (TB < 2 ? TB : 2) * kBackSum;
+    constexpr int ring = kBackWaves * kBackDepth<TX, TB> * back_slot<TX, TB>(), sums = kBackWaves * (TB < 2 ? TB : 2) * kBackSum;
     return ring > sums ? ring : sums;
 }
-static_assert(back_lds<1>() <= 160 * 1024 && back_lds<2>() <= 160 * 1024 && back_lds<4>() <= 160 * 1024, "LDS");
+static_assert(back_lds<bf16_t, 1>() <= 160 * 1024 && back_lds<bf16_t, 2>() <= 160 * 1024 && back_lds<bf16_t, 4>() <= 160 * 1024, "LDS");
+static_assert(back_lds<float, 1>() <= 160 * 1024 && back_lds<float, 2>() <= 160 * 1024, "LDS");
+
+// 8 columns of a token as operands: a bf16 number is one, an fp32 number the sum of three, its first 8 bits, the next 8 and the last.  Products with W's two
+// bits are exact, so that the sum is as good as one of fp32 products, at a third of the bf16 rate, five times that of fp32.  What is no number stays
+// in the first; the parts of one under 2^-110 may be lost under the least bf16 number.
+template <typename TX> constexpr int kBackParts = sizeof(TX) == 2 ? 1 : 3;
+__device__ __forceinline__ void back_parts(const unsigned char* tokens, int l15, int kq, bf16x8 (&x)[1]) {
+    x[0] = *reinterpret_cast<const bf16x8*>(tokens + (l15 * 4 + kq) * 16);
+}
+__device__ __forceinline__ void back_parts(const unsigned char* tokens, int l15, int kq, bf16x8 (&x)[3]) {   // 16-byte piece c of row t is at c ^ t % 8
+    u32x4 part[3];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(tokens + l15 * 128 + ((kq * 2 + h) ^ (l15 & 7)) * 16);
+        uint32_t p[3][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t u = v[i], size = u & 0x7fffffffu;
+            const bool number = size < 0x7f800000u;
+            p[0][i] = size > 0x7f800000u ? u | 0x00400000u : u;
+            const float rest = number ? __uint_as_float(u) - __uint_as_float(u & 0xffff0000u) : 0.f;
+            p[1][i] = __float_as_uint(rest);
+            p[2][i] = __float_as_uint(rest - __uint_as_float(p[1][i] & 0xffff0000u));
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) part[k][h * 2 + i] = __builtin_amdgcn_perm(p[k][2 * i + 1], p[k][2 * i], 0x07060302u);   // the upper halves
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) x[k] = __builtin_bit_cast(bf16x8, part[k]);
+}
+__device__ __forceinline__ void back_store(bf16_t* to, float a, float b) { *reinterpret_cast<uint32_t*>(to) = pack_bf16x2(a, b); }
+__device__ __forceinline__ void back_store(float* to, float a, float b) { *reinterpret_cast<float2*>(to) = make_float2(a, b); }
 
 // Offsets stay in 31 bits: 64 rows of dy are 128 MB at most, 32 of W 2 MB.  What bounds it is how soon the codes come (1 token of 5120 -> 13824, 38 MB, 14 us
 // and 3 for the second launch) and, from 33 tokens on, the matrix instructions: 512 x 4096 -> 4096 0.69 PFLOP/s, 512 x 4096 -> 14336 0.82.
-template <int TB>
+template <typename TX, int TB>
 __global__ __launch_bounds__(kBackWaves * 64) void gemm_mx4_back_kernel(const MxBackArgs a) {
-    constexpr int D = kBackDepth<TB>, NL = 3 + TB, kSlot = back_slot<TB>();
+    constexpr int D = kBackDepth<TX, TB>, EB = sizeof(TX), kSlot = back_slot<TX, TB>();
+    constexpr int PER = EB * 2, ROWS = 64 / PER, ND = TB * 16 / ROWS, NL = 3 + ND, P = kBackParts<TX>;   // 16-byte pieces of a token, tokens of a load instruction
     static_assert((D - 1) * NL < 64, "vmcnt");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l15 = lane & 15, kq = lane >> 4;
     const int id = xcd_order(blockIdx.x, a.tiles * a.blocks * a.splits);   // blocks of tokens, then tiles of the same rows next to each other
     const int block = id % a.blocks, rest = id / a.blocks, part = rest / a.tiles, i0 = (rest - part * a.tiles) * kBackInputs;
-    const int t0 = block * kBackTokens, tokens = min(kBackTokens, a.T - t0);
+    const int t0 = block * kBackTokens<TX>, tokens = min(kBackTokens<TX>, a.T - t0);
     const int all = ceil_div(a.d_out, kBackStep), share = ceil_div(all, a.splits), end = min(all, part * share + share);
-    const uint32_t bytes = (uint32_t)a.d_in / 2, ld = (uint32_t)a.d_out * 2;
+    const uint32_t bytes = (uint32_t)a.d_in / 2, ld = (uint32_t)a.d_out * EB;
 
     // Row kq * 8 + r of a step lies at position r * 4 + kq, so that a read of the four kq's is one piece of LDS
     const auto row_at = [](int p) { return (p & 3) * 8 + (p >> 2); };
-    uint32_t at_w[2], at_dy[TB];
+    uint32_t at_w[2], at_dy[ND];
     const uint32_t chunk = (uint32_t)i0 / 2 + (lane & 3) * 16;   // d_in % 32 == 0: there or not
 #pragma unroll
     for (int j = 0; j < 2; ++j) at_w[j] = chunk < bytes ? (uint32_t)row_at(j * 16 + (lane >> 2)) * bytes + chunk : kOutside;
+    const int piece = EB == 2 ? lane & 3 : (lane & 7) ^ (lane >> 3);   // of dy, see back_parts
     const uint32_t at_s = lane < kBackStep ? (uint32_t)row_at(lane) * 16 : kOutside;
 #pragma unroll
-    for (int b = 0; b < TB; ++b) {
-        const int t = b * 16 + (lane >> 2);
-        at_dy[b] = t < tokens ? (uint32_t)t * ld + (lane & 3) * 16 : kOutside;
+    for (int b = 0; b < ND; ++b) {
+        const int t = b * ROWS + lane / PER;
+        at_dy[b] = t < tokens ? (uint32_t)t * ld + piece * 16 : kOutside;
     }
-    const auto dy = back_rsrc(a.dy + (size_t)t0 * a.d_out, (uint32_t)tokens * ld);
+    const auto dy = back_rsrc(static_cast<const TX*>(a.dy) + (size_t)t0 * a.d_out, (uint32_t)tokens * ld);
     const uint8_t* const scale = a.scale + (size_t)(i0 / kMxChunk) * ((size_t)a.d_out * 16);
     unsigned char* const ring = smem + wave * D * kSlot;
     int req = part * share + wave, req_at = 0;
@@ -90,10 +127,10 @@ __global__ __launch_bounds__(kBackWaves * 64) void gemm_mx4_back_kernel(const Mx
         for (int j = 0; j < 2; ++j)
             back_load(w, slot + j * 1024, at_w[j]);
         back_load(s, slot + 2048, at_s);
-        const bool there = (lane & 3) * 8 < rows;   // columns of dy; d_out % 8 == 0
+        const bool there = piece * (16 / EB) < rows;   // columns of dy; d_out % 8 == 0
 #pragma unroll
-        for (int b = 0; b < TB; ++b)
-            back_load(dy, slot + 3072 + b * 1024, there && at_dy[b] != kOutside ? at_dy[b] + (uint32_t)o * 2 : kOutside);
+        for (int b = 0; b < ND; ++b)
+            back_load(dy, slot + 3072 + b * 1024, there && at_dy[b] != kOutside ? at_dy[b] + (uint32_t)o * EB : kOutside);
         req += kBackWaves;
     };
 #pragma unroll
@@ -110,13 +147,13 @@ __global__ __launch_bounds__(kBackWaves * 64) void gemm_mx4_back_kernel(const Mx
         at = at + 1 == D ? 0 : at + 1;
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * NL) : "memory");
         uint32_t w[8], e[8];
-        bf16x8 x[TB];
+        bf16x8 x[TB][P];
 #pragma unroll
         for (int r = 0; r < 8; ++r) w[r] = *reinterpret_cast<const uint32_t*>(slot + (r * 4 + kq) * 64 + l15 * 4);
 #pragma unroll
         for (int r = 0; r < 8; ++r) e[r] = *reinterpret_cast<const uint32_t*>(slot + 2048 + (r * 4 + kq) * 16 + (l15 >> 2) * 4);
 #pragma unroll
-        for (int b = 0; b < TB; ++b) x[b] = *reinterpret_cast<const bf16x8*>(slot + 3072 + b * 1024 + (l15 * 4 + kq) * 16);
+        for (int b = 0; b < TB; ++b) back_parts(slot + 3072 + b * 512 * EB, l15, kq, x[b]);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot is read
         request();
         u32x4 v[8];
@@ -128,7 +165,9 @@ __global__ __launch_bounds__(kBackWaves * 64) void gemm_mx4_back_kernel(const Mx
 #pragma unroll
             for (int k = 0; k < 4; ++k) f[k] = __builtin_amdgcn_perm(v[2 * k + 1][j >> 1], v[2 * k][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-            for (int b = 0; b < TB; ++b) acc[j][b] = back_mfma(__builtin_bit_cast(bf16x8, f), x[b], acc[j][b]);
+            for (int k = P - 1; k >= 0; --k)   // the smallest first
+#pragma unroll
+                for (int b = 0; b < TB; ++b) acc[j][b] = back_mfma(__builtin_bit_cast(bf16x8, f), x[b][k], acc[j][b]);
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land in what follows
@@ -155,60 +194,78 @@ __global__ __launch_bounds__(kBackWaves * 64) void gemm_mx4_back_kernel(const Mx
                 const int i = i0 + ((from >> 4) * 4 + c) * 8 + jq * 2;
                 const size_t o = (size_t)(t0 + t) * a.d_in + i;
                 if (i < a.d_in) {
-                    if (a.part != nullptr) *reinterpret_cast<float2*>(a.part + (size_t)part * a.T * a.d_in + o) = make_float2(sum[0][c], sum[1][c]);
-                    else *reinterpret_cast<uint32_t*>(a.dx + o) = pack_bf16x2(sum[0][c], sum[1][c]);
+                    if (a.part != nullptr) back_store(a.part + (size_t)part * a.T * a.d_in + o, sum[0][c], sum[1][c]);
+                    else back_store(static_cast<TX*>(a.dx) + o, sum[0][c], sum[1][c]);
                 }
             }
         }
     }
 }
 
-__global__ __launch_bounds__(256) void gemm_mx4_back_sum_kernel(const float* __restrict__ part, int splits, size_t all, bf16_t* __restrict__ dx) {
+template <typename TX>
+__global__ __launch_bounds__(256) void gemm_mx4_back_sum_kernel(const float* __restrict__ part, int splits, size_t all, TX* __restrict__ dx) {
     const size_t o = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (o >= all) return;
     f32x4 sum = *reinterpret_cast<const f32x4*>(part + o);
     for (int p = 1; p < splits; ++p) sum += *reinterpret_cast<const f32x4*>(part + (size_t)p * all + o);
-    *reinterpret_cast<uint2*>(dx + o) = make_uint2(pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3]));
+    back_store(dx + o, sum[0], sum[1]);
+    back_store(dx + o + 2, sum[2], sum[3]);
 }
 
 // Or dequantize_mx4_turned_kernel and a product of bf16 matrices, which reads W's 16 bits a value again, in tiles of more tokens.  From the codes and so, us:
 // 4096 -> 4096, 1, 32, 64, 256 and 512 tokens 10.1, 12.4, 16.7, 19.9, 24.9 and 30.6, 29.9, 31.1, 29.2, 33.1; 5120 -> 13824 17.9, 20.2, 25.1, 66.7, 125
 // and 62.9, 63.5, 65.6, 79.4, 110; 14336 -> 4096, 256 and 512, 448 and 896 workgroups, 48.9 and 93.0, and 59.5 and 75.6; 4096 -> 14336, 512, 256
-// workgroups, 73.5 and 92.6; 2048 -> 8192, 1024 and 1536 42.2 and 79.4, and 47.5 and 57.8.
-bool mx4_back_takes(int T, int d_in) {
-    return T <= 256 || (T <= 1024 && ceil_div(d_in, kBackInputs) * ceil_div(T, kBackTokens) <= 256);
+// workgroups, 73.5 and 92.6; 2048 -> 8192, 1024 and 1536 42.2 and 79.4, and 47.5 and 57.8.  fp32, with products of fp32 matrices: 4096 -> 4096, 1, 64, 512
+// and 2048 12.5, 19.5, 71.7 and 305, and 43.6, 79.2, 285 and 703; 5120 -> 13824 20.4, 44.0, 295 and 1021, and 213, 321, 1325 and 3824; beyond
+// 65536 tokens a grid might have too many workgroups.
+bool mx4_back_takes(int T, int d_in, bool bf16) {
+    if (!bf16) return T <= 65536;
+    return T <= 256 || (T <= 1024 && ceil_div(d_in, kBackInputs) * ceil_div(T, kBackTokens<bf16_t>) <= 256);
 }
 // Workgroups to a tile: as fill the CUs once, with a step to every wavefront, as far as there is room for their sums
-static int back_splits(int T, int d_in, int d_out, size_t room) {
-    const int tiles = ceil_div(d_in, kBackInputs) * ceil_div(T, kBackTokens), steps = ceil_div(d_out, kBackStep);
+static int back_splits(int T, int tiles, int d_in, int d_out, size_t room) {
+    const int steps = ceil_div(d_out, kBackStep);
     int n = tiles < 256 ? 256 / tiles : 1;
     n = n < steps / kBackWaves ? n : steps / kBackWaves;
     const size_t fit = room / ((size_t)T * d_in * sizeof(float));
     n = (size_t)n < fit ? n : (int)fit;
     return n < 1 ? 1 : ceil_div(steps, ceil_div(steps, n));   // none without steps
 }
-template <int TB>
-static hipError_t launch_back(const MxBackArgs& a, hipStream_t stream) {
-    const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_back_kernel<TB>), back_lds<TB>());
+template <typename TX, int TB>
+static hipError_t launch_tiles(const MxBackArgs& a, hipStream_t stream) {
+    const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_back_kernel<TX, TB>), back_lds<TX, TB>());
     if (e != hipSuccess) return e;
-    gemm_mx4_back_kernel<TB><<<a.tiles * a.blocks * a.splits, kBackWaves * 64, back_lds<TB>(), stream>>>(a);
+    gemm_mx4_back_kernel<TX, TB><<<a.tiles * a.blocks * a.splits, kBackWaves * 64, back_lds<TX, TB>(), stream>>>(a);
     return hipGetLastError();
 }
-hipError_t launch_mx4_back(const void* dy, const uint8_t* W, const uint8_t* scale, int T, int d_in, int d_out, void* dx, void* ws, size_t room,
-                           hipStream_t stream) {
-    const int splits = back_splits(T, d_in, d_out, room);
-    const MxBackArgs a{(const bf16_t*)dy, W, scale, (bf16_t*)dx, splits > 1 ? (float*)ws : nullptr, T, d_in, d_out, ceil_div(d_in, kBackInputs),
-                       ceil_div(T, kBackTokens), splits};
-    const hipError_t e = T <= 16 ? launch_back<1>(a, stream) : T <= 32 ? launch_back<2>(a, stream) : launch_back<4>(a, stream);
-    if (e != hipSuccess || splits == 1) return e;
-    const size_t all = (size_t)T * d_in;
-    gemm_mx4_back_sum_kernel<<<(int)((all + 1023) / 1024), 256, 0, stream>>>(a.part, splits, all, a.dx);
+template <typename TX>
+static hipError_t launch_back(MxBackArgs a, size_t room, hipStream_t stream) {
+    a.tiles = ceil_div(a.d_in, kBackInputs);
+    a.blocks = ceil_div(a.T, kBackTokens<TX>);
+    a.splits = back_splits(a.T, a.tiles * a.blocks, a.d_in, a.d_out, room);
+    float* const part = a.part;
+    if (a.splits == 1) a.part = nullptr;
+    hipError_t e;
+    if constexpr (sizeof(TX) == 2) e = a.T <= 16 ? launch_tiles<TX, 1>(a, stream) : a.T <= 32 ? launch_tiles<TX, 2>(a, stream) : launch_tiles<TX, 4>(a, stream);
+    else e = a.T <= 16 ? launch_tiles<TX, 1>(a, stream) : launch_tiles<TX, 2>(a, stream);
+    if (e != hipSuccess || a.splits == 1) return e;
+    const size_t all = (size_t)a.T * a.d_in;
+    gemm_mx4_back_sum_kernel<<<(int)((all + 1023) / 1024), 256, 0, stream>>>(part, a.splits, all, static_cast<TX*>(a.dx));
     return hipGetLastError();
+}
+hipError_t launch_mx4_back(const void* dy, const uint8_t* W, const uint8_t* scale, int T, int d_in, int d_out, bool bf16, void* dx, void* ws, size_t room,
+                           hipStream_t stream) {
+    const MxBackArgs a{dy, W, scale, dx, (float*)ws, T, d_in, d_out, 0, 0, 0};
+    return bf16 ? launch_back<bf16_t>(a, room, stream) : launch_back<float>(a, room, stream);
 }
 hipError_t mx4_back_init_kernels() {
-    hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_back_kernel<1>), back_lds<1>());
-    if (e == hipSuccess) e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_back_kernel<2>), back_lds<2>());
-    if (e == hipSuccess) e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_back_kernel<4>), back_lds<4>());
+    hipError_t e = hipSuccess;
+    const auto set = [&](auto kern, int lds) { if (e == hipSuccess) e = ensure_lds_limit(reinterpret_cast<const void*>(kern), lds); };
+    set(&gemm_mx4_back_kernel<bf16_t, 1>, back_lds<bf16_t, 1>());
+    set(&gemm_mx4_back_kernel<bf16_t, 2>, back_lds<bf16_t, 2>());
+    set(&gemm_mx4_back_kernel<bf16_t, 4>, back_lds<bf16_t, 4>());
+    set(&gemm_mx4_back_kernel<float, 1>, back_lds<float, 1>());
+    set(&gemm_mx4_back_kernel<float, 2>, back_lds<float, 2>());
     return e;
 }
 

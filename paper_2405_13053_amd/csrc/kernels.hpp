@@ -254,9 +254,9 @@ hipError_t launch_gemm_mx4(const uint8_t* q, const uint8_t* q_scale, const uint8
 bool base_gemm_mx4_in_one(int T, int d_in);   // the quantisation and the product of a few tokens in one launch
 hipError_t launch_base_gemm_mx4_in_one(const void* x, const uint8_t* W, const uint8_t* w_scale, int T, int d_in, int d_out, bool bf16, void* out,
                                        hipStream_t stream);
-// The gradient with respect to a few tokens' rows, bf16, from the codes; ws: `room` bytes for sums of parts
-bool mx4_back_takes(int T, int d_in);
-hipError_t launch_mx4_back(const void* dy, const uint8_t* W, const uint8_t* scale, int T, int d_in, int d_out, void* dx, void* ws, size_t room,
+// The gradient with respect to rows from the codes, for a few of them in bf16; ws: `room` bytes for sums of parts
+bool mx4_back_takes(int T, int d_in, bool bf16);
+hipError_t launch_mx4_back(const void* dy, const uint8_t* W, const uint8_t* scale, int T, int d_in, int d_out, bool bf16, void* dx, void* ws, size_t room,
                            hipStream_t stream);
 I8Plan gemm_mx4_plan(int T, int d_in, int d_out, int N, bool grouped);
 

@@ -23,7 +23,7 @@ def test_results_of_builtins_are_waited_for_on_every_path(source, kernels, tmp_p
                    stdout=subprocess.DEVNULL, stderr=subprocess.DEVNULL)
     text = asm.read_text()
     names = set(re.findall(r"^(_Z\S*(?:%s)\S*):" % kernels, text, re.M))
-    assert len(names) >= (3 if source == "gemm_mx4_back" else 10)
+    assert len(names) >= (5 if source == "gemm_mx4_back" else 10)
     text = text.replace("v_mfma_scale_f32_16x16x128_f8f6f4", waits.MFMA)
     assert names <= {fn for fn, op, _ in waits._parse(text)[0] if op == waits.MFMA}
     monkeypatch.setattr(waits, "AFTER", 8)

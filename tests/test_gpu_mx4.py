@@ -189,31 +189,36 @@ def test_base_gemm_mx4_and_its_gradient(T, d_in, d_out, dtype):
     close(dx, mx.product(dy.double(), V.t()), mx.product(dy.double().abs(), V.t().abs()), d_out)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T,d_in,d_out", [(1, 32, 8), (1, 128, 264), (15, 160, 4096), (16, 4096, 512), (17, 608, 8200), (32, 416, 4104), (33, 2080, 1376),
                                           (48, 1056, 1000), (64, 5120, 13824), (65, 96, 1160), (129, 4096, 72), (200, 544, 2056), (256, 14336, 1024),
                                           (257, 4096, 4096), (513, 4128, 520), (1000, 1376, 2080), (1024, 2048, 8192), (1025, 256, 9000), (320, 8224, 64),
-                                          (3, 131072, 64), (2, 64, 300000), (40, 32, 131072)])
-def test_gradient_from_the_codes(T, d_in, d_out):
-    """Its tiles of 128 inputs and 64 tokens, 32 outputs a step, with sums of parts and without; beyond 1024 tokens or 256 tiles by way of the values."""
+                                          (3, 131072, 64), (2, 64, 300000), (40, 32, 131072), (65536, 96, 40), (65537, 64, 40)])
+def test_gradient_from_the_codes(T, d_in, d_out, dtype):
+    """Its tiles of 128 inputs and 64 tokens (fp32: 32), 32 outputs a step, with sums of parts and without; beyond 1024 tokens or 256 tiles bf16 goes by way
+    of the values.  fp32 rows are three bf16 rows, whose products with two bits are exact and are added 32 at a time: 3 / 32 d_out additions."""
     g = gen(T + d_in + d_out)
     W, ws, V = operand(d_out, d_in, g)
-    dy = torch.randn((T, d_out), generator=g, device="cuda").bfloat16()
-    dx = torch.full((T + 1, d_in), 7.0, device="cuda", dtype=torch.bfloat16)
+    dy = torch.randn((T, d_out), generator=g, device="cuda").to(dtype)
+    dx = torch.full((T + 1, d_in), 7.0, device="cuda", dtype=dtype)
     m.base_gemm_mx4_backward(dy, W, ws, out=dx[:T])
     close(dx[:T], mx.product(dy.double(), V.t()), mx.product(dy.double().abs(), V.t().abs()), d_out)
     assert (dx[T] == 7).all()
     assert torch.equal(dx[:T], m.base_gemm_mx4_backward(dy, W, ws))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T", [2, 40, 100])
-def test_gradient_of_what_is_not_finite(T):
+def test_gradient_of_what_is_not_finite(T, dtype):
     """A row of dy with an infinity or a NaN keeps it to itself; a block of W without a number reaches its 32 inputs of every row."""
     g = gen(90 + T)
     W, ws = m.quantize_mx4(torch.randn((520, 416), generator=g, device="cuda"))
-    dy = torch.randn((T, 520), generator=g, device="cuda").bfloat16()
+    dy = torch.randn((T, 520), generator=g, device="cuda").to(dtype)
     clean = m.base_gemm_mx4_backward(dy, W, ws)
     bad = dy.clone()
     bad[1, 513] = float("nan")
+    if dtype == torch.float32:
+        bad.view(torch.int32)[1, 513] = 0x7f800001   # a NaN in the last bit only
     bad[0, 7] = float("inf")
     dx = m.base_gemm_mx4_backward(bad, W, ws)
     assert torch.equal(dx[2:], clean[2:]) and torch.isnan(dx[1]).all() and not torch.isfinite(dx[0]).any()
