@@ -20,6 +20,7 @@ namespace meteora {
 
 constexpr int kBackWaves = 8, kBackInputs = 128, kBackStep = 32;
 template <typename TX> constexpr int kBackTokens = sizeof(TX) == 2 ? 64 : 32;   // of a workgroup
+constexpr int kBackScales = kBackStep * kBackInputs / 2, kBackDy = kBackScales + 1024;   // where scales (of 32 rows; room for 64 pieces) and dy are in a slot
 constexpr int kBackSum = 8 * (1024 + 16);   // bytes of a wavefront's sums of 16 tokens: 8 registers of 4 values; 4 banks apart
 
 struct MxBackArgs {
@@ -41,7 +42,7 @@ __device__ __forceinline__ f32x4 back_mfma(const bf16x8& w, const bf16x8& x, con
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, acc, 0, 0, 0);
 }
 
-template <typename TX, int TB> constexpr int back_slot() { return 2048 + 1024 + TB * 512 * (int)sizeof(TX); }
+template <typename TX, int TB> constexpr int back_slot() { return kBackDy + TB * 512 * (int)sizeof(TX); }
 template <typename TX, int TB> constexpr int kBackDepth = back_slot<TX, TB>() <= 4096 ? 4 : back_slot<TX, TB>() <= 5120 ? 3 : 2;
 template <typename TX, int TB>
 constexpr int back_lds() {
@@ -126,11 +127,11 @@ __global__ __launch_bounds__(kBackWaves * 64) void gemm_mx4_back_kernel(const Mx
 #pragma unroll
         for (int j = 0; j < 2; ++j)
             back_load(w, slot + j * 1024, at_w[j]);
-        back_load(s, slot + 2048, at_s);
+        back_load(s, slot + kBackScales, at_s);
         const bool there = piece * (16 / EB) < rows;   // columns of dy; d_out % 8 == 0
 #pragma unroll
         for (int b = 0; b < ND; ++b)
-            back_load(dy, slot + 3072 + b * 1024, there && at_dy[b] != kOutside ? at_dy[b] + (uint32_t)o * EB : kOutside);
+            back_load(dy, slot + kBackDy + b * 1024, there && at_dy[b] != kOutside ? at_dy[b] + (uint32_t)o * EB : kOutside);
         req += kBackWaves;
     };
 #pragma unroll
@@ -151,9 +152,9 @@ __global__ __launch_bounds__(kBackWaves * 64) void gemm_mx4_back_kernel(const Mx
 #pragma unroll
         for (int r = 0; r < 8; ++r) w[r] = *reinterpret_cast<const uint32_t*>(slot + (r * 4 + kq) * 64 + l15 * 4);
 #pragma unroll
-        for (int r = 0; r < 8; ++r) e[r] = *reinterpret_cast<const uint32_t*>(slot + 2048 + (r * 4 + kq) * 16 + (l15 >> 2) * 4);
+        for (int r = 0; r < 8; ++r) e[r] = *reinterpret_cast<const uint32_t*>(slot + kBackScales + (r * 4 + kq) * 16 + (l15 >> 2) * 4);
 #pragma unroll
-        for (int b = 0; b < TB; ++b) back_parts(slot + 3072 + b * 512 * EB, l15, kq, x[b]);
+        for (int b = 0; b < TB; ++b) back_parts(slot + kBackDy + b * 512 * EB, l15, kq, x[b]);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot is read
         request();
         u32x4 v[8];
