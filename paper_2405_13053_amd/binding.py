@@ -746,37 +746,48 @@ def experts_workspace_bytes(T, d, f, N, k) -> int:
     return int(load_library().meteora_experts_workspace_bytes(T, d, f, N, k))
 
 
-def _chk_experts(x, W1, W2, w1_scale, w2_scale, base, out):
-    """Checks what experts_forward and moe_forward share; (d, f, N)."""
+def _chk_experts(x, W1, W2, w1_scale, w2_scale, base, out, ws):
+    """Checks what experts_forward and moe_forward share; (T, d, f, N)."""
     T, d = x.shape
     N, d2, cols = W2.shape
-    mx4 = w1_scale is not None
-    f = cols * 2 if mx4 else cols
+    dtype = x.dtype
     if (w1_scale is None) != (w2_scale is None):
         raise ValueError("W1 and W2 are both in 4 bits, with scales, or neither")
     # written out, as in linear_forward
-    if not (x.is_cuda and x.is_contiguous() and W1.is_contiguous() and W2.is_contiguous() and out.is_contiguous() and out.dtype == x.dtype and
-            out.shape == (T, d) and d2 == d and W1.shape == (N, 2 * f, d // 2 if mx4 else d) and
-            W1.dtype == W2.dtype == (torch.uint8 if mx4 else x.dtype) and
-            (base is None or (base.dtype == x.dtype and base.shape == (T, d) and base.is_contiguous()))):
-        wt = torch.uint8 if mx4 else x.dtype
+    if w1_scale is None:
+        f = cols
+        ok = W1.dtype == W2.dtype == dtype and W1.shape == (N, 2 * f, d)
+    else:
+        f = cols * 2
+        ok = (W1.dtype == W2.dtype == w1_scale.dtype == w2_scale.dtype == torch.uint8 and W1.shape == (N, 2 * f, d // 2) and
+              w1_scale.shape == (N, (d + 511) // 512, 2 * f, 16) and w2_scale.shape == (N, (f + 511) // 512, d, 16) and
+              w1_scale.is_contiguous() and w2_scale.is_contiguous())
+    if not (ok and x.is_cuda and x.is_contiguous() and W1.is_contiguous() and W2.is_contiguous() and out.is_contiguous() and
+            out.dtype == dtype and out.shape == (T, d) and d2 == d and
+            (base is None or (base.dtype == dtype and base.shape == (T, d) and base.is_contiguous())) and
+            (ws is None or (ws.dtype == torch.uint8 and ws.is_contiguous()))):
+        mx4 = w1_scale is not None
+        wt = torch.uint8 if mx4 else dtype
         _chk(x, "x"); _chk(W1, "W1", wt, (N, 2 * f, d // 2 if mx4 else d)); _chk(W2, "W2", wt, (N, d, cols))
-        _chk(base, "base", x.dtype, (T, d)); _chk(out, "out", x.dtype, (T, d))
-    if mx4:
-        _chk(w1_scale, "w1_scale", torch.uint8, (N, *mx4_scale_shape(2 * f, d)))
-        _chk(w2_scale, "w2_scale", torch.uint8, (N, *mx4_scale_shape(d, f)))
-    return d, f, N
+        _chk(base, "base", dtype, (T, d)); _chk(out, "out", dtype, (T, d)); _chk(ws, "ws", torch.uint8)
+        if mx4:
+            _chk(w1_scale, "w1_scale", torch.uint8, (N, *mx4_scale_shape(2 * f, d)))
+            _chk(w2_scale, "w2_scale", torch.uint8, (N, *mx4_scale_shape(d, f)))
+    return T, d, f, N
 
 
 def experts_forward(x, topk_idx, topk_w, W1, W2, w1_scale=None, w2_scale=None, scale: float = 1.0,
                     base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """meteora_experts_forward: out[t] = base[t] + scale * sum_j topk_w[t,j] * MLP_e(x[t]), e = topk_idx[t,j], for up to 64 tokens.
     W1[N,2f,d], W2[N,d,f] in x's dtype; with w1_scale, w2_scale in 4 bits, quantize_mx4 of every matrix: W1[N,2f,d/2], W2[N,d,f/2]."""
-    T, k = topk_idx.shape
     if out is None:
         out = torch.empty_like(x)
-    d, f, N = _chk_experts(x, W1, W2, w1_scale, w2_scale, base, out)
-    _chk(topk_idx, "topk_idx", torch.int32, (x.shape[0], k)); _chk(topk_w, "topk_w", torch.float32, (x.shape[0], k)); _chk(ws, "ws", torch.uint8)
+    T, d, f, N = _chk_experts(x, W1, W2, w1_scale, w2_scale, base, out, ws)
+    routed = topk_idx.shape
+    k = routed[-1] if routed else 0
+    if not (routed == topk_w.shape == (T, k) and topk_idx.dtype == torch.int32 and topk_w.dtype == torch.float32 and topk_idx.is_contiguous() and
+            topk_w.is_contiguous()):
+        _chk(topk_idx, "topk_idx", torch.int32, (T, k)); _chk(topk_w, "topk_w", torch.float32, (T, k))
     ws = _ws(ws, lambda: experts_workspace_bytes(T, d, f, N, k), x.device)
     _chk_device(x, topk_idx, topk_w, W1, W2, w1_scale, w2_scale, base, out, ws)
     st = load_library().meteora_experts_forward(_pe(x), _pe(topk_idx), _pe(topk_w), _p(W1), _p(w1_scale), _p(W2), _p(w2_scale), T, d, f, N, k,
@@ -792,11 +803,10 @@ def moe_forward(x, W_gate, gate_bias, W1, W2, k: int, w1_scale=None, w2_scale=No
                 return_routing: bool = False):
     """meteora_moe_forward: experts_forward behind its gate, W_gate[d,N] f32 and gate_bias[N] f32 or None; with `return_routing`
     (out, topk_idx[T,k], topk_w[T,k])."""
-    T = x.shape[0]
     if out is None:
         out = torch.empty_like(x)
-    d, f, N = _chk_experts(x, W1, W2, w1_scale, w2_scale, base, out)
-    _chk(W_gate, "W_gate", torch.float32, (d, N)); _chk(gate_bias, "gate_bias", torch.float32, (N,)); _chk(ws, "ws", torch.uint8)
+    T, d, f, N = _chk_experts(x, W1, W2, w1_scale, w2_scale, base, out, ws)
+    _chk(W_gate, "W_gate", torch.float32, (d, N)); _chk(gate_bias, "gate_bias", torch.float32, (N,))
     idx = w = None
     if return_routing:
         idx = torch.empty((T, k), dtype=torch.int32, device=x.device)
