@@ -117,6 +117,17 @@ def test_bf16_widths_that_are_no_multiple_of_32(T, N, k, d, f):
     close(m.experts_forward(x, idx, w, *layer.weights), layer.reference(x, idx, w))
 
 
+@pytest.mark.parametrize("T", [1, 4, 64])
+@pytest.mark.parametrize("d,f,mx4", [(8, 8, False), (8, 131072, False), (131072, 8, False), (32, 131072, True), (131072, 32, True)])
+def test_least_and_largest_widths(T, d, f, mx4):
+    g = gen(T + d)
+    layer, x = Layer(3, d, f, mx4, g), randn((T, d), g)
+    Wg = randn((d, 3), g, d ** -0.5, torch.float32)
+    out, idx, w = m.moe_forward(x, Wg, None, *layer.weights, 2, **layer.scales, return_routing=True)
+    close(out, layer.reference(x, idx, w))
+    assert torch.equal(out, m.experts_forward(x, idx, w, *layer.weights, **layer.scales))
+
+
 @pytest.mark.parametrize("mx4", [True, False])
 @pytest.mark.parametrize("T", [1, 4, 13, 64])
 def test_padding_and_ids_outside(T, mx4):
