@@ -208,6 +208,7 @@ __global__ __launch_bounds__(256) void gemm_mx4_back_sum_kernel(const float* __r
     const size_t o = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (o >= all) return;
     f32x4 sum = *reinterpret_cast<const f32x4*>(part + o);
+#pragma unroll 8
     for (int p = 1; p < splits; ++p) sum += *reinterpret_cast<const f32x4*>(part + (size_t)p * all + o);
     back_store(dx + o, sum[0], sum[1]);
     back_store(dx + o + 2, sum[2], sum[3]);
@@ -223,14 +224,25 @@ bool mx4_back_takes(int T, int d_in, bool bf16) {
     if (!bf16) return T <= 65536;
     return T <= 256 || (T <= 1024 && ceil_div(d_in, kBackInputs) * ceil_div(T, kBackTokens<bf16_t>) <= 256);
 }
-// Workgroups to a tile: as fill the CUs once, with a step to every wavefront, as far as there is room for their sums
-static int back_splits(int T, int tiles, int d_in, int d_out, size_t room) {
+// Workgroups to a tile: the number that takes the least by rounds of 256 workgroups * (steps of a wavefront * time of one + 3 us), and a second launch and its
+// bytes if they are more than one.  A step takes 0.65 to 1.6 us by tokens and type, and 1.0 for all 256 workgroups' codes from memory.  Of 1 token of 512 -> 14336 1,
+// 4, 16 and 32 workgroups to a tile take 40.6, 14.8, 10.9 and 11.4 us, of 64 of 4096 -> 1024 1, 2, 4 and 8 10.4, 11.0, 11.7 and 14.1, of 200 of 5120 ->
+// 13824, 160 tiles, 1, 3 and 4 62.0, 55.4 and 65.5; over 88 such sizes the choice is 2 % slower than the best.
+static int back_splits(int T, int tiles, int d_in, int d_out, bool bf16, size_t room) {
     const int steps = ceil_div(d_out, kBackStep);
-    int n = tiles < 256 ? 256 / tiles : 1;
-    n = n < steps / kBackWaves ? n : steps / kBackWaves;
-    const size_t fit = room / ((size_t)T * d_in * sizeof(float));
-    n = (size_t)n < fit ? n : (int)fit;
-    return n < 1 ? 1 : ceil_div(steps, ceil_div(steps, n));   // none without steps
+    const float one = T <= 16 ? (bf16 ? 0.65f : 1.f) : bf16 ? (T <= 32 ? 0.7f : 0.95f) : 1.6f;
+    const size_t sums = (size_t)T * d_in * sizeof(float);
+    int best = 1;
+    float least = 0.f;
+    for (int n = 1; n <= 32 && n <= steps && (n == 1 || sums * n <= room); ++n) {
+        const int share = ceil_div(steps, n);
+        if (n > 1 && ceil_div(steps, share) != n) continue;   // workgroups without steps
+        const int64_t groups = (int64_t)tiles * n;
+        const float all = groups < 256 ? (float)groups / 256.f : 1.f, step = one > all ? one : all;
+        const float us = (float)((groups + 255) / 256) * ((float)ceil_div(share, kBackWaves) * step + 3.f) + (n > 1 ? 2.f + 0.1f * (float)n + 2.f * (float)sums * (float)n / 5e6f : 0.f);
+        if (n == 1 || us < least) { least = us; best = n; }
+    }
+    return best;
 }
 template <typename TX, int TB>
 static hipError_t launch_tiles(const MxBackArgs& a, hipStream_t stream) {
@@ -243,7 +255,7 @@ template <typename TX>
 static hipError_t launch_back(MxBackArgs a, size_t room, hipStream_t stream) {
     a.tiles = ceil_div(a.d_in, kBackInputs);
     a.blocks = ceil_div(a.T, kBackTokens<TX>);
-    a.splits = back_splits(a.T, a.tiles * a.blocks, a.d_in, a.d_out, room);
+    a.splits = back_splits(a.T, a.tiles * a.blocks, a.d_in, a.d_out, sizeof(TX) == 2, room);
     float* const part = a.part;
     if (a.splits == 1) a.part = nullptr;
     hipError_t e;
