@@ -99,7 +99,7 @@ meteora_status meteora_base_gemm_mx4(const void* x, const uint8_t* W, const uint
     if (!ws || !aligned(ws, 256) || ws_bytes < base_gemm_bytes(T, d_in)) return METEORA_ERR_WORKSPACE;
     if (T == 0) return METEORA_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (base_gemm_mx4_in_one(T, d_in))
+    if (base_gemm_mx4_in_one(T, d_in, d_out))
         return status(launch_base_gemm_mx4_in_one(x, W, w_scale, T, d_in, d_out, dt == METEORA_BF16, out, st));
     uint8_t* q = static_cast<uint8_t*>(ws);
     uint8_t* scale = q + align_up((size_t)T * (d_in / 2), 256);

@@ -11,7 +11,7 @@
 // gemm_mx4_ring_kernel   many rows: tiles of 64 x 64 to 256 x 256, rings of LDS slots, scales in registers
 // gemm_mx4_wave_kernel   few rows: a ring to every wavefront, scales in its slots
 // gemm_mx4_one_kernel    up to 256 inputs: no ring
-// gemm_mx4_row_kernel    up to 4 tokens of meteora_base_gemm_mx4: their quantisation too
+// gemm_mx4_row_kernel    up to 16 tokens of meteora_base_gemm_mx4: their quantisation too
 #include "common.hpp"
 #include "gemm_mfma.hpp"
 #include "gemm_rows.hpp"
@@ -181,21 +181,20 @@ __global__ __launch_bounds__(WV * 64) void gemm_mx4_wave_kernel(const GemmMx4Arg
 
 // ------------------------------------------------------------------------------------------
 // A few tokens and their quantisation in one launch (meteora_base_gemm_mx4): every workgroup quantises all of x itself, into LDS, while its
-// first tiles of W are on their way, which costs less than a launch in front: 1, 2 and 4 tokens of 4096 -> 4096 4.7, 5.3 and 5.6 us, with a launch
-// of quantize_mx4_kernel in front 6.9, 6.8 and 6.9; of 4096 -> 14336, where workgroups follow one another on a CU, 9.1, 9.6 and 12.3, and 11.1, 10.8 and 11.1.  W goes through the wavefronts' rings as above; a lane
-// without a row of its own multiplies another's, and its result is not kept.
+// first tiles of W are on their way, which costs less than a launch in front (graphs of calls, weights in turn): 1, 2, 4 and 8 tokens of 4096 -> 4096 4.7,
+// 5.3, 5.5 and 7.7 us, with quantize_mx4_kernel in front 6.9, 6.8, 6.9 and 7.0 and a launch more for the host; 16 of 1024 -> 4096 4.8 and 6.1; 4 and 6 of
+// 5120 -> 5120 8.5 and 8.9, and 8.5 and 8.6; 3 and 4 of 4096 -> 14336, where workgroups follow one another on a CU, 10.0 and 12.2, and 11.2 and 11.0.
+// W goes through the wavefronts' rings as above; a lane without a row of its own multiplies another's, and its result is not kept.
 // ------------------------------------------------------------------------------------------
-constexpr int kRowThreads = 256, kRowMaxTokens = 4, kRowMaxInputs = 16384;   // of all tokens
+constexpr int kRowThreads = 256, kRowMaxTokens = 16, kRowHeld = 18, kRowMaxInputs = kRowHeld * kRowThreads * 8;   // of all tokens, in whole chunks
 constexpr int row_mx4_stride(int d) { return (d / 2 + 127) / 128 * 128 + 16; }   // bytes; rows start 4 banks apart
 constexpr int row_mx4_bytes(int T, int d) { return T * (row_mx4_stride(d) + mx4_chunks(d) * 16); }
 template <int RB, int D>
 constexpr int row_mx4_ring_bytes() { return 4 * D * RB * 2304; }   // and the sums in its place
 template <int RB, int D>
-constexpr int row_mx4_lds_most() { return row_mx4_ring_bytes<RB, D>() + kRowMaxInputs / 2 + kRowMaxTokens * (127 + 16) + kRowMaxInputs / 32 + kRowMaxTokens * 16; }
+constexpr int row_mx4_lds_most() { return row_mx4_ring_bytes<RB, D>() + kRowMaxInputs / 2 + kRowMaxTokens * (127 + 16) + kRowMaxInputs / 32; }
 
-// HELD: pieces of 8 inputs to a thread.  kRowHeld: of tokens whose last chunks are padded
-constexpr int kRowHeld = 9;
-static_assert(kRowMaxInputs + kRowMaxTokens * (kMxChunk - 32) <= kRowHeld * kRowThreads * 8, "pieces");
+// HELD: pieces of 8 inputs to a thread
 template <typename TX, int RB, int D, int HELD>
 __global__ __launch_bounds__(kRowThreads) void gemm_mx4_row_kernel(const GemmMx4Args a, const TX* __restrict__ x) {
     constexpr int WV = 4, NL = 3 * RB;
@@ -820,9 +819,12 @@ static hipError_t launch_row(GemmMx4Args a, const TX* x, hipStream_t stream) {
         kern<<<a.tiles_n, kRowThreads, lds, stream>>>(a, x);
         return hipGetLastError();
     };
-    return a.T * mx4_chunks(a.d_in * 2) * kMxChunk <= 4096 ? go(&gemm_mx4_row_kernel<TX, RB, D, 2>) : go(&gemm_mx4_row_kernel<TX, RB, D, kRowHeld>);
+    const int held = ceil_div(a.T * mx4_chunks(a.d_in * 2) * kMxChunk, kRowThreads * 8);
+    return held <= 2 ? go(&gemm_mx4_row_kernel<TX, RB, D, 2>) : held <= 9 ? go(&gemm_mx4_row_kernel<TX, RB, D, 9>) : go(&gemm_mx4_row_kernel<TX, RB, D, kRowHeld>);
 }
-bool base_gemm_mx4_in_one(int T, int d_in) { return T <= kRowMaxTokens && T * d_in <= kRowMaxInputs; }
+bool base_gemm_mx4_in_one(int T, int d_in, int d_out) {
+    return T <= kRowMaxTokens && T * mx4_chunks(d_in) * kMxChunk <= (d_out <= 4096 ? kRowMaxInputs : d_out <= 8192 ? 20480 : 12288);
+}
 
 template <typename TX>
 static hipError_t launch_base(const GemmMx4Args& a, const TX* x, hipStream_t stream) {
@@ -871,8 +873,11 @@ static hipError_t init_tail() {
 }
 template <typename TX, int RB, int D>
 static hipError_t init_row() {
-    const hipError_t e = ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_row_kernel<TX, RB, D, 2>), row_mx4_lds_most<RB, D>());
-    return e != hipSuccess ? e : ensure_lds_limit(reinterpret_cast<const void*>(&gemm_mx4_row_kernel<TX, RB, D, kRowHeld>), row_mx4_lds_most<RB, D>());
+    hipError_t e = hipSuccess;
+    for (const void* k : {reinterpret_cast<const void*>(&gemm_mx4_row_kernel<TX, RB, D, 2>), reinterpret_cast<const void*>(&gemm_mx4_row_kernel<TX, RB, D, 9>),
+                          reinterpret_cast<const void*>(&gemm_mx4_row_kernel<TX, RB, D, kRowHeld>)})
+        if (e == hipSuccess) e = ensure_lds_limit(k, row_mx4_lds_most<RB, D>());
+    return e;
 }
 template <typename TO>
 static hipError_t init_mx4() {   // every kernel that launch_mx4 and launch_base may start

@@ -251,7 +251,7 @@ hipError_t launch_dequantize_mx4(const uint8_t* q, const uint8_t* scale, int row
                                  hipStream_t stream);
 hipError_t launch_gemm_mx4(const uint8_t* q, const uint8_t* q_scale, const uint8_t* W, const uint8_t* w_scale, const int32_t* offsets,
                            int T, int d_in, int d_out, int N, bool bf16, void* out, hipStream_t stream);
-bool base_gemm_mx4_in_one(int T, int d_in);   // the quantisation and the product of a few tokens in one launch
+bool base_gemm_mx4_in_one(int T, int d_in, int d_out);   // the quantisation and the product of a few tokens in one launch
 hipError_t launch_base_gemm_mx4_in_one(const void* x, const uint8_t* W, const uint8_t* w_scale, int T, int d_in, int d_out, bool bf16, void* out,
                                        hipStream_t stream);
 // The gradient with respect to rows from the codes, for a few of them in bf16; ws: `room` bytes for sums of parts

@@ -190,6 +190,22 @@ def test_base_gemm_mx4_and_its_gradient(T, d_in, d_out, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,d_in,d_out", [(16, 32, 8), (16, 2304, 4096), (16, 2336, 4096), (15, 2080, 1376), (16, 992, 5120), (9, 4096, 104), (5, 7168, 72), (5, 7200, 72),
+                                          (1, 36864, 40), (1, 36896, 40), (5, 4096, 8192), (6, 4096, 4104), (3, 4096, 8200), (4, 4096, 8200), (16, 256, 12296),
+                                          (2, 16416, 24), (13, 1056, 2056)])
+def test_rows_quantised_in_the_product(T, d_in, d_out, dtype):
+    """Up to 16 tokens of 36864 inputs in whole chunks (fewer for many outputs), and a little more: as quantised before it."""
+    g = gen(T + d_in + d_out)
+    x = torch.randn((T, d_in), generator=g, device="cuda").to(dtype)
+    W, ws, V = operand(d_out, d_in, g)
+    out = torch.full((T + 1, d_out), 7.0, device="cuda", dtype=dtype)
+    m.base_gemm_mx4(x, W, ws, out=out[:T])
+    v = mx.values(*mx.quantize(x))
+    close(out[:T], mx.product(v, V), mx.product(v.abs(), V.abs()), d_in / 32)
+    assert (out[T] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T,d_in,d_out", [(1, 32, 8), (1, 128, 264), (15, 160, 4096), (16, 4096, 512), (17, 608, 8200), (32, 416, 4104), (33, 2080, 1376),
                                           (48, 1056, 1000), (64, 5120, 13824), (65, 96, 1160), (129, 4096, 72), (200, 544, 2056), (256, 14336, 1024),
                                           (257, 4096, 4096), (513, 4128, 520), (1000, 1376, 2080), (1024, 2048, 8192), (1025, 256, 9000), (320, 8224, 64),
