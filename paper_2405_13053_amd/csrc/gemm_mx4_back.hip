@@ -215,10 +215,10 @@ __global__ __launch_bounds__(256) void gemm_mx4_back_sum_kernel(const float* __r
 }
 
 // Or dequantize_mx4_turned_kernel and a product of bf16 matrices, which reads W's 16 bits a value again, in tiles of more tokens.  From the codes and so, us:
-// 4096 -> 4096, 1, 32, 64, 256 and 512 tokens 10.1, 12.4, 16.7, 19.9, 24.9 and 30.6, 29.9, 31.1, 29.2, 33.1; 5120 -> 13824 17.9, 20.2, 25.1, 66.7, 125
+// 4096 -> 4096, 1, 32, 64, 256 and 512 tokens 10.1, 12.4, 16.7, 19.9, 24.9 and 30.6, 29.9, 31.1, 29.2, 33.1; 5120 -> 13824 18.2, 22.2, 25.2, 60.6, 125
 // and 62.9, 63.5, 65.6, 79.4, 110; 14336 -> 4096, 256 and 512, 448 and 896 workgroups, 48.9 and 93.0, and 59.5 and 75.6; 4096 -> 14336, 512, 256
 // workgroups, 73.5 and 92.6; 2048 -> 8192, 1024 and 1536 42.2 and 79.4, and 47.5 and 57.8.  fp32, with products of fp32 matrices: 4096 -> 4096, 1, 64, 512
-// and 2048 12.5, 19.5, 71.7 and 305, and 43.6, 79.2, 285 and 703; 5120 -> 13824 20.4, 44.0, 295 and 1021, and 213, 321, 1325 and 3824; beyond
+// and 2048 12.3, 19.4, 71.2 and 272, and 43.6, 79.2, 285 and 703; 5120 -> 13824 19.8, 42.4, 268 and 1045, and 213, 321, 1325 and 3824; beyond
 // 65536 tokens a grid might have too many workgroups.
 bool mx4_back_takes(int T, int d_in, bool bf16) {
     if (!bf16) return T <= 65536;
