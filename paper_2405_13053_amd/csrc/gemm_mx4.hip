@@ -306,8 +306,10 @@ constexpr int ring_mx4_lds() {
 }
 
 // The tile leaves by way of LDS, 32 (16) rows a wavefront at a time, so that stores are 16-byte pieces of whole rows.  Through the L2,
-// see kWriteThrough.
-template <typename TO, int MB, int NB>
+// see kWriteThrough.  KEPT: where rows are no whole lines they stay in the L2 until the neighbouring tile's part is there; written through, a line
+// goes to memory in two parts.  That is worth it where the output is most of what there is to move (5195 x 96 -> 13200 31.6 and 69.7 us, 8192 x 64
+// -> 4104 18.0 and 23.2), not behind larger tiles (4096 x 1024 -> 4104 22.2 and 20.7, 8192 x 4096 -> 4104 83.0 and 79.6).
+template <typename TO, int MB, int NB, bool KEPT>
 __device__ __forceinline__ void ring_mx4_epilogue(const GemmMx4Args& a, f32x4 (&acc)[MB][NB], unsigned char* smem, int e, int row0,
                                                  int rows, int n0, int wm, int wn, int wave, int lane) {
     constexpr int EB = sizeof(TO), RS = MB % 2 == 0 ? 32 : 16;
@@ -317,6 +319,7 @@ __device__ __forceinline__ void ring_mx4_epilogue(const GemmMx4Args& a, f32x4 (&
     __syncthreads();   // every wavefront is done with the operand tiles
     unsigned char* ep = smem + wave * RS * EST;
     const uint32_t row_bytes = (uint32_t)a.d_out * EB;
+    const bool whole = row_bytes % 128 == 0;   // all of a line is this tile's
     const __amdgpu_buffer_rsrc_t out = __builtin_amdgcn_make_buffer_rsrc((TO*)a.out + (size_t)row0 * a.d_out, 0,
                                                                          (uint32_t)rows * row_bytes, 0x00020000);
     auto sync = [] {   // orders this wavefront's own LDS accesses
@@ -341,7 +344,8 @@ __device__ __forceinline__ void ring_mx4_epilogue(const GemmMx4Args& a, f32x4 (&
             const u32x4 v = *reinterpret_cast<const u32x4*>(ep + r * EST + c * 16);
             // rows past the tile's last are past the resource's end, and so are the pieces sent there for their column
             const uint32_t at = col < a.d_out ? (uint32_t)(wm + mb * 16 + r) * row_bytes + (uint32_t)col * EB : 0xffffffffu;
-            __builtin_amdgcn_raw_buffer_store_b128(v, out, at, 0, kWriteThrough);
+            if (!KEPT || whole) __builtin_amdgcn_raw_buffer_store_b128(v, out, at, 0, kWriteThrough);
+            else __builtin_amdgcn_raw_buffer_store_b128(v, out, at, 0, 0);
         }
         sync();
         __builtin_amdgcn_sched_barrier(0);   // accumulators leave their registers 32 rows at a time
@@ -589,7 +593,7 @@ __device__ __forceinline__ void ring_mx4_tile(const GemmMx4Args& a, unsigned cha
 #pragma unroll
         for (int ni = 0; ni < NB; ++ni) asm volatile("" : "+a"(acc[mi][ni]));   // values from here on, not before
     __builtin_amdgcn_sched_barrier(0);
-    ring_mx4_epilogue<TO, MB, NB>(a, acc, smem, e, row0, rows, n0, wm, wn, wave, lane);
+    ring_mx4_epilogue<TO, MB, NB, false>(a, acc, smem, e, row0, rows, n0, wm, wn, wave, lane);
 }
 
 // Two copies of the loop for the two policies of W's loads, see gemm_mx4_ring_kernel.
@@ -706,7 +710,7 @@ __global__ __launch_bounds__(256) void gemm_mx4_one_kernel(const GemmMx4Args a) 
                 acc[mi][ni] = ks == 0 ? mfma_mx4<0>(__builtin_bit_cast(u32x4, f.w[ni]), __builtin_bit_cast(u32x4, f.x[mi]), acc[mi][ni], sw[ni], sx[mi])
                                       : mfma_mx4<1>(__builtin_bit_cast(u32x4, f.w[ni]), __builtin_bit_cast(u32x4, f.x[mi]), acc[mi][ni], sw[ni], sx[mi]);
     }
-    ring_mx4_epilogue<TO, MB, NB>(a, acc, smem, e, row0, rows, n0, wm, wn, wave, lane);
+    ring_mx4_epilogue<TO, MB, NB, true>(a, acc, smem, e, row0, rows, n0, wm, wn, wave, lane);
 }
 
 template <typename TO, int TB, int RB, int WV, int D>
