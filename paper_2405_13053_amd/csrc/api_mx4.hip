@@ -35,7 +35,7 @@ size_t base_gemm_bytes(int T, int d_in) {   // the quantised rows, then their sc
 // themselves the parts are in the values' place.
 size_t values_bytes(int d_in, int d_out, meteora_dtype dt) { return align_up((size_t)d_in * d_out * (dt == METEORA_BF16 ? 2 : 4), 256); }
 size_t splits_bytes(int T, int d_in, int d_out, meteora_dtype dt) {
-    return dt == METEORA_BF16 && !mx4_back_takes(T, d_in, true) ? (size_t)gemm_few_tile_splits(T, d_out, d_in) * T * d_in * sizeof(float) : 0;
+    return dt == METEORA_BF16 && !mx4_back_takes(T, d_in, d_out, true) ? (size_t)gemm_few_tile_splits(T, d_out, d_in) * T * d_in * sizeof(float) : 0;
 }
 
 }  // namespace
@@ -123,7 +123,7 @@ meteora_status meteora_base_gemm_mx4_backward(const void* dy, const uint8_t* W, 
     if (T == 0) return METEORA_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool bf16 = dt == METEORA_BF16;
-    if (mx4_back_takes(T, d_in, bf16))
+    if (mx4_back_takes(T, d_in, d_out, bf16))
         return status(launch_mx4_back(dy, W, w_scale, T, d_in, d_out, bf16, dx, ws, values_bytes(d_in, d_out, dt), st));
     hipError_t e = launch_dequantize_mx4(W, w_scale, d_out, d_in, true, bf16, ws, st);
     if (e != hipSuccess) return METEORA_ERR_HIP;

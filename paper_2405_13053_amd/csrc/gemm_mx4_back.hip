@@ -1,4 +1,5 @@
-// Gradient of a projection with its weight in 4 bits (quant_mx4.hpp) with respect to its input, of a few tokens in bf16, from the codes themselves:
+// Gradient of a projection with its weight in 4 bits (quant_mx4.hpp) with respect to its input from the codes themselves, for some hundred tokens in bf16 and for
+// most batches in fp32 (see mx4_back_takes):
 //
 //     dx[t,i] = sum_o dy[t,o] * 2^(E[o, i / 32] - 127) * W[o,i]
 //
@@ -218,11 +219,14 @@ __global__ __launch_bounds__(256) void gemm_mx4_back_sum_kernel(const float* __r
 // 4096 -> 4096, 1, 32, 64, 256 and 512 tokens 10.1, 12.4, 16.7, 19.9, 24.9 and 30.6, 29.9, 31.1, 29.2, 33.1; 5120 -> 13824 18.2, 22.2, 25.2, 60.6, 125
 // and 62.9, 63.5, 65.6, 79.4, 110; 14336 -> 4096, 256 and 512, 448 and 896 workgroups, 48.9 and 93.0, and 59.5 and 75.6; 4096 -> 14336, 512, 256
 // workgroups, 73.5 and 92.6; 2048 -> 8192, 1024 and 1536 42.2 and 79.4, and 47.5 and 57.8.  fp32, with products of fp32 matrices: 4096 -> 4096, 1, 64, 512
-// and 2048 12.3, 19.4, 71.2 and 272, and 43.6, 79.2, 285 and 703; 5120 -> 13824 19.8, 42.4, 268 and 1045, and 213, 321, 1325 and 3824; beyond
-// 65536 tokens a grid might have too many workgroups.
-bool mx4_back_takes(int T, int d_in, bool bf16) {
-    if (!bf16) return T <= 65536;
-    return T <= 256 || (T <= 1024 && ceil_div(d_in, kBackInputs) * ceil_div(T, kBackTokens<bf16_t>) <= 256);
+// and 2048 12.3, 19.4, 71.2 and 272, and 43.6, 79.2, 285 and 703; 5120 -> 13824 19.8, 42.4, 268 and 1045, and 213, 321, 1325 and 3824; 131072 x 4096 ->
+// 256 2611 and 3023.  Of few outputs a workgroup has little more than its start and end: 65536 x 4096 -> 8, 64, 128 and 160 989, 996, 1007 and 1176, and 237,
+// 510, 843 and 1032, 8192 x 512 -> 8, 96, 128 and 160 21.8, 21.6, 21.7 and 24.4, and 12.8, 21.4, 25.2 and 28.6; that takes more than two rounds of
+// workgroups to matter: 2048 x 512 -> 8 7.9 and 9.9, 512 x 4096 -> 8 and 64 12.5 and 12.7, and 12.1 and 16.2.
+bool mx4_back_takes(int T, int d_in, int d_out, bool bf16) {
+    const int tiles = ceil_div(d_in, kBackInputs);
+    if (!bf16) return d_out > kMxBackFewOutputs || (int64_t)tiles * ceil_div(T, kBackTokens<float>) <= 512;
+    return T <= 256 || (T <= 1024 && tiles * ceil_div(T, kBackTokens<bf16_t>) <= 256);
 }
 // Workgroups to a tile: the number that takes the least by rounds of 256 workgroups * (steps of a wavefront * time of one + 3 us), and a second launch and its
 // bytes if they are more than one.  A step takes 0.65 to 1.6 us by tokens and type, and 1.0 for all 256 workgroups' codes from memory.  Of 1 token of 512 -> 14336 1,
@@ -266,10 +270,24 @@ static hipError_t launch_back(MxBackArgs a, size_t room, hipStream_t stream) {
     gemm_mx4_back_sum_kernel<<<(int)((all + 1023) / 1024), 256, 0, stream>>>(part, a.splits, all, static_cast<TX*>(a.dx));
     return hipGetLastError();
 }
+// Batches of up to kBackGroups workgroups, far below the 2^32 threads of a grid; each is 1024 rounds of workgroups, so that their ends cost nothing
+constexpr int kBackGroups = 1 << 18;
+template <typename TX>
+static hipError_t launch_batches(MxBackArgs a, size_t room, hipStream_t stream) {
+    const int all = a.T, most = kBackGroups / ceil_div(a.d_in, kBackInputs) * kBackTokens<TX>;   // d_in <= 131072: 1024 tiles at most
+    for (int t0 = 0; t0 < all; t0 += most) {
+        a.T = all - t0 < most ? all - t0 : most;
+        const hipError_t e = launch_back<TX>(a, room, stream);
+        if (e != hipSuccess) return e;
+        a.dy = static_cast<const TX*>(a.dy) + (size_t)a.T * a.d_out;
+        a.dx = static_cast<TX*>(a.dx) + (size_t)a.T * a.d_in;
+    }
+    return hipSuccess;
+}
 hipError_t launch_mx4_back(const void* dy, const uint8_t* W, const uint8_t* scale, int T, int d_in, int d_out, bool bf16, void* dx, void* ws, size_t room,
                            hipStream_t stream) {
     const MxBackArgs a{dy, W, scale, dx, (float*)ws, T, d_in, d_out, 0, 0, 0};
-    return bf16 ? launch_back<bf16_t>(a, room, stream) : launch_back<float>(a, room, stream);
+    return bf16 ? launch_batches<bf16_t>(a, room, stream) : launch_batches<float>(a, room, stream);
 }
 hipError_t mx4_back_init_kernels() {
     hipError_t e = hipSuccess;

@@ -254,8 +254,10 @@ hipError_t launch_gemm_mx4(const uint8_t* q, const uint8_t* q_scale, const uint8
 bool base_gemm_mx4_in_one(int T, int d_in, int d_out);   // the quantisation and the product of a few tokens in one launch
 hipError_t launch_base_gemm_mx4_in_one(const void* x, const uint8_t* W, const uint8_t* w_scale, int T, int d_in, int d_out, bool bf16, void* out,
                                        hipStream_t stream);
-// The gradient with respect to rows from the codes, for a few of them in bf16; ws: `room` bytes for sums of parts
-bool mx4_back_takes(int T, int d_in, bool bf16);
+// The gradient with respect to rows from the codes, where mx4_back_takes says so: in fp32 always with more than kMxBackFewOutputs outputs.  ws: `room` bytes
+// for sums of parts
+constexpr int kMxBackFewOutputs = 192;
+bool mx4_back_takes(int T, int d_in, int d_out, bool bf16);
 hipError_t launch_mx4_back(const void* dy, const uint8_t* W, const uint8_t* scale, int T, int d_in, int d_out, bool bf16, void* dx, void* ws, size_t room,
                            hipStream_t stream);
 I8Plan gemm_mx4_plan(int T, int d_in, int d_out, int N, bool grouped);
