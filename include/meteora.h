@@ -443,7 +443,8 @@ int meteora_gemm_mx4_kernel(int T, int d_in, int d_out, int N, int grouped, cons
  * meteora_base_gemm_mx4_backward: its gradient with respect to x, the rounding of x passed by (the weight is frozen and has none):
  *   dx[t,i] = sum_c dy[t,c] * V(W[c,i])
  * dy and dx in dt, dy as it is (not quantised), fp32 sums, one rounding.  ws holds sums of parts, or beyond some sizes the weight's values,
- * transposed, of every call anew: meteora_base_gemm_mx4_backward_workspace_bytes(d_in, d_out, dt), whatever T.
+ * transposed, of every call anew: meteora_base_gemm_mx4_backward_workspace_bytes(d_in, d_out, dt), whatever T (bf16: two bytes a value and more;
+ * fp32: four, 32 MB at most for more than 192 outputs).
  */
 size_t meteora_base_gemm_mx4_workspace_bytes(int T, int d_in);
 

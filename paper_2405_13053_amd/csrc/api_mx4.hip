@@ -32,8 +32,13 @@ size_t base_gemm_bytes(int T, int d_in) {   // the quantised rows, then their sc
     return align_up((size_t)T * (d_in / 2), 256) + align_up(mx4_scale_bytes(T, d_in), 256);
 }
 // The gradient's: the transposed values, then (bf16) the parts of a split contraction, which numbers the outputs d_in.  Where it reads the codes
-// themselves the parts are in the values' place.
-size_t values_bytes(int d_in, int d_out, meteora_dtype dt) { return align_up((size_t)d_in * d_out * (dt == METEORA_BF16 ? 2 : 4), 256); }
+// themselves the parts are in the values' place; fp32 with more than few outputs reads nothing else, and has room for parts as large as up to 16384 outputs ask for
+// (25.6 MB, at 100000 tokens of 32 inputs; a batch whose parts do not fit gets fewer of them).
+constexpr size_t kBackParts = (size_t)32 << 20;
+size_t values_bytes(int d_in, int d_out, meteora_dtype dt) {
+    const size_t all = align_up((size_t)d_in * d_out * (dt == METEORA_BF16 ? 2 : 4), 256);
+    return dt == METEORA_F32 && d_out > kMxBackFewOutputs && all > kBackParts ? kBackParts : all;
+}
 size_t splits_bytes(int T, int d_in, int d_out, meteora_dtype dt) {
     return dt == METEORA_BF16 && !mx4_back_takes(T, d_in, d_out, true) ? (size_t)gemm_few_tile_splits(T, d_out, d_in) * T * d_in * sizeof(float) : 0;
 }
