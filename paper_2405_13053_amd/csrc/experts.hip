@@ -662,9 +662,10 @@ static_assert(kManyThreads >= kExpertsMaxTokens * kMaxTopK, "a pair to a thread"
 // us.  A K tile of w wavefronts took, 4 bits and blocks of 16 tokens (20 tokens of 16 experts, 4096 and 2048 wide), 0.54, 0.57, 0.62, 0.69, 0.85, 0.91,
 // 0.94, 1.24 us for w = 1 to 8, and with blocks of 32 (64 tokens of 8 experts, 4096 and 14336) 0.70, 0.74, 0.83, 0.97, 1.25, 1.32, 1.45, 1.6.
 // Calls of 33 tokens of 28 experts, 2080 and 1376 wide, with w = 4, 5 and 8 for the first product 51.6, 49.4, 55.5; of 64 of 8, 4096 and 14336, w = 4, 7, 8
-// 166, 150, 159, and the second product with w = 8 whole and in two and four parts 180, 152, 154.
+// 166, 150, 159, and the second product with w = 8 whole and in two and four parts 180, 152, 154.  In bf16 K tiles are shorter by about the same share for all w,
+// so that one model does for both kinds of weights and blocks: over 16 calls of 6 to 64 tokens of 4 to 64 experts the best of all w and parts takes 0 to 4 %
+// less than the choice in 4 bits and 0 to 6 % in bf16 (13 tokens of 8 experts, 4096 and 3584: 125 us, and 119 with w = 2).
 struct Tiling { int waves, splits; };
-template <typename WT>
 __device__ __forceinline__ Tiling choose_tiling(int blocks, int units, int nk, bool may_split, int lane) {   // a wavefront; units: of channels
     const int w = (lane & 7) + 1, splits = 1 << (lane >> 3 & 3);
     const int items = blocks * ((units + w - 1) / w) * splits;
@@ -727,8 +728,8 @@ __device__ __forceinline__ void make_plan(const ExpertsArgs& a, Plan& plan, Expe
         first[lane] = at;
         for (int i = 0; i < mine; ++i) plan.block[end - mine + i] = (uint32_t)lane | (uint32_t)min(R, n - i * R) << 8 | (uint32_t)(at + i * R) << 16;
         const int blocks = __builtin_amdgcn_readlane(end, 63);
-        const Tiling up = choose_tiling<WT>(blocks, ceil_div(a.f, 16), ceil_div(WT::row_bytes(a.d), 128), false, lane);
-        const Tiling down = choose_tiling<WT>(blocks, ceil_div(a.d, 32), ceil_div(WT::row_bytes(a.f), 128), true, lane);
+        const Tiling up = choose_tiling(blocks, ceil_div(a.f, 16), ceil_div(WT::row_bytes(a.d), 128), false, lane);
+        const Tiling down = choose_tiling(blocks, ceil_div(a.d, 32), ceil_div(WT::row_bytes(a.f), 128), true, lane);
         if (lane == 0) {
             plan.blocks = blocks;
             plan.up_waves = up.waves;
@@ -1062,7 +1063,10 @@ static hipError_t launch(ExpertsArgs a, hipStream_t stream) {
         a.W_gate = nullptr;   // done
     }
     if (few) return launch_few<WT>(a, stream);
-    // blocks of 16 or of 32 tokens: 64 tokens of 2 of 8 experts of 4096 and 3584 62.0 and 49.9 us, 32 tokens 43.6 and 48.6
+    // Blocks of 16 or of 32 tokens, us.  4 bits: 64 tokens of 2 of 8 experts of 4096 and 3584 62.0 and 49.9, 32 tokens 43.6 and 48.6; 64 of 2 of 8 of 4096 and 14336
+    // 182 and 151; 48 of 2 of 4 of 4096 42.7 and 40.3; 33 of 4 of 28 of 2080 and 1376 45.0 and 50.7; 64 of 2 of 64 of 1024 29.4 and 32.5.  bf16: 64 of 2 of 8 of 4096
+    // and 3584 152 and 128, 32 tokens 127 and 128; 48 of 2 of 4 of 4096 and 2048 55.8 and 50.2; 20 of 2 of 16 of 4096 and 1024 79.2 and 78.3; of 4 of 28 of 2048 and
+    // 1024, 64 tokens, where the rule takes 16, 76.9 and 72.7.
     return a.T * a.k <= 10 * a.N || a.T <= 16 ? launch_many<WT, 1>(a, stream) : launch_many<WT, 2>(a, stream);
 }
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t stream) {

@@ -8,7 +8,7 @@
 // products (see gemm_i8.hip) with the scales as a third operand.  Lane kq * 16 + l15 holds row l15 and block kq of an instruction's four;
 // the word of scales that it needs for 512 inputs is bytes kq * 4 .. + 3 of the row's 16, and 16 rows' words are 256 bytes on end.
 //
-// gemm_mx4_ring_kernel   many rows: tiles of 64 x 64 to 256 x 256, rings of LDS slots, scales in registers
+// gemm_mx4_ring_kernel   many rows: tiles of 64 x 64 to 256 x 256, rings of LDS slots, scales in registers with two slots, in the slots of deeper rings
 // gemm_mx4_wave_kernel   few rows: a ring to every wavefront, scales in its slots
 // gemm_mx4_one_kernel    up to 256 inputs: no ring
 // gemm_mx4_row_kernel    up to 16 tokens of meteora_base_gemm_mx4: their quantisation too
@@ -307,8 +307,9 @@ constexpr int ring_mx4_lds() {
 
 // The tile leaves by way of LDS, 32 (16) rows a wavefront at a time, so that stores are 16-byte pieces of whole rows.  Through the L2,
 // see kWriteThrough.  KEPT: where rows are no whole lines they stay in the L2 until the neighbouring tile's part is there; written through, a line
-// goes to memory in two parts.  That is worth it where the output is most of what there is to move (5195 x 96 -> 13200 31.6 and 69.7 us, 8192 x 64
-// -> 4104 18.0 and 23.2), not behind larger tiles (4096 x 1024 -> 4104 22.2 and 20.7, 8192 x 4096 -> 4104 83.0 and 79.6).
+// goes to memory in two parts.  That is worth it in gemm_mx4_one_kernel (5195 x 96 -> 13200 31.6 and 69.7 us, 8192 x 64 -> 4104 18.0 and 23.2), whose
+// four or five workgroups to a CU all store at once, not behind rings, however short: kept and written through, 4096 x 288, 512 and 1024 -> 4104 19.0, 19.1 and
+// 22.3, and 17.1, 17.1 and 20.8; 8192 x 288 and 768 -> 13200 72 and 84, and 69 and 81; 1000 x 288 -> 13200 14.1 and 12.2; fp32, 4096 x 288 -> 4104 22.5 and 21.0.
 template <typename TO, int MB, int NB, bool KEPT>
 __device__ __forceinline__ void ring_mx4_epilogue(const GemmMx4Args& a, f32x4 (&acc)[MB][NB], unsigned char* smem, int e, int row0,
                                                  int rows, int n0, int wm, int wn, int wave, int lane) {

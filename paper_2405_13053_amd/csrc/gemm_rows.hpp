@@ -22,7 +22,7 @@ struct GemmRowsArgs {
     int T, d_in, d_out, N;  // d_in: bytes of a row
     int tiles_m, tiles_n;   // row tiles of the grid (at least as many as there are), column tiles
     int tile_cols;          // columns of a tile (wave kernel)
-    int tail;               // 1: the tiles of a last, half-empty round are left to gemm_i8_tail_kernel
+    int tail;               // 1: the tiles of a last, half-empty round are left to the product's tail kernel (gemm_i8_, gemm_mx4_tail_kernel)
     int past_caches;        // 1: W is more than the caches keep from one call to the next
 };
 
