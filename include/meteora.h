@@ -425,6 +425,9 @@ meteora_status meteora_dequantize_mx4(const uint8_t* q /*[rows,d/2]*/, const uin
  * Products of two values are exact, sums fp32 in an order that depends on the sizes, one rounding where dt (the type of out) is
  * METEORA_BF16.  offsets, N, groups and rows of no group as in meteora_gemm_i8.  w_scale: the N matrices' scales one behind the other, each
  * meteora_mx4_scale_bytes(d_out, d_in); q_scale: meteora_mx4_scale_bytes(T, d_in).
+ * Weights are frozen: there is no gradient for W.  The gradient with respect to the rows that were quantised (the rounding passed by) is
+ * dx[t,i] = sum_c dy[t,c] * V(W[e,c,i]): of one matrix meteora_base_gemm_mx4_backward, of groups that entry point once for every group with rows, on
+ * the group's rows of dy and its matrix, which takes the offsets on the host; no call computes it for all groups at once.
  * Limits: those of the rows for both operands, d_out % 8 == 0, d_out <= 2^20, N <= 64, T * d_out < 2^33.
  *
  * meteora_gemm_mx4_kernel: the kernel that these sizes lead to, as meteora_gemm_i8_kernel ("one" for up to 256 inputs).
@@ -514,8 +517,9 @@ meteora_status meteora_unsort_backward(const void* dy /*[T,d]*/, const void* ys 
  * Limits: T <= 64, N <= 64, k <= 8, d % 8 == 0, f % 8 == 0 (in 4 bits % 32), d, f <= 131072.
  * ws: meteora_experts_workspace_bytes(T, d, f, N, k) bytes, which also holds any smaller T; 0 outside the limits.
  *
- * meteora_moe_forward: the same behind its gate, as meteora_gate_topk routes (k <= N; the logits' sums in an order of their own, so that
- * two that are equal to fp32 accuracy may rank the other way there).  topk_idx_out / topk_w_out receive the routing if they are not NULL.
+ * meteora_moe_forward: the same behind its gate, as meteora_gate_topk routes (k <= N).  The logits' sums are in an order of their own, for one token in
+ * another than for more, so that two that are equal to fp32 accuracy may rank the other way there, or in a batch of another size; logits that are equal
+ * throughout (columns of W_gate and biases that are equal) go to the lowest index always.  topk_idx_out / topk_w_out receive the routing if they are not NULL.
  * These two have no gradients.
  */
 size_t meteora_experts_workspace_bytes(int T, int d, int f, int N, int k);

@@ -5,7 +5,10 @@
 //
 // Weights are bf16, or 4-bit values with block scales (quant_mx4.hpp) that become bf16 in registers, exactly, so that both run on
 // v_mfma_f32_16x16x32_bf16 with x as it is: W is the first operand, the tokens are the 16 columns of the second.  h is rounded to bf16 once, as
-// the operand of the second product; sums are fp32.
+// the operand of the second product; sums are fp32.  That rounding takes the output's error from 0.0017 of the output, which is its own rounding, to 0.0023.  h as two
+// bf16 parts would do without it and double the columns of the second product: 32 tokens' K tiles of 4 bits would no longer leave room for three slots in
+// LDS, and blocks of 16 tokens instead read W again (64 tokens of 8 experts, both products in such
+// blocks, 182 instead of 151 us), which is why it is not done.
 //
 // The weights of the experts in use are what there is to read, once, and what the time goes into: 2 experts of 4096 and 14336 in 4 bits, 187 MB, take 42 us
 // (4.5 TB/s), 8 of them and 64 tokens 154 (4.9).  Every wavefront streams its rows through a ring of its own (see gemm_rows.hpp), K tiles of 128 bytes

@@ -79,3 +79,14 @@ def test_moe_forward(T, N, k, d, f, mx4):
     Wg = randn((d, N), g, d ** -0.5, torch.float32)
     out, idx, w = m.moe_forward(x, Wg, None, *layer.weights, k, **layer.scales, scale=0.5, base=base, return_routing=True)
     close(out, layer, x, idx, w, scale=0.5, base=base)
+
+
+@pytest.mark.parametrize("T", [1, 4, 16, 64])
+@pytest.mark.parametrize("d,N", [(64, 6), (1000, 28), (8192, 8), (8200, 64)])
+def test_equal_columns_go_to_the_lowest_index(T, d, N):
+    """Of columns of the gate that are equal the first ones are chosen, whatever order a batch's sums are in."""
+    g = gen(T + d)
+    layer, x = Layer(N, d, 32, False, g), randn((T, d), g)
+    Wg = randn((d, 2), g, d ** -0.5, torch.float32)[:, torch.arange(N, device="cuda") % 2].contiguous()
+    _, idx, w = m.moe_forward(x, Wg, None, *layer.weights, 2, return_routing=True)
+    assert (idx == idx[:, :1] % 2 + torch.tensor([0, 2], device="cuda")).all() and (idx[:, 0] < 2).all() and (w == 0.5).all()

@@ -55,3 +55,20 @@ def test_fp32_batches():
     at = torch.tensor([0, 33, 4095, 8159, 8191, 8192, 8193, T - 1], device="cuda")
     gc.close(dx[at], gc.reference(dy[at], V, torch.float32, True))
     assert (dx[T] == 7).all() and (dx[:T:40] != 0).any(1).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_groups_one_by_one(dtype):
+    """The gradient of a product over groups with respect to its rows: a call for every group that has some."""
+    g = gen(33)
+    bounds, d_in, d_out = [0, 7, 7, 300, 333], 352, 136
+    parts = [operand(d_out, d_in, g) for _ in range(4)]
+    W, ws = torch.stack([p[0] for p in parts]), torch.stack([p[1] for p in parts])
+    dy = torch.randn((340, d_out), generator=g, device="cuda").to(dtype)
+    dx = torch.full((340, d_in), 7.0, device="cuda", dtype=dtype)
+    for e, (a, b) in enumerate(zip(bounds, bounds[1:])):
+        if b > a:
+            m.base_gemm_mx4_backward(dy[a:b], W[e], ws[e], out=dx[a:b])
+            codes = from_codes(b - a, d_in, d_out, dtype)
+            gc.close(dx[a:b], gc.reference(dy[a:b], parts[e][2], dtype, codes))
+    assert (dx[bounds[-1]:] == 7).all()
