@@ -8,7 +8,7 @@
 // the operand of the second product; sums are fp32.  That rounding takes the output's error from 0.0017 of the output, which is its own rounding, to 0.0023.  h as two
 // bf16 parts would do without it and double the columns of the second product: 32 tokens' K tiles of 4 bits would no longer leave room for three slots in
 // LDS, and blocks of 16 tokens instead read W again (64 tokens of 8 experts, both products in such
-// blocks, 182 instead of 151 us), which is why it is not done.
+// blocks, 174 instead of 150 us), which is why it is not done.
 //
 // The weights of the experts in use are what there is to read, once, and what the time goes into: 2 experts of 4096 and 14336 in 4 bits, 187 MB, take 42 us
 // (4.5 TB/s), 8 of them and 64 tokens 154 (4.9).  Every wavefront streams its rows through a ring of its own (see gemm_rows.hpp), K tiles of 128 bytes
@@ -665,9 +665,9 @@ static_assert(kManyThreads >= kExpertsMaxTokens * kMaxTopK, "a pair to a thread"
 // us.  A K tile of w wavefronts took, 4 bits and blocks of 16 tokens (20 tokens of 16 experts, 4096 and 2048 wide), 0.54, 0.57, 0.62, 0.69, 0.85, 0.91,
 // 0.94, 1.24 us for w = 1 to 8, and with blocks of 32 (64 tokens of 8 experts, 4096 and 14336) 0.70, 0.74, 0.83, 0.97, 1.25, 1.32, 1.45, 1.6.
 // Calls of 33 tokens of 28 experts, 2080 and 1376 wide, with w = 4, 5 and 8 for the first product 51.6, 49.4, 55.5; of 64 of 8, 4096 and 14336, w = 4, 7, 8
-// 166, 150, 159, and the second product with w = 8 whole and in two and four parts 180, 152, 154.  In bf16 K tiles are shorter by about the same share for all w,
-// so that one model does for both kinds of weights and blocks: over 16 calls of 6 to 64 tokens of 4 to 64 experts the best of all w and parts takes 0 to 4 %
-// less than the choice in 4 bits and 0 to 6 % in bf16 (13 tokens of 8 experts, 4096 and 3584: 125 us, and 119 with w = 2).
+// 166, 150, 159, and the second product with w = 8 whole and in two and four parts 180, 152, 154.  The model is that of 4 bits
+// for both kinds of weights: of 16 calls of 6 to 64 tokens of 4 to 64 experts the best of all w and parts takes 0 to 2 % less than the choice in 4 bits and 0 to 8 % in
+// bf16, where fewer wavefronts would do (first product of 13 tokens of 8 experts, 4096 and 3584, 129 us, with w = 2 119; 32 tokens 127 and 120).
 struct Tiling { int waves, splits; };
 __device__ __forceinline__ Tiling choose_tiling(int blocks, int units, int nk, bool may_split, int lane) {   // a wavefront; units: of channels
     const int w = (lane & 7) + 1, splits = 1 << (lane >> 3 & 3);
@@ -1067,9 +1067,9 @@ static hipError_t launch(ExpertsArgs a, hipStream_t stream) {
     }
     if (few) return launch_few<WT>(a, stream);
     // Blocks of 16 or of 32 tokens, us.  4 bits: 64 tokens of 2 of 8 experts of 4096 and 3584 62.0 and 49.9, 32 tokens 43.6 and 48.6; 64 of 2 of 8 of 4096 and 14336
-    // 182 and 151; 48 of 2 of 4 of 4096 42.7 and 40.3; 33 of 4 of 28 of 2080 and 1376 45.0 and 50.7; 64 of 2 of 64 of 1024 29.4 and 32.5.  bf16: 64 of 2 of 8 of 4096
-    // and 3584 152 and 128, 32 tokens 127 and 128; 48 of 2 of 4 of 4096 and 2048 55.8 and 50.2; 20 of 2 of 16 of 4096 and 1024 79.2 and 78.3; of 4 of 28 of 2048 and
-    // 1024, 64 tokens, where the rule takes 16, 76.9 and 72.7.
+    // 174 and 150; 48 of 2 of 4 of 4096 41.3 and 38.5; 33 of 4 of 28 of 2080 and 1376 43.4 and 49.8; 64 of 2 of 64 of 1024 28.6 and 32.0.  bf16: 64 of 2 of 8 of 4096
+    // and 3584 145 and 127, 32 tokens 127 and 127; 48 of 2 of 4 of 4096 and 2048 54.6 and 49.7; 20 of 2 of 16 of 4096 and 1024 78.5 and 78.2; 64 of 4 of 28 of 2048 and
+    // 1024 75.9 and 76.1.
     return a.T * a.k <= 10 * a.N || a.T <= 16 ? launch_many<WT, 1>(a, stream) : launch_many<WT, 2>(a, stream);
 }
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t stream) {
